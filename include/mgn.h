@@ -59,6 +59,10 @@ typedef enum {
                     paper's section "Performance Study") */
 } mgn_precision;
 
+/* Storage types of the row and time operators below: MGN_FP32, MGN_BF16 and,
+ * where it says so, 8-bit rows. */
+#define MGN_E4M3 2
+
 typedef struct {
   int32_t latent;    /* l: 64, 128 or 256 */
   int32_t n_blocks;  /* K >= 0 message-passing blocks */
@@ -218,6 +222,102 @@ mgn_status mgn_norm_accumulate(const float* x, int64_t rows, int32_t cols, doubl
 mgn_status mgn_norm_apply(const float* x, int64_t rows, int32_t cols, const double* stats, double eps, float* out,
                           mgn_stream stream);
 
+/* ---- node rows outside the network: 8 bits, norm ----
+ *
+ * Device arrays of rows [n][cols], 1 <= cols <= MGN_ROW_MAX_COLS, contiguous
+ * and aligned to their type (fp32 4 bytes, bf16 2); row counts are 64-bit.
+ * Asynchronous on `stream`, no allocation, no atomics; the same inputs give the
+ * same bits.  MGN_E_ARG for sizes or types outside what is stated, a NULL or
+ * misaligned pointer, or arrays that overlap where it is not allowed.
+ *
+ * 8-bit rows are codes q [slots][cols] (one e4m3 byte a column: 4 exponent
+ * bits, 3 of mantissa, largest value 448, no infinity) and scale
+ * [slots][ceil(cols / MGN_ROWS8_BLOCK)] (fp32, one for each block of 128
+ * columns, the last may be shorter); a code stands for its value times its
+ * block's scale.  The scales written here are the least power of two (at least
+ * 2^-126; 1 for a block of zeros) that brings the block's largest finite
+ * magnitude to 448 or less, so each value is rounded once, to nearest even, and
+ * rows stored, read back and stored again are the same bytes.  An infinity is
+ * stored as +-448 times the scale, a NaN as a NaN; neither changes the scale of
+ * its neighbours. */
+#define MGN_ROW_MAX_COLS 8192
+#define MGN_ROWS8_BLOCK 128
+/* Stores rows in 8 bits: slot slots[i] takes row src_rows[i] of src
+ * [n_src][cols] (src_type MGN_FP32 or MGN_BF16), i < n.  NULL index arrays mean
+ * i itself (then n must not exceed n_src or n_slots).  Pairs with an index
+ * outside [0, n_src) or [0, n_slots) are skipped; slots must be distinct within
+ * one call; slots that no pair names keep what they hold. */
+mgn_status mgn_rows_store8(const void* src, int32_t src_type, int64_t n_src, int32_t cols, const int32_t* src_rows,
+                           const int32_t* slots, int64_t n, uint8_t* q, float* scale, int64_t n_slots,
+                           mgn_stream stream);
+/* Reads 8-bit rows back: row dst_rows[i] of dst [n_dst][cols] (dst_type
+ * MGN_FP32 or MGN_BF16) takes the values of slot slots[i], i < n; with add != 0
+ * it takes the sum of them and of what it held (MGN_FP32 only).  Indices as
+ * above (dst_rows distinct within one call); any finite scale is allowed. */
+mgn_status mgn_rows_load8(const uint8_t* q, const float* scale, int64_t n_slots, int32_t cols, const int32_t* slots,
+                          const int32_t* dst_rows, int64_t n, void* dst, int32_t dst_type, int64_t n_dst, int32_t add,
+                          mgn_stream stream);
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   t = x + res;  y = t / sqrt(mean(t^2) + eps) * weight.
+ * x, res (NULL: none) and total (NULL: not stored) have storage type `type`
+ * (MGN_FP32 or MGN_BF16); y has y_type, with MGN_E4M3 8-bit rows in y and
+ * y_scale (NULL otherwise).  weight: fp32 [cols], or NULL for ones.  Sums are
+ * taken in fp32 and y from the unrounded t.  total may be x or res, and y may
+ * be x or res if it has their type and total is not that array too; no other
+ * overlap.  A row whose squares pass the fp32 range gives zeros, a NaN or an
+ * infinity in a row NaNs there.  eps > 0 and finite. */
+mgn_status mgn_rms_norm(const void* x, const void* res, int32_t type, int64_t rows, int32_t cols, const float* weight,
+                        float eps, void* total, void* y, int32_t y_type, float* y_scale, mgn_stream stream);
+/* Its backward: total [rows][cols] is the sum that was normalised (x itself
+ * without a residual), dy = dL/dy (8-bit rows: of the values before their
+ * rounding), d_total (NULL: none) a gradient that reaches total on another way
+ * (the residual stream).  dx receives the whole gradient of total, which is
+ * that of x and of res alike; it may be dy, d_total or total.  All of `type`.
+ * dweight (fp32 [cols], NULL: not wanted) is overwritten, or added to when
+ * accumulate != 0; work is a device scratch array of MGN_RMS_WORK_PER_COL * cols
+ * floats, overwritten (NULL allowed without dweight). */
+#define MGN_RMS_WORK_PER_COL 1024
+mgn_status mgn_rms_norm_grad(const void* total, int32_t type, const float* weight, float eps, const void* dy,
+                             const void* d_total, int64_t rows, int32_t cols, void* dx, float* dweight,
+                             int32_t accumulate, float* work, mgn_stream stream);
+
+/* ---- along time: gated linear recurrence ----
+ *
+ * Every column of every row carries a state over the steps of a trajectory
+ * (section "Model": next-step prediction; section "Results": rollouts of
+ * hundreds of steps and their temporal means):
+ *   f_t = sigmoid(g_t), z_t = 1 - f_t;   h_t = f_t h_{t-1} + z_t x_t,
+ * h_{-1} = h0 (NULL: zeros).  g_t = log(t) makes h the running mean of x.
+ * g, x [steps][rows][cols] of one storage type (MGN_FP32 or MGN_BF16), or x as
+ * 8-bit rows (x_type MGN_E4M3, codes in x, x_scale
+ * [steps][rows][ceil(cols / 128)]).  starts [steps] (NULL: none): a nonzero
+ * entry begins a trajectory, its step takes 0 for h_{t-1}.  States are fp32: h
+ * [steps][rows][cols] (NULL: not stored), h_last [rows][cols] = the last state
+ * (NULL: not wanted; it may be h0, so that a rollout's step updates its state
+ * in place; with no steps it is h0).  A weight f or z below 2^-126 counts as 0
+ * and its term is left out whatever it multiplies: g = +inf (or the type's
+ * largest value) holds a state through steps whose x is not defined, -inf
+ * replaces it.
+ * work: device scratch of mgn_gated_scan_work bytes, 16-byte aligned (NULL
+ * when that is 0); MGN_E_NOMEM when work_bytes is less.  steps, rows >= 0,
+ * 1 <= cols <= MGN_ROW_MAX_COLS.  Arrays must not overlap beyond what is
+ * stated; otherwise as the rows above. */
+mgn_status mgn_gated_scan_work(int64_t steps, int64_t rows, int32_t cols, size_t* bytes);
+mgn_status mgn_gated_scan(const void* g, int32_t g_type, const void* x, int32_t x_type, const float* x_scale,
+                          const uint8_t* starts, const float* h0, int64_t steps, int64_t rows, int32_t cols, float* h,
+                          float* h_last, void* work, size_t work_bytes, mgn_stream stream);
+/* Its backward, from the forward's arguments and its h: dh [steps][rows][cols]
+ * = dL/dh (NULL: zeros), dh_last [rows][cols] = dL/dh_last (NULL: zeros), both
+ * fp32.  dg receives dL/dg in g's type, dx dL/dx in x's type (g's for 8-bit x:
+ * of the values the codes stand for), dh0 (NULL: not wanted; it may be
+ * dh_last, so that windows of a long trajectory hand it on) dL/dh0 in fp32.
+ * A term left out in the forward has no gradient. */
+mgn_status mgn_gated_scan_grad(const void* g, int32_t g_type, const void* x, int32_t x_type, const float* x_scale,
+                               const uint8_t* starts, const float* h0, const float* h, const float* dh,
+                               const float* dh_last, int64_t steps, int64_t rows, int32_t cols, void* dg, void* dx,
+                               float* dh0, void* work, size_t work_bytes, mgn_stream stream);
+
 /* Device workspace mgn_forward/mgn_backward need for graph g (bytes) under
  * the model's checkpointing setting.  For a forward-only fp32 plan with a halo
  * this includes 4 * latent bytes per halo node that mgn_forward can do without
@@ -341,6 +441,20 @@ mgn_status mgn_copy_latents(const mgn_model* owner, const int32_t* send_rows, co
 mgn_status mgn_add_latent_grads(mgn_model* owner, const float* d_halo_k, int64_t n_halo, const int32_t* recv_idx,
                                 const int32_t* send_rows, int64_t n, mgn_stream stream);
 
+/* The exchange in 8 bits (a quarter of the bytes between the parts): the
+ * forward's owner packs its latents into slots 0 .. n-1 of q [n][latent] and
+ * scale [n][ceil(latent / 128)], which are what is sent; the holder reads them
+ * back with mgn_rows_load8 into halo[k].  cols, the columns of a slot, must be
+ * the model's latent size.  v as in mgn_copy_latents; a row outside [0, n_owned)
+ * leaves its slot as it was. */
+mgn_status mgn_pack_latents8(const mgn_model* owner, const int32_t* send_rows, int64_t n, uint8_t* q, float* scale,
+                             int32_t cols, mgn_stream stream);
+/* And its backward: the holder packs the rows recv_idx of its d_halo block with
+ * mgn_rows_store8; the owner adds slots 0 .. n-1 to rows send_rows of its dL/dv
+ * (as mgn_add_latent_grads does with fp32 rows; send_rows distinct). */
+mgn_status mgn_add_latent_grads8(mgn_model* owner, const uint8_t* q, const float* scale, int32_t cols,
+                                 const int32_t* send_rows, int64_t n, mgn_stream stream);
+
 /* One exchange list of a lockstep step (device index arrays, n entries, from
  * mgn_halo_masks): the halo rows recv_idx of part `part` are the node rows
  * send_rows of part `owner`. */
@@ -363,6 +477,15 @@ mgn_status mgn_lockstep_forward(int32_t n_parts, mgn_model* const* models, const
                                 const float* const* node_feat, const float* const* edge_feat, float* const* halo,
                                 float* const* out, void* const* workspace, const size_t* ws_bytes,
                                 const mgn_halo_link* links, int32_t n_links, mgn_stream stream);
+/* The same with every exchange in 8 bits (mgn_pack_latents8, mgn_rows_load8).
+ * q and scale are device scratch of slots rows (slots >= every link's n, of
+ * cols = latent bytes and ceil(cols / 128) floats each), used by link after link in
+ * stream order. */
+mgn_status mgn_lockstep_forward8(int32_t n_parts, mgn_model* const* models, const mgn_graph* graphs,
+                                 const float* const* node_feat, const float* const* edge_feat, float* const* halo,
+                                 float* const* out, void* const* workspace, const size_t* ws_bytes,
+                                 const mgn_halo_link* links, int32_t n_links, uint8_t* q, float* scale, int64_t slots,
+                                 int32_t cols, mgn_stream stream);
 /* The staged backward of the same parts: every part's decoder backward;
  * for k = K-1 .. 0 every part's block backward, then every link's
  * mgn_add_latent_grads from d_halo[part]; every part's encoder backward.
@@ -372,6 +495,12 @@ mgn_status mgn_lockstep_forward(int32_t n_parts, mgn_model* const* models, const
 mgn_status mgn_lockstep_backward(int32_t n_parts, mgn_model* const* models, const float* const* d_out,
                                  float* d_params, int accumulate, float* const* d_halo, const mgn_halo_link* links,
                                  int32_t n_links, mgn_stream stream);
+/* The same with the halo gradients in 8 bits (mgn_rows_store8,
+ * mgn_add_latent_grads8); q, scale, slots as in mgn_lockstep_forward8. */
+mgn_status mgn_lockstep_backward8(int32_t n_parts, mgn_model* const* models, const float* const* d_out,
+                                  float* d_params, int accumulate, float* const* d_halo, const mgn_halo_link* links,
+                                  int32_t n_links, uint8_t* q, float* scale, int64_t slots, int32_t cols,
+                                  mgn_stream stream);
 
 /* Masked mean squared error (Algorithm 1: local squared error, mean over the
  * loss-masked nodes and outputs) and its gradient, device pointers:

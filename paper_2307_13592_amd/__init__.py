@@ -16,7 +16,7 @@ import numpy as np
 from . import build as _build
 
 MGN_OK, MGN_E_ARG, MGN_E_GRAPH, MGN_E_STATE, MGN_E_NOMEM, MGN_E_HIP, MGN_E_UNSUPPORTED = range(7)
-MGN_FP32, MGN_BF16 = 0, 1
+MGN_FP32, MGN_BF16, MGN_E4M3 = 0, 1, 2
 STATUS_NAMES = ["MGN_OK", "MGN_E_ARG", "MGN_E_GRAPH", "MGN_E_STATE", "MGN_E_NOMEM", "MGN_E_HIP", "MGN_E_UNSUPPORTED"]
 
 # every symbol include/mgn.h declares
@@ -28,7 +28,10 @@ EXPORTS = ["mgn_create", "mgn_destroy", "mgn_last_error", "mgn_param_count", "mg
            "mgn_forward", "mgn_backward", "mgn_forward_begin", "mgn_forward_block", "mgn_forward_end",
            "mgn_backward_begin", "mgn_backward_block", "mgn_backward_end", "mgn_halo_masks", "mgn_copy_latents",
            "mgn_add_latent_grads", "mgn_lockstep_forward", "mgn_lockstep_backward", "mgn_mse_grad",
-           "mgn_mse_grad_global", "mgn_timing_enable", "mgn_timing_read", "mgn_forward_noalloc"]
+           "mgn_mse_grad_global", "mgn_timing_enable", "mgn_timing_read", "mgn_forward_noalloc",
+           "mgn_rows_store8", "mgn_rows_load8", "mgn_rms_norm", "mgn_rms_norm_grad", "mgn_gated_scan_work",
+           "mgn_gated_scan", "mgn_gated_scan_grad", "mgn_pack_latents8", "mgn_add_latent_grads8",
+           "mgn_lockstep_forward8", "mgn_lockstep_backward8"]
 TIMERS = ["encode", "edge_fwd", "node_fwd", "decode", "edge_bwd", "node_bwd", "input_grad", "weight_grad",
           "other", "node_proj", "exchange"]
 
@@ -101,6 +104,18 @@ def lib() -> C.CDLL:
             "mgn_add_latent_grads": (C.c_int, [vp, vp, i64, vp, vp, i64, vp]),
             "mgn_lockstep_forward": (C.c_int, [i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
             "mgn_lockstep_backward": (C.c_int, [i32, vp, vp, vp, C.c_int, vp, vp, i32, vp]),
+            "mgn_rows_store8": (C.c_int, [vp, i32, i64, i32, vp, vp, i64, vp, vp, i64, vp]),
+            "mgn_rows_load8": (C.c_int, [vp, vp, i64, i32, vp, vp, i64, vp, i32, i64, i32, vp]),
+            "mgn_rms_norm": (C.c_int, [vp, vp, i32, i64, i32, vp, C.c_float, vp, vp, i32, vp, vp]),
+            "mgn_rms_norm_grad": (C.c_int, [vp, i32, vp, C.c_float, vp, vp, i64, i32, vp, vp, i32, vp, vp]),
+            "mgn_gated_scan_work": (C.c_int, [i64, i64, i32, vp]),
+            "mgn_gated_scan": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i64, i64, i32, vp, vp, vp, C.c_size_t, vp]),
+            "mgn_gated_scan_grad": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, vp, vp,
+                                              C.c_size_t, vp]),
+            "mgn_pack_latents8": (C.c_int, [vp, vp, i64, vp, vp, i32, vp]),
+            "mgn_add_latent_grads8": (C.c_int, [vp, vp, vp, i32, vp, i64, vp]),
+            "mgn_lockstep_forward8": (C.c_int, [i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i64, i32, vp]),
+            "mgn_lockstep_backward8": (C.c_int, [i32, vp, vp, vp, C.c_int, vp, vp, i32, vp, vp, i64, i32, vp]),
             "mgn_mse_grad": (C.c_int, [vp, vp, vp, i64, i32, vp, vp, vp]),
             "mgn_mse_grad_global": (C.c_int, [vp, vp, vp, i64, i32, i64, vp, vp, vp]),
             "mgn_timing_enable": (C.c_int, [vp, C.c_int]),
@@ -301,6 +316,194 @@ def mgn_rollout_update(out, node_feat, col0: int = 3, stream=None) -> None:
                                     _stream(stream)))
 
 
+MGN_ROW_MAX_COLS = 8192
+MGN_ROWS8_BLOCK = 128
+MGN_RMS_WORK_PER_COL = 1024
+
+
+def rows8_blocks(cols: int) -> int:
+    """Scales of an 8-bit row of `cols` columns."""
+    return -(-cols // MGN_ROWS8_BLOCK)
+
+
+def _type(t, name: str, e4m3: bool = False) -> int:
+    """Storage type of a row array from its torch dtype (uint8: 8-bit codes)."""
+    import torch
+    if t is None:
+        raise ValueError(f"{name}: expected a device tensor, got None")
+    if t.dtype == torch.float32:
+        return MGN_FP32
+    if t.dtype == torch.bfloat16:
+        return MGN_BF16
+    if e4m3 and t.dtype == torch.uint8:
+        return MGN_E4M3
+    raise ValueError(f"{name}: unsupported storage type {t.dtype}")
+
+
+def _rows(t, name: str):
+    if t is None or t.dim() != 2:
+        raise ValueError(f"{name}: expected [rows][cols]")
+    return t.shape
+
+
+def _opt(t, dtype, name: str, **kw):
+    return None if t is None else _devt(t, dtype, name, **kw)
+
+
+def _call(fn: str, stream, first, *rest):
+    """Calls the entry point `fn`(*args, stream) on the device of its tensors:
+    returns a function of the arguments.  All tensors lie on one device; the
+    default stream is that device's current one."""
+    import torch
+    dev = first.device
+    for t in rest:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{fn}: tensors on different devices ({dev} and {t.device})")
+    f = getattr(lib(), fn)
+    if not first.is_cuda or dev.index == torch.cuda.current_device():
+        return lambda *args: _check(f(*args, _stream(stream)))
+
+    def on_device(*args):
+        with torch.cuda.device(dev):
+            _check(f(*args, _stream(stream)))
+    return on_device
+
+
+def _scratch(nbytes: int, device, stream):
+    """Device scratch for one call on `stream`: from torch's allocator, on that
+    stream, so that it is not handed out again before the call has run (and
+    belongs to a HIP graph that records the call)."""
+    import torch
+    if nbytes == 0:
+        return None
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def mgn_rows_store8(src, q, scale, src_rows=None, slots=None, stream=None) -> None:
+    """Stores rows of src (device float32 or bfloat16 [n_src][cols]) in 8 bits:
+    slot slots[i] of q (uint8 [n_slots][cols]) and scale (float32
+    [n_slots][rows8_blocks(cols)]) takes row src_rows[i].  src_rows, slots:
+    int32 device tensors of one length, or None for 0, 1, 2, ...; without
+    either, every row of src is stored."""
+    import torch
+    n_src, cols = _rows(src, "src")
+    n_slots = _rows(q, "q")[0]
+    n = src_rows.numel() if src_rows is not None else slots.numel() if slots is not None else n_src
+    call = _call("mgn_rows_store8", stream, src, q, scale, src_rows, slots)
+    call(_devt(src, src.dtype, "src"), _type(src, "src"), n_src, cols, _opt(src_rows, torch.int32, "src_rows"),
+         _opt(slots, torch.int32, "slots", numel=n), n, _devt(q, torch.uint8, "q", shape=(n_slots, cols)),
+         _devt(scale, torch.float32, "scale", shape=(n_slots, rows8_blocks(cols))), n_slots)
+
+
+def mgn_rows_load8(q, scale, dst, slots=None, dst_rows=None, add: bool = False, stream=None) -> None:
+    """Reads 8-bit rows back: row dst_rows[i] of dst (device float32 or
+    bfloat16 [n_dst][cols]) takes the values of slot slots[i] (add: the sum of
+    them and of what it holds, float32 only).  Without index tensors every
+    slot is read."""
+    import torch
+    n_slots, cols = _rows(q, "q")
+    n_dst = _rows(dst, "dst")[0]
+    n = dst_rows.numel() if dst_rows is not None else slots.numel() if slots is not None else n_slots
+    call = _call("mgn_rows_load8", stream, q, scale, dst, slots, dst_rows)
+    call(_devt(q, torch.uint8, "q"), _devt(scale, torch.float32, "scale", shape=(n_slots, rows8_blocks(cols))), n_slots,
+         cols, _opt(slots, torch.int32, "slots", numel=n), _opt(dst_rows, torch.int32, "dst_rows", numel=n), n,
+         _devt(dst, dst.dtype, "dst", shape=(n_dst, cols)), _type(dst, "dst"), n_dst, int(bool(add)))
+
+
+def mgn_rms_norm(x, weight, y, res=None, total=None, y_scale=None, eps: float = 1e-6, stream=None) -> None:
+    """y = t / sqrt(mean(t^2) + eps) * weight for t = x + res, rows of device
+    tensors.  x, res, total: float32 or bfloat16, one type; total takes t.  y:
+    float32, bfloat16, or uint8 for 8-bit rows with their scales in y_scale.
+    weight: float32 [cols] or None."""
+    import torch
+    rows, cols = _rows(x, "x")
+    yt = _type(y, "y", e4m3=True)
+    call = _call("mgn_rms_norm", stream, x, weight, y, res, total, y_scale)
+    call(_devt(x, x.dtype, "x"), _opt(res, x.dtype, "res", shape=(rows, cols)), _type(x, "x"), rows, cols,
+         _opt(weight, torch.float32, "weight", numel=cols), C.c_float(eps),
+         _opt(total, x.dtype, "total", shape=(rows, cols)), _devt(y, y.dtype, "y", shape=(rows, cols)), yt,
+         _opt(y_scale, torch.float32, "y_scale", shape=(rows, rows8_blocks(cols))))
+
+
+def mgn_rms_norm_grad(total, weight, dy, dx, dweight=None, d_total=None, accumulate: bool = False, work=None,
+                      eps: float = 1e-6, stream=None) -> None:
+    """Backward of mgn_rms_norm: dx (the gradient of x and of res) and dweight
+    (float32 [cols], overwritten or added to) from the normalised sum `total`,
+    dy and the gradient d_total that reaches the sum otherwise.  work: float32
+    scratch of MGN_RMS_WORK_PER_COL * cols for dweight (None: allocated)."""
+    import torch
+    rows, cols = _rows(total, "total")
+    call = _call("mgn_rms_norm_grad", stream, total, weight, dy, dx, dweight, d_total, work)
+    pt = _devt(total, total.dtype, "total")
+    if dweight is not None and work is None:
+        work = _scratch(4 * MGN_RMS_WORK_PER_COL * cols, total.device, stream)
+        pw = _dev(work)
+    else:
+        pw = _opt(work, torch.float32, "work", min_numel=MGN_RMS_WORK_PER_COL * cols)
+    call(pt, _type(total, "total"), _opt(weight, torch.float32, "weight", numel=cols), C.c_float(eps),
+         _devt(dy, total.dtype, "dy", shape=(rows, cols)), _opt(d_total, total.dtype, "d_total", shape=(rows, cols)),
+         rows, cols, _devt(dx, total.dtype, "dx", shape=(rows, cols)),
+         _opt(dweight, torch.float32, "dweight", numel=cols), int(bool(accumulate)), pw)
+
+
+def mgn_gated_scan_work(steps: int, rows: int, cols: int) -> int:
+    """Bytes of device scratch mgn_gated_scan and its backward need."""
+    n = C.c_size_t()
+    _check(lib().mgn_gated_scan_work(int(steps), int(rows), int(cols), C.byref(n)))
+    return int(n.value)
+
+
+def _scan_args(g, x, x_scale, starts, h0, work, stream):
+    """Marshalled arguments the recurrence and its backward share."""
+    import torch
+    if g is None or g.dim() != 3:
+        raise ValueError("g: expected [steps][rows][cols]")
+    T, rows, cols = shape = tuple(g.shape)
+    xt = _type(x, "x", e4m3=True)
+    if xt != MGN_E4M3 and x.dtype != g.dtype:
+        raise ValueError(f"x: expected {g.dtype} (as g) or uint8 codes, got {x.dtype}")
+    need = mgn_gated_scan_work(T, rows, cols)
+    pg = _devt(g, g.dtype, "g")
+    if work is None:
+        work = _scratch(need, g.device, stream)
+    nb = 0 if work is None else work.numel() * work.element_size()
+    head = (pg, _type(g, "g"), _devt(x, x.dtype, "x", shape=shape), xt,
+            _opt(x_scale, torch.float32, "x_scale", shape=(T, rows, rows8_blocks(cols))),
+            _opt(starts, torch.uint8, "starts", shape=(T,)), _opt(h0, torch.float32, "h0", shape=(rows, cols)))
+    return shape, head, (_dev(work), nb), work
+
+
+def mgn_gated_scan(g, x, h=None, h_last=None, h0=None, starts=None, x_scale=None, work=None, stream=None) -> None:
+    """h_t = sigmoid(g_t) h_{t-1} + sigmoid(-g_t) x_t along the first axis of
+    device tensors [steps][rows][cols].  g, x: float32 or bfloat16, or x uint8
+    codes with x_scale; h (all states) and h_last (the last; it may be h0):
+    float32, either may be None; starts: uint8 [steps].  work: device scratch of
+    mgn_gated_scan_work bytes (None: allocated)."""
+    import torch
+    (T, rows, cols), head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
+    call = _call("mgn_gated_scan", stream, g, x, x_scale, starts, h0, h, h_last, keep)
+    call(*head, T, rows, cols, _opt(h, torch.float32, "h", shape=(T, rows, cols)),
+         _opt(h_last, torch.float32, "h_last", shape=(rows, cols)), *tail)
+
+
+def mgn_gated_scan_grad(g, x, h, dg, dx, dh=None, dh_last=None, dh0=None, h0=None, starts=None, x_scale=None,
+                        work=None, stream=None) -> None:
+    """Backward of mgn_gated_scan from its arguments, its h and the float32
+    gradients dh [steps][rows][cols] and dh_last [rows][cols]: dg (g's type), dx
+    (x's type; g's for 8-bit x) and dh0 (float32, or None; it may be dh_last)."""
+    import torch
+    shape, head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
+    T, rows, cols = shape
+    call = _call("mgn_gated_scan_grad", stream, g, x, x_scale, starts, h0, h, dg, dx, dh, dh_last, dh0, keep)
+    call(*head, _devt(h, torch.float32, "h", shape=shape), _opt(dh, torch.float32, "dh", shape=shape),
+         _opt(dh_last, torch.float32, "dh_last", shape=(rows, cols)), T, rows, cols,
+         _devt(dg, g.dtype, "dg", shape=shape), _devt(dx, g.dtype, "dx", shape=shape),
+         _opt(dh0, torch.float32, "dh0", shape=(rows, cols)), *tail)
+
+
 def mgn_workspace_size(model, graph: mgn_graph) -> int:
     n = C.c_size_t()
     _check(lib().mgn_workspace_size(model, C.byref(graph), C.byref(n)), model)
@@ -382,9 +585,45 @@ def mgn_add_latent_grads(owner, d_halo_k, recv_idx, send_rows, stream=None) -> N
                                       _dev(send_rows), int(send_rows.numel()), _stream(stream)), owner)
 
 
+def _slots8(q, scale):
+    """8-bit slots of an exchange: (q, scale, slots, cols)."""
+    import torch
+    slots, cols = _rows(q, "q")
+    return (_devt(q, torch.uint8, "q"), _devt(scale, torch.float32, "scale", shape=(slots, rows8_blocks(cols))), slots,
+            cols)
+
+
+def mgn_pack_latents8(owner, send_rows, q, scale, stream=None) -> None:
+    """Slots 0 .. n-1 of q (uint8 [slots][latent]) and scale take the owner's
+    current node latents[send_rows] in 8 bits (device tensors)."""
+    import torch
+    n = send_rows.numel()
+    pq, ps, slots, cols = _slots8(q, scale)
+    if slots < n:
+        raise ValueError("q: expected at least as many slots as send_rows")
+    _check(lib().mgn_pack_latents8(owner, _devt(send_rows, torch.int32, "send_rows"), n, pq, ps, cols,
+                                   _stream(stream)), owner)
+
+
+def mgn_add_latent_grads8(owner, q, scale, send_rows, stream=None) -> None:
+    """owner's dL/dv[send_rows[i]] += the values of slot i (device tensors)."""
+    import torch
+    n = send_rows.numel()
+    pq, ps, slots, cols = _slots8(q, scale)
+    if slots < n:
+        raise ValueError("q: expected at least as many slots as send_rows")
+    _check(lib().mgn_add_latent_grads8(owner, pq, ps, cols, _devt(send_rows, torch.int32, "send_rows"), n,
+                                       _stream(stream)), owner)
+
+
 def _ptrs(ts):
     """C array of device pointers (NULL for None)."""
     return (C.c_void_p * len(ts))(*[None if t is None else t.data_ptr() for t in ts])
+
+
+def _links(links):
+    return (mgn_halo_link * max(len(links), 1))(*[mgn_halo_link(p, q, r.data_ptr(), s.data_ptr(), r.numel())
+                                                  for p, q, r, s in links])
 
 
 def mgn_lockstep_forward(models, graphs, node_feats, edge_feats, halos, outs, workspaces, links,
@@ -394,21 +633,42 @@ def mgn_lockstep_forward(models, graphs, node_feats, edge_feats, halos, outs, wo
     P = len(models)
     ms = (C.c_void_p * P)(*[m.value for m in models])
     gs = (mgn_graph * P)(*graphs)
-    lk = (mgn_halo_link * max(len(links), 1))(*[mgn_halo_link(p, q, r.data_ptr(), s.data_ptr(), r.numel())
-                                                 for p, q, r, s in links])
     wb = (C.c_size_t * P)(*[w.numel() * w.element_size() for w in workspaces])
     st = lib().mgn_lockstep_forward(P, ms, gs, _ptrs(node_feats), _ptrs(edge_feats), _ptrs(halos), _ptrs(outs),
-                                    _ptrs(workspaces), wb, lk, len(links), _stream(stream))
+                                    _ptrs(workspaces), wb, _links(links), len(links), _stream(stream))
+    _check(st)
+
+
+def mgn_lockstep_forward8(models, graphs, node_feats, edge_feats, halos, outs, workspaces, links, q, scale,
+                          stream=None) -> None:
+    """mgn_lockstep_forward with every exchange in 8 bits; q (uint8
+    [slots][latent]), scale: device scratch of as many slots as the longest link."""
+    P = len(models)
+    ms = (C.c_void_p * P)(*[m.value for m in models])
+    gs = (mgn_graph * P)(*graphs)
+    wb = (C.c_size_t * P)(*[w.numel() * w.element_size() for w in workspaces])
+    st = lib().mgn_lockstep_forward8(P, ms, gs, _ptrs(node_feats), _ptrs(edge_feats), _ptrs(halos), _ptrs(outs),
+                                     _ptrs(workspaces), wb, _links(links), len(links), *_slots8(q, scale),
+                                     _stream(stream))
     _check(st)
 
 
 def mgn_lockstep_backward(models, d_outs, d_params, d_halos, links, accumulate: bool = False, stream=None) -> None:
     P = len(models)
     ms = (C.c_void_p * P)(*[m.value for m in models])
-    lk = (mgn_halo_link * max(len(links), 1))(*[mgn_halo_link(p, q, r.data_ptr(), s.data_ptr(), r.numel())
-                                                 for p, q, r, s in links])
     st = lib().mgn_lockstep_backward(P, ms, _ptrs(d_outs), _dev(d_params), int(bool(accumulate)), _ptrs(d_halos),
-                                     lk, len(links), _stream(stream))
+                                     _links(links), len(links), _stream(stream))
+    _check(st)
+
+
+def mgn_lockstep_backward8(models, d_outs, d_params, d_halos, links, q, scale, accumulate: bool = False,
+                           stream=None) -> None:
+    """mgn_lockstep_backward with the halo gradients in 8 bits (q, scale as in
+    mgn_lockstep_forward8)."""
+    P = len(models)
+    ms = (C.c_void_p * P)(*[m.value for m in models])
+    st = lib().mgn_lockstep_backward8(P, ms, _ptrs(d_outs), _dev(d_params), int(bool(accumulate)), _ptrs(d_halos),
+                                      _links(links), len(links), *_slots8(q, scale), _stream(stream))
     _check(st)
 
 

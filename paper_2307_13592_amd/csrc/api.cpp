@@ -1462,6 +1462,64 @@ mgn_status mgn_add_latent_grads(mgn_model* owner, const float* d_halo_k, int64_t
   return MGN_OK;
 }
 
+mgn_status mgn_pack_latents8(const mgn_model* owner, const int32_t* send_rows, int64_t n, uint8_t* q, float* scale,
+                             int32_t cols, mgn_stream stream) {
+  mgn_model* m = const_cast<mgn_model*>(owner);
+  if (!m) return fail(nullptr, MGN_E_ARG, "mgn_pack_latents8: model is NULL");
+  if (n < 0 || cols != m->L) return fail(m, MGN_E_ARG, "mgn_pack_latents8: bad sizes (cols is the latent size)");
+  if (n == 0) return MGN_OK;
+  if (!send_rows || !q || !scale) return fail(m, MGN_E_ARG, "mgn_pack_latents8: NULL argument");
+  if (!aligned(send_rows, 4) || !aligned(scale, 4))
+    return fail(m, MGN_E_ARG, "mgn_pack_latents8: misaligned pointer");
+  int j;
+  if (m->fwd_next >= 0)
+    j = m->fwd_next;
+  else if (m->fwd_done)
+    j = m->K;
+  else
+    return fail(m, MGN_E_STATE, "mgn_pack_latents8: the owner has no forward pass in progress or done");
+  const Views b(m);
+  Rows8Args a{};
+  a.x = b.V(j);
+  a.rows = send_rows;
+  a.q = q;
+  a.scale = scale;
+  a.n = a.n_slots = n;
+  a.n_rows = b.no;
+  a.cols = m->L;
+  Timed t_(m, MGN_T_EXCHANGE, (hipStream_t)stream);
+  hipError_t e = launch_rows_store8(a, MGN_FP32, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(m, e, "mgn_pack_latents8");
+  return MGN_OK;
+}
+
+mgn_status mgn_add_latent_grads8(mgn_model* owner, const uint8_t* q, const float* scale, int32_t cols,
+                                 const int32_t* send_rows, int64_t n, mgn_stream stream) {
+  mgn_model* m = owner;
+  if (!m) return fail(nullptr, MGN_E_ARG, "mgn_add_latent_grads8: model is NULL");
+  if (n < 0 || cols != m->L) return fail(m, MGN_E_ARG, "mgn_add_latent_grads8: bad sizes (cols is the latent size)");
+  if (!m->bwd_active || !m->fwd_done)
+    return fail(m, MGN_E_STATE, "mgn_add_latent_grads8: the owner has no backward pass in progress");
+  if (n == 0) return MGN_OK;
+  if (!q || !scale || !send_rows) return fail(m, MGN_E_ARG, "mgn_add_latent_grads8: NULL argument");
+  if (!aligned(send_rows, 4) || !aligned(scale, 4))
+    return fail(m, MGN_E_ARG, "mgn_add_latent_grads8: misaligned pointer");
+  const Views b(m);
+  Rows8Args a{};
+  a.out = b.ws + b.p.DV[m->bwd_a];
+  a.rows = send_rows;
+  a.q = const_cast<uint8_t*>(q);
+  a.scale = const_cast<float*>(scale);
+  a.n = a.n_slots = n;
+  a.n_rows = b.no;
+  a.cols = m->L;
+  a.add = 1;
+  Timed t_(m, MGN_T_EXCHANGE, (hipStream_t)stream);
+  hipError_t e = launch_rows_load8(a, MGN_FP32, (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(m, e, "mgn_add_latent_grads8");
+  return MGN_OK;
+}
+
 }  // extern "C"
 
 // Lockstep step of several parts on one device (one stream): the staged
@@ -1485,22 +1543,37 @@ mgn_status check_links(int32_t n_parts, mgn_model* const* models, const mgn_halo
   }
   return MGN_OK;
 }
-}  // namespace
+// Scratch of an exchange in 8 bits (q NULL: the exchange is in fp32).
+struct Slots8 {
+  uint8_t* q = nullptr;
+  float* scale = nullptr;
+};
 
-extern "C" {
+mgn_status check_slots(int32_t n_parts, mgn_model* const* models, const mgn_halo_link* links, int32_t n_links,
+                       const uint8_t* q, const float* scale, int64_t slots, int32_t cols, const char* fn) {
+  const std::string f(fn);
+  for (int32_t p = 0; models && p < n_parts; ++p)
+    if (slots < 0 || (models[p] && models[p]->L != cols))
+      return fail(nullptr, MGN_E_ARG, f + ": bad sizes (cols is the latent size)");
+  if (!q || !scale || !aligned(scale, 4)) return fail(nullptr, MGN_E_ARG, f + ": NULL or misaligned scratch");
+  for (int32_t i = 0; links && i < n_links; ++i)
+    if (links[i].n > slots)
+      return fail(nullptr, MGN_E_ARG, f + ": link " + std::to_string(i) + " has more rows than the scratch has slots");
+  return MGN_OK;
+}
 
-mgn_status mgn_lockstep_forward(int32_t n_parts, mgn_model* const* models, const mgn_graph* graphs,
-                                const float* const* node_feat, const float* const* edge_feat, float* const* halo,
-                                float* const* out, void* const* workspace, const size_t* ws_bytes,
-                                const mgn_halo_link* links, int32_t n_links, mgn_stream stream) {
-  mgn_status s = check_links(n_parts, models, links, n_links, halo, "mgn_lockstep_forward");
+mgn_status lockstep_forward(int32_t n_parts, mgn_model* const* models, const mgn_graph* graphs,
+                            const float* const* node_feat, const float* const* edge_feat, float* const* halo,
+                            float* const* out, void* const* workspace, const size_t* ws_bytes,
+                            const mgn_halo_link* links, int32_t n_links, Slots8 s8, hipStream_t st, const char* fn) {
+  const std::string f(fn);
+  mgn_status s = check_links(n_parts, models, links, n_links, halo, fn);
   if (s) return s;
   if (!graphs || !node_feat || !edge_feat || !out || !workspace || !ws_bytes)
-    return fail(nullptr, MGN_E_ARG, "mgn_lockstep_forward: NULL array");
-  hipStream_t st = (hipStream_t)stream;
+    return fail(nullptr, MGN_E_ARG, f + ": NULL array");
   for (int32_t p = 0; p < n_parts; ++p) {
     s = fwd_begin(models[p], &graphs[p], node_feat[p], edge_feat[p], halo ? halo[p] : nullptr, out[p], workspace[p],
-                  ws_bytes[p], st, "mgn_lockstep_forward");
+                  ws_bytes[p], st, fn);
     if (s) return s;
   }
   const int K = models[0]->K;
@@ -1509,39 +1582,47 @@ mgn_status mgn_lockstep_forward(int32_t n_parts, mgn_model* const* models, const
       const mgn_halo_link& ln = links[i];
       if (ln.n == 0) continue;
       const int64_t nh = graphs[ln.part].n_halo;
-      s = mgn_copy_latents(models[ln.owner], ln.send_rows, ln.recv_idx, ln.n,
-                           halo[ln.part] + (size_t)k * nh * models[ln.part]->L, nh, stream);
-      if (s) return fail(nullptr, s, std::string("mgn_lockstep_forward: ") + mgn_last_error(models[ln.owner]));
+      const int L = models[ln.part]->L;
+      float* hk = halo[ln.part] + (size_t)k * nh * L;
+      if (!s8.q) {
+        s = mgn_copy_latents(models[ln.owner], ln.send_rows, ln.recv_idx, ln.n, hk, nh, st);
+        if (s) return fail(nullptr, s, f + ": " + mgn_last_error(models[ln.owner]));
+        continue;
+      }
+      s = mgn_pack_latents8(models[ln.owner], ln.send_rows, ln.n, s8.q, s8.scale, L, st);
+      if (s) return fail(nullptr, s, f + ": " + mgn_last_error(models[ln.owner]));
+      Timed t_(models[ln.part], MGN_T_EXCHANGE, st);
+      s = mgn_rows_load8(s8.q, s8.scale, ln.n, L, nullptr, ln.recv_idx, ln.n, hk, MGN_FP32, nh, 0, st);
+      if (s) return s;
     }
     for (int32_t p = 0; p < n_parts; ++p) {
-      s = fwd_block(models[p], st, "mgn_lockstep_forward");
+      s = fwd_block(models[p], st, fn);
       if (s) return s;
     }
   }
   for (int32_t p = 0; p < n_parts; ++p) {
-    s = fwd_end(models[p], st, "mgn_lockstep_forward");
+    s = fwd_end(models[p], st, fn);
     if (s) return s;
   }
   return MGN_OK;
 }
 
-mgn_status mgn_lockstep_backward(int32_t n_parts, mgn_model* const* models, const float* const* d_out,
-                                 float* d_params, int accumulate, float* const* d_halo, const mgn_halo_link* links,
-                                 int32_t n_links, mgn_stream stream) {
-  mgn_status s = check_links(n_parts, models, links, n_links, d_halo, "mgn_lockstep_backward");
+mgn_status lockstep_backward(int32_t n_parts, mgn_model* const* models, const float* const* d_out, float* d_params,
+                             int accumulate, float* const* d_halo, const mgn_halo_link* links, int32_t n_links,
+                             Slots8 s8, hipStream_t st, const char* fn) {
+  const std::string f(fn);
+  mgn_status s = check_links(n_parts, models, links, n_links, d_halo, fn);
   if (s) return s;
-  if (!d_out) return fail(nullptr, MGN_E_ARG, "mgn_lockstep_backward: NULL array");
-  hipStream_t st = (hipStream_t)stream;
+  if (!d_out) return fail(nullptr, MGN_E_ARG, f + ": NULL array");
   // one gradient buffer: the first part writes (or adds, accumulate), the others add, in part order
   for (int32_t p = 0; p < n_parts; ++p) {
-    s = bwd_begin(models[p], d_out[p], d_params, accumulate || p > 0, d_halo ? d_halo[p] : nullptr, st,
-                  "mgn_lockstep_backward");
+    s = bwd_begin(models[p], d_out[p], d_params, accumulate || p > 0, d_halo ? d_halo[p] : nullptr, st, fn);
     if (s) return s;
   }
   const int K = models[0]->K;
   for (int k = K - 1; k >= 0; --k) {
     for (int32_t p = 0; p < n_parts; ++p) {
-      s = bwd_block(models[p], st, "mgn_lockstep_backward");
+      s = bwd_block(models[p], st, fn);
       if (s) return s;
     }
     for (int32_t i = 0; i < n_links; ++i) {
@@ -1549,16 +1630,65 @@ mgn_status mgn_lockstep_backward(int32_t n_parts, mgn_model* const* models, cons
       if (ln.n == 0) continue;
       mgn_model* mp = models[ln.part];
       const int64_t nh = mp->g.n_halo;
-      s = mgn_add_latent_grads(models[ln.owner], d_halo[ln.part] + (size_t)k * nh * mp->L, nh, ln.recv_idx,
-                               ln.send_rows, ln.n, stream);
-      if (s) return fail(nullptr, s, std::string("mgn_lockstep_backward: ") + mgn_last_error(models[ln.owner]));
+      const float* dk = d_halo[ln.part] + (size_t)k * nh * mp->L;
+      if (!s8.q) {
+        s = mgn_add_latent_grads(models[ln.owner], dk, nh, ln.recv_idx, ln.send_rows, ln.n, st);
+      } else {
+        {
+          Timed t_(mp, MGN_T_EXCHANGE, st);
+          s = mgn_rows_store8(dk, MGN_FP32, nh, mp->L, ln.recv_idx, nullptr, ln.n, s8.q, s8.scale, ln.n, st);
+        }
+        if (s) return s;
+        s = mgn_add_latent_grads8(models[ln.owner], s8.q, s8.scale, mp->L, ln.send_rows, ln.n, st);
+      }
+      if (s) return fail(nullptr, s, f + ": " + mgn_last_error(models[ln.owner]));
     }
   }
   for (int32_t p = 0; p < n_parts; ++p) {
-    s = bwd_end(models[p], st, "mgn_lockstep_backward");
+    s = bwd_end(models[p], st, fn);
     if (s) return s;
   }
   return MGN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mgn_status mgn_lockstep_forward(int32_t n_parts, mgn_model* const* models, const mgn_graph* graphs,
+                                const float* const* node_feat, const float* const* edge_feat, float* const* halo,
+                                float* const* out, void* const* workspace, const size_t* ws_bytes,
+                                const mgn_halo_link* links, int32_t n_links, mgn_stream stream) {
+  return lockstep_forward(n_parts, models, graphs, node_feat, edge_feat, halo, out, workspace, ws_bytes, links,
+                          n_links, Slots8{}, (hipStream_t)stream, "mgn_lockstep_forward");
+}
+
+mgn_status mgn_lockstep_forward8(int32_t n_parts, mgn_model* const* models, const mgn_graph* graphs,
+                                 const float* const* node_feat, const float* const* edge_feat, float* const* halo,
+                                 float* const* out, void* const* workspace, const size_t* ws_bytes,
+                                 const mgn_halo_link* links, int32_t n_links, uint8_t* q, float* scale, int64_t slots,
+                                 int32_t cols, mgn_stream stream) {
+  mgn_status s = check_slots(n_parts, models, links, n_links, q, scale, slots, cols, "mgn_lockstep_forward8");
+  if (s) return s;
+  return lockstep_forward(n_parts, models, graphs, node_feat, edge_feat, halo, out, workspace, ws_bytes, links,
+                          n_links, Slots8{q, scale}, (hipStream_t)stream, "mgn_lockstep_forward8");
+}
+
+mgn_status mgn_lockstep_backward(int32_t n_parts, mgn_model* const* models, const float* const* d_out,
+                                 float* d_params, int accumulate, float* const* d_halo, const mgn_halo_link* links,
+                                 int32_t n_links, mgn_stream stream) {
+  return lockstep_backward(n_parts, models, d_out, d_params, accumulate, d_halo, links, n_links, Slots8{},
+                           (hipStream_t)stream, "mgn_lockstep_backward");
+}
+
+mgn_status mgn_lockstep_backward8(int32_t n_parts, mgn_model* const* models, const float* const* d_out,
+                                  float* d_params, int accumulate, float* const* d_halo, const mgn_halo_link* links,
+                                  int32_t n_links, uint8_t* q, float* scale, int64_t slots, int32_t cols,
+                                  mgn_stream stream) {
+  mgn_status s = check_slots(n_parts, models, links, n_links, q, scale, slots, cols, "mgn_lockstep_backward8");
+  if (s) return s;
+  return lockstep_backward(n_parts, models, d_out, d_params, accumulate, d_halo, links, n_links, Slots8{q, scale},
+                           (hipStream_t)stream, "mgn_lockstep_backward8");
 }
 
 }  // extern "C"

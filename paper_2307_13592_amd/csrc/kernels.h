@@ -161,6 +161,45 @@ struct DwGroup {
   float* part;
 };
 
+// Rows in 8 bits (rows8.h): row rows[i] (null: i) of x (store) or of out
+// (load) and slot slots[i] (null: i) of q / scale, i < n; a pair with an index
+// outside its range is skipped.  add: the row takes the sum with what it held.
+struct Rows8Args {
+  const void* x;
+  void* out;
+  const int32_t *rows, *slots;
+  uint8_t* q;
+  float* scale;
+  int64_t n, n_rows, n_slots;
+  int cols, add;
+};
+// Root-mean-square norm.  Forward: x, res (or null) -> total (or null), y
+// (y_scale with 8-bit rows).  Backward: x = the sum the forward normalised,
+// dy, res = the gradient arriving at that sum (or null) -> total = its whole
+// gradient; part: [MGN_RMS_WORK_PER_COL][cols] partials of dw, or null.
+struct RmsArgs {
+  const void *x, *res, *dy;
+  const float* w;
+  void *total, *y;
+  float *y_scale, *part;
+  int64_t rows;
+  int cols;
+  float eps;
+};
+// Gated recurrence (scan.hip): [steps][rows][cols] arrays, states [rows][cols].
+struct ScanArgs {
+  const void *g, *x;
+  const float* x_scale;  // 8-bit x only
+  const uint8_t* starts;
+  const float *h0, *dh, *dh_last;
+  float* h;  // read by the backward
+  float *h_last, *dh0;
+  void *dg, *dx;
+  void* work;
+  int64_t steps, rows;
+  int cols;
+};
+
 // ------------------------------------------------------------ launchers ---
 hipError_t launch_zero(float* p, int64_t n, hipStream_t st);
 hipError_t launch_halo_bf16(const float* H, int K, int64_t n_halo, int64_t n_owned, int L, void* V16,
@@ -299,6 +338,18 @@ hipError_t launch_dw_reduce(const float* part, int S, int O, int I, float* dst, 
 // else over this call's masked rows.
 hipError_t launch_mse(const float* out, const float* target, const uint8_t* mask, int64_t n, int d,
                       int64_t global_rows, float* loss, float* d_out, hipStream_t st);
+
+// Rows outside the MLPs (rows.hip).  type: of x, res, total, dy (load8: of
+// out); cols <= MGN_ROW_MAX_COLS.  launch_rms_norm_grad takes no rows too
+// (dw: zeros, or left as it is with accumulate).
+hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st);
+hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st);
+hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t st);
+hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st);
+// Gated recurrence (scan.hip); steps may be 0.
+size_t scan_work_bytes(int64_t steps, int64_t rows, int cols);
+hipError_t launch_scan(const ScanArgs& a, int g_type, int x_type, hipStream_t st);
+hipError_t launch_scan_grad(const ScanArgs& a, int g_type, int x_type, hipStream_t st);
 
 // tile sizes the host needs to know (rows per edge sub-tile, per prec/L/D)
 int edge_tile_rows(int prec, int L, int D);

@@ -16,8 +16,9 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from . import mgn_halo_masks, mgn_lockstep_backward, mgn_lockstep_forward, mgn_mse_grad_global, mgn_sgd_step
-from .runner import Session
+from . import (mgn_halo_masks, mgn_lockstep_backward, mgn_lockstep_backward8, mgn_lockstep_forward,
+               mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step)
+from .runner import LatentCache, Session
 
 
 def nocomm_edges(send, recv, part):
@@ -32,10 +33,14 @@ def nocomm_edges(send, recv, part):
 class Lockstep:
     """P parts of one mesh; graphs[p] from mgn_graph_build(..., part, n_nodes, p),
     node_feats[p] / edge_feats[p] the part's owned-node and local-edge
-    features (local order)."""
+    features (local order).  halo8: the halo latents pass from part to part in
+    8 bits with a scale per 128 columns (a quarter of the bytes); grads8: the
+    halo gradients do too."""
 
     def __init__(self, latent: int, K: int, depth: int, precision: str, part, graphs: list, node_feats: list,
-                 edge_feats: list, params, device: str = "cuda", recompute: int = 0):
+                 edge_feats: list, params, device: str = "cuda", recompute: int = 0, halo8: bool = False,
+                 grads8: bool = False):
+        self.halo8, self.grads8 = halo8, grads8
         self.K, self.latent, self.P = K, latent, len(graphs)
         self.device = torch.device(device)
         self.sessions = []
@@ -54,14 +59,20 @@ class Lockstep:
                 if recv.size:
                     self.links.append((p, q, dev(recv), dev(send)))
         self.d_params = torch.empty(self.sessions[0].n_params, dtype=torch.float32, device=self.device)
+        # one link's packed rows at a time
+        self.packed = (LatentCache(max([r.numel() for _, _, r, _ in self.links], default=1), latent, device)
+                       if halo8 or grads8 else None)
 
     def forward(self, stream=None):
         """Encoders of every part; per block, the halo copies of every link,
         then the block on every part; decoders (mgn_lockstep_forward)."""
         S = self.sessions
-        mgn_lockstep_forward([s.model for s in S], [s.gs for s in S], [s.node_feat for s in S],
-                             [s.edge_feat for s in S], [s.halo for s in S], [s.out for s in S],
-                             [s.workspace for s in S], self.links, stream)
+        args = ([s.model for s in S], [s.gs for s in S], [s.node_feat for s in S], [s.edge_feat for s in S],
+                [s.halo for s in S], [s.out for s in S], [s.workspace for s in S], self.links)
+        if self.halo8:
+            mgn_lockstep_forward8(*args, self.packed.q, self.packed.scale, stream)
+        else:
+            mgn_lockstep_forward(*args, stream)
         return [s.out for s in S]
 
     def mse(self, targets, masks=None, stream=None):
@@ -91,8 +102,11 @@ class Lockstep:
             if not isinstance(d, torch.Tensor):
                 d = torch.as_tensor(np.ascontiguousarray(d, np.float32)).to(self.device)
             ds.append(d.contiguous())
-        mgn_lockstep_backward([s.model for s in S], ds, self.d_params, [s.d_halo for s in S], self.links, False,
-                              stream)
+        args = ([s.model for s in S], ds, self.d_params, [s.d_halo for s in S], self.links)
+        if self.grads8:
+            mgn_lockstep_backward8(*args, self.packed.q, self.packed.scale, False, stream)
+        else:
+            mgn_lockstep_backward(*args, False, stream)
         return self.d_params
 
     def sgd(self, lr: float, stream=None):
@@ -106,3 +120,4 @@ class Lockstep:
             s.close()
         self.sessions = []
         self.links = []
+        self.packed = None

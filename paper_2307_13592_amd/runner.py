@@ -9,7 +9,8 @@ import torch
 from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_destroy, mgn_forward,
                mgn_graph_validate, mgn_mse_grad, mgn_param_count, mgn_set_params, mgn_set_recompute,
                mgn_norm_accumulate, mgn_norm_apply, MGN_NORM_WORK_PER_COL, mgn_rollout_update, mgn_set_h1_stash,
-               mgn_set_inference, mgn_sgd_step, mgn_workspace_size)
+               mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
+               mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks)
 
 
 class Session:
@@ -98,15 +99,27 @@ class Session:
         """Parameter update with the last backward's gradient (or `grad`)."""
         mgn_sgd_step(self.model, self.d_params if grad is None else grad, lr, stream)
 
-    def rollout(self, steps: int, col0: int = 3, stream=None):
+    def rollout(self, steps: int, col0: int = 3, stream=None, memory=None, history=None):
         """`steps` next-step predictions, each fed back into the flow columns
-        of the node features (q <- q + p); returns the outputs of every step."""
+        of the node features (q <- q + p); returns the outputs of every step.
+        memory: a GatedMemory of this session's outputs with a gate; the
+        increments fed back are then its states, h <- f h + (1 - f) p.
+        history: a LatentCache of at least steps * n_owned slots; the outputs
+        are then kept there in 8 bits (step t in slots t n_owned ..), and the
+        cache is returned."""
+        n = self.out.shape[0]
         outs = []
-        for _ in range(steps):
+        if history is not None and (history.cols != self.out.shape[1] or history.slots < steps * n):
+            raise ValueError("history: expected steps * n_owned slots of node_out columns")
+        for t in range(steps):
             self.forward(stream)
-            outs.append(self.out.clone())
-            mgn_rollout_update(self.out, self.node_feat, col0, stream)
-        return outs
+            if history is not None:
+                history.store(self.out, first=t * n, stream=stream)
+            else:
+                outs.append(self.out.clone())
+            p = self.out if memory is None else memory.step(self.out, stream=stream)
+            mgn_rollout_update(p, self.node_feat, col0, stream)
+        return outs if history is None else history
 
     def mse(self, target, mask=None, stream=None):
         loss = torch.empty(2, dtype=torch.float32, device=self.device)
@@ -148,3 +161,110 @@ class Normalizer:
         mgn_norm_apply(x, self.stats, out, self.eps, stream)
         return out
 
+
+class LatentCache:
+    """`slots` rows of `cols` columns held in 8 bits on the device (codes q,
+    one scale per 128 columns): packed halo rows, or the history of a rollout
+    or of a trajectory's node latents."""
+
+    def __init__(self, slots: int, cols: int, device: str = "cuda"):
+        self.slots, self.cols = slots, cols
+        self.q = torch.zeros((slots, cols), dtype=torch.uint8, device=device)
+        self.scale = torch.ones((slots, rows8_blocks(cols)), dtype=torch.float32, device=device)
+
+    def store(self, src, first: int = 0, src_rows=None, slots=None, stream=None):
+        """Rows of src (or its src_rows) into the slots given, or into first,
+        first + 1, ..."""
+        if slots is not None:
+            mgn_rows_store8(src, self.q, self.scale, src_rows, slots, stream)
+            return
+        q, scale = self._span(first, src.shape[0] if src_rows is None else src_rows.numel())
+        mgn_rows_store8(src, q, scale, src_rows, None, stream)
+
+    def load(self, dst, first: int = 0, slots=None, dst_rows=None, add: bool = False, stream=None):
+        """The slots given, or first, first + 1, ..., into dst (or its dst_rows)."""
+        if slots is not None:
+            mgn_rows_load8(self.q, self.scale, dst, slots, dst_rows, add, stream)
+        else:
+            q, scale = self._span(first, dst.shape[0] if dst_rows is None else dst_rows.numel())
+            mgn_rows_load8(q, scale, dst, None, dst_rows, add, stream)
+        return dst
+
+    def window(self, first: int, steps: int, rows: int):
+        """Codes and scales of steps x rows slots from `first` on, as the
+        recurrence reads them: ([steps][rows][cols], [steps][rows][blocks])."""
+        q, scale = self._span(first, steps * rows)
+        return q.view(steps, rows, self.cols), scale.view(steps, rows, -1)
+
+    def _span(self, first: int, n: int):
+        if first < 0 or first + n > self.slots:
+            raise ValueError(f"slots {first} .. {first + n} of {self.slots}")
+        return self.q[first:first + n], self.scale[first:first + n]
+
+
+class RmsNorm:
+    """Root-mean-square norm of node rows with a weight per column, and the
+    addition of a residual before it."""
+
+    def __init__(self, cols: int, device: str = "cuda", eps: float = 1e-6):
+        self.cols, self.eps = cols, eps
+        self.weight = torch.ones(cols, dtype=torch.float32, device=device)
+        self.d_weight = torch.zeros_like(self.weight)
+
+    def apply(self, x, res=None, dtype=None, stream=None):
+        """(y, t): y the norm of t = x + res (of x without a residual) in
+        `dtype` (x's by default)."""
+        y = torch.empty_like(x, dtype=x.dtype if dtype is None else dtype)
+        total = x if res is None else torch.empty_like(x)
+        mgn_rms_norm(x, self.weight, y, res, None if res is None else total, None, self.eps, stream)
+        return y, total
+
+    def store(self, x, cache: LatentCache, first: int = 0, res=None, stream=None):
+        """The norm of x + res in 8 bits, into the cache's slots from `first`
+        on; returns the sum."""
+        q, scale = cache._span(first, x.shape[0])
+        total = x if res is None else torch.empty_like(x)
+        mgn_rms_norm(x, self.weight, q, res, None if res is None else total, scale, self.eps, stream)
+        return total
+
+    def grad(self, total, dy, d_total=None, accumulate: bool = False, stream=None):
+        """dL/dt from dy and the gradient that reaches t otherwise; d_weight
+        takes (accumulate: adds) dL/dweight."""
+        dx = torch.empty_like(total)
+        mgn_rms_norm_grad(total, self.weight, dy, dx, self.d_weight, d_total, accumulate, None, self.eps, stream)
+        return dx
+
+
+class GatedMemory:
+    """A gated linear recurrence over time on rows of `cols` columns:
+    h <- f h + (1 - f) x with f = sigmoid(g).  step() carries `state` along a
+    rollout; scan() and grad() run whole trajectories.  gate: logits
+    [rows][cols] that step() uses when it is given none."""
+
+    def __init__(self, rows: int, cols: int, device: str = "cuda", gate=None):
+        self.state = torch.zeros((rows, cols), dtype=torch.float32, device=device)
+        self.gate = gate
+
+    def step(self, x, g=None, x_scale=None, stream=None):
+        """One time step (x, g [rows][cols]); returns the state."""
+        g = self.gate if g is None else g
+        if g is None:
+            raise ValueError("g: no gate given")
+        mgn_gated_scan(g[None], x[None], None, self.state, self.state, None,
+                       None if x_scale is None else x_scale[None], None, stream)
+        return self.state
+
+    def scan(self, g, x, starts=None, x_scale=None, stream=None):
+        """Every state of a trajectory [steps][rows][cols] that continues from
+        `state`, which becomes the last one."""
+        h = torch.empty(g.shape, dtype=torch.float32, device=g.device)
+        self.h0 = self.state.clone()
+        mgn_gated_scan(g, x, h, self.state, self.h0, starts, x_scale, None, stream)
+        return h
+
+    def grad(self, g, x, h, dh=None, dh_last=None, starts=None, x_scale=None, stream=None):
+        """(dg, dx, dh0) of the last scan()."""
+        dg, dx = torch.empty_like(g), torch.empty_like(g)
+        dh0 = torch.empty_like(self.state)
+        mgn_gated_scan_grad(g, x, h, dg, dx, dh, dh_last, dh0, self.h0, starts, x_scale, None, stream)
+        return dg, dx, dh0
