@@ -226,8 +226,8 @@ mgn_status mgn_norm_apply(const float* x, int64_t rows, int32_t cols, const doub
  *
  * Device arrays of rows [n][cols], 1 <= cols <= MGN_ROW_MAX_COLS, contiguous
  * and aligned to their type (fp32 4 bytes, bf16 2); row counts are 64-bit.
- * Asynchronous on `stream`, no allocation, no atomics; the same inputs give the
- * same bits.  MGN_E_ARG for sizes or types outside what is stated, a NULL or
+ * Asynchronous on `stream`, no allocation, no atomics; the same inputs, in
+ * arrays of the same alignment, give the same bits.  MGN_E_ARG for sizes or types outside what is stated, a NULL or
  * misaligned pointer, or arrays that overlap where it is not allowed.
  *
  * 8-bit rows are codes q [slots][cols] (one e4m3 byte a column: 4 exponent

@@ -9,6 +9,7 @@ kernels of libmgn.so; there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -331,42 +332,50 @@ def _type(t, name: str, e4m3: bool = False) -> int:
     import torch
     if t is None:
         raise ValueError(f"{name}: expected a device tensor, got None")
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return MGN_FP32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return MGN_BF16
-    if e4m3 and t.dtype == torch.uint8:
+    if e4m3 and t.dtype is torch.uint8:
         return MGN_E4M3
     raise ValueError(f"{name}: unsupported storage type {t.dtype}")
 
 
-def _rows(t, name: str):
-    if t is None or t.dim() != 2:
-        raise ValueError(f"{name}: expected [rows][cols]")
+def _shape(t, name: str, dims: int = 2):
+    if t is None or t.dim() != dims:
+        raise ValueError(f"{name}: expected {'[steps]' if dims == 3 else ''}[rows][cols]")
     return t.shape
 
 
-def _opt(t, dtype, name: str, **kw):
-    return None if t is None else _devt(t, dtype, name, **kw)
+def _arr(t, name: str, dtype, shape, dev):
+    """Device pointer of an array of this type and shape on device `dev`
+    (None -> NULL).  One comparison per property: these calls are short."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous() and t.is_cuda:
+        return t.data_ptr()
+    _devt(t, dtype, name, shape=shape)  # says what is wrong, but for the device
+    raise ValueError(f"{name}: expected a tensor on {dev}, got one on {t.device}")
 
 
-def _call(fn: str, stream, first, *rest):
-    """Calls the entry point `fn`(*args, stream) on the device of its tensors:
-    returns a function of the arguments.  All tensors lie on one device; the
-    default stream is that device's current one."""
+def _need(p, name: str):
+    if p is None:
+        raise ValueError(f"{name}: expected a device tensor, got None")
+    return p
+
+
+def _run(fn: str, dev, stream, *args) -> None:
+    """Calls the entry point fn(*args, stream) on the device of its arrays;
+    without a stream given, on the current one of that device."""
     import torch
-    dev = first.device
-    for t in rest:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{fn}: tensors on different devices ({dev} and {t.device})")
     f = getattr(lib(), fn)
-    if not first.is_cuda or dev.index == torch.cuda.current_device():
-        return lambda *args: _check(f(*args, _stream(stream)))
-
-    def on_device(*args):
+    if dev.index == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else int(stream))
+    else:
         with torch.cuda.device(dev):
-            _check(f(*args, _stream(stream)))
-    return on_device
+            st = f(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream))
+    if st != MGN_OK:
+        _check(st)
 
 
 def _scratch(nbytes: int, device, stream):
@@ -374,12 +383,17 @@ def _scratch(nbytes: int, device, stream):
     stream, so that it is not handed out again before the call has run (and
     belongs to a HIP graph that records the call)."""
     import torch
-    if nbytes == 0:
-        return None
     if stream is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _lists(a, b, rows: int, dev):
+    """Pointers and length of two int32 index lists, either of them None."""
+    import torch
+    n = a.numel() if a is not None else b.numel() if b is not None else rows
+    return _arr(a, "index list", torch.int32, (n,), dev), _arr(b, "index list", torch.int32, (n,), dev), n
 
 
 def mgn_rows_store8(src, q, scale, src_rows=None, slots=None, stream=None) -> None:
@@ -389,13 +403,12 @@ def mgn_rows_store8(src, q, scale, src_rows=None, slots=None, stream=None) -> No
     int32 device tensors of one length, or None for 0, 1, 2, ...; without
     either, every row of src is stored."""
     import torch
-    n_src, cols = _rows(src, "src")
-    n_slots = _rows(q, "q")[0]
-    n = src_rows.numel() if src_rows is not None else slots.numel() if slots is not None else n_src
-    call = _call("mgn_rows_store8", stream, src, q, scale, src_rows, slots)
-    call(_devt(src, src.dtype, "src"), _type(src, "src"), n_src, cols, _opt(src_rows, torch.int32, "src_rows"),
-         _opt(slots, torch.int32, "slots", numel=n), n, _devt(q, torch.uint8, "q", shape=(n_slots, cols)),
-         _devt(scale, torch.float32, "scale", shape=(n_slots, rows8_blocks(cols))), n_slots)
+    n_src, cols = _shape(src, "src")
+    n_slots, dev = _shape(q, "q")[0], src.device
+    rows, at, n = _lists(src_rows, slots, n_src, dev)
+    _run("mgn_rows_store8", dev, stream, _need(_arr(src, "src", src.dtype, (n_src, cols), dev), "src"),
+         _type(src, "src"), n_src, cols, rows, at, n, _arr(q, "q", torch.uint8, (n_slots, cols), dev),
+         _need(_arr(scale, "scale", torch.float32, (n_slots, rows8_blocks(cols)), dev), "scale"), n_slots)
 
 
 def mgn_rows_load8(q, scale, dst, slots=None, dst_rows=None, add: bool = False, stream=None) -> None:
@@ -404,13 +417,12 @@ def mgn_rows_load8(q, scale, dst, slots=None, dst_rows=None, add: bool = False, 
     them and of what it holds, float32 only).  Without index tensors every
     slot is read."""
     import torch
-    n_slots, cols = _rows(q, "q")
-    n_dst = _rows(dst, "dst")[0]
-    n = dst_rows.numel() if dst_rows is not None else slots.numel() if slots is not None else n_slots
-    call = _call("mgn_rows_load8", stream, q, scale, dst, slots, dst_rows)
-    call(_devt(q, torch.uint8, "q"), _devt(scale, torch.float32, "scale", shape=(n_slots, rows8_blocks(cols))), n_slots,
-         cols, _opt(slots, torch.int32, "slots", numel=n), _opt(dst_rows, torch.int32, "dst_rows", numel=n), n,
-         _devt(dst, dst.dtype, "dst", shape=(n_dst, cols)), _type(dst, "dst"), n_dst, int(bool(add)))
+    n_slots, cols = _shape(q, "q")
+    n_dst, dev = _shape(dst, "dst")[0], q.device
+    rows, at, n = _lists(dst_rows, slots, n_slots, dev)
+    _run("mgn_rows_load8", dev, stream, _need(_arr(q, "q", torch.uint8, (n_slots, cols), dev), "q"),
+         _need(_arr(scale, "scale", torch.float32, (n_slots, rows8_blocks(cols)), dev), "scale"), n_slots, cols, at,
+         rows, n, _arr(dst, "dst", dst.dtype, (n_dst, cols), dev), _type(dst, "dst"), n_dst, 1 if add else 0)
 
 
 def mgn_rms_norm(x, weight, y, res=None, total=None, y_scale=None, eps: float = 1e-6, stream=None) -> None:
@@ -419,13 +431,13 @@ def mgn_rms_norm(x, weight, y, res=None, total=None, y_scale=None, eps: float = 
     float32, bfloat16, or uint8 for 8-bit rows with their scales in y_scale.
     weight: float32 [cols] or None."""
     import torch
-    rows, cols = _rows(x, "x")
+    shape = rows, cols = _shape(x, "x")
+    dev, dt = x.device, x.dtype
     yt = _type(y, "y", e4m3=True)
-    call = _call("mgn_rms_norm", stream, x, weight, y, res, total, y_scale)
-    call(_devt(x, x.dtype, "x"), _opt(res, x.dtype, "res", shape=(rows, cols)), _type(x, "x"), rows, cols,
-         _opt(weight, torch.float32, "weight", numel=cols), C.c_float(eps),
-         _opt(total, x.dtype, "total", shape=(rows, cols)), _devt(y, y.dtype, "y", shape=(rows, cols)), yt,
-         _opt(y_scale, torch.float32, "y_scale", shape=(rows, rows8_blocks(cols))))
+    _run("mgn_rms_norm", dev, stream, _arr(x, "x", dt, shape, dev), _arr(res, "res", dt, shape, dev), _type(x, "x"),
+         rows, cols, _arr(weight, "weight", torch.float32, (cols,), dev), eps, _arr(total, "total", dt, shape, dev),
+         _arr(y, "y", y.dtype, shape, dev), yt,
+         None if y_scale is None else _arr(y_scale, "y_scale", torch.float32, (rows, rows8_blocks(cols)), dev))
 
 
 def mgn_rms_norm_grad(total, weight, dy, dx, dweight=None, d_total=None, accumulate: bool = False, work=None,
@@ -435,20 +447,25 @@ def mgn_rms_norm_grad(total, weight, dy, dx, dweight=None, d_total=None, accumul
     dy and the gradient d_total that reaches the sum otherwise.  work: float32
     scratch of MGN_RMS_WORK_PER_COL * cols for dweight (None: allocated)."""
     import torch
-    rows, cols = _rows(total, "total")
-    call = _call("mgn_rms_norm_grad", stream, total, weight, dy, dx, dweight, d_total, work)
-    pt = _devt(total, total.dtype, "total")
-    if dweight is not None and work is None:
-        work = _scratch(4 * MGN_RMS_WORK_PER_COL * cols, total.device, stream)
-        pw = _dev(work)
+    shape = rows, cols = _shape(total, "total")
+    dev, dt = total.device, total.dtype
+    pt = _arr(total, "total", dt, shape, dev)
+    if work is not None:
+        pw = _devt(work, torch.float32, "work", min_numel=MGN_RMS_WORK_PER_COL * cols)
+        if work.device != dev:
+            raise ValueError(f"work: expected a tensor on {dev}, got one on {work.device}")
+    elif dweight is not None:
+        work = _scratch(4 * MGN_RMS_WORK_PER_COL * cols, dev, stream)
+        pw = work.data_ptr()
     else:
-        pw = _opt(work, torch.float32, "work", min_numel=MGN_RMS_WORK_PER_COL * cols)
-    call(pt, _type(total, "total"), _opt(weight, torch.float32, "weight", numel=cols), C.c_float(eps),
-         _devt(dy, total.dtype, "dy", shape=(rows, cols)), _opt(d_total, total.dtype, "d_total", shape=(rows, cols)),
-         rows, cols, _devt(dx, total.dtype, "dx", shape=(rows, cols)),
-         _opt(dweight, torch.float32, "dweight", numel=cols), int(bool(accumulate)), pw)
+        pw = None
+    _run("mgn_rms_norm_grad", dev, stream, pt, _type(total, "total"),
+         _arr(weight, "weight", torch.float32, (cols,), dev), eps, _need(_arr(dy, "dy", dt, shape, dev), "dy"),
+         _arr(d_total, "d_total", dt, shape, dev), rows, cols, _need(_arr(dx, "dx", dt, shape, dev), "dx"),
+         _arr(dweight, "dweight", torch.float32, (cols,), dev), 1 if accumulate else 0, pw)
 
 
+@functools.lru_cache(maxsize=256)
 def mgn_gated_scan_work(steps: int, rows: int, cols: int) -> int:
     """Bytes of device scratch mgn_gated_scan and its backward need."""
     n = C.c_size_t()
@@ -459,21 +476,24 @@ def mgn_gated_scan_work(steps: int, rows: int, cols: int) -> int:
 def _scan_args(g, x, x_scale, starts, h0, work, stream):
     """Marshalled arguments the recurrence and its backward share."""
     import torch
-    if g is None or g.dim() != 3:
-        raise ValueError("g: expected [steps][rows][cols]")
-    T, rows, cols = shape = tuple(g.shape)
+    shape = T, rows, cols = _shape(g, "g", 3)
+    dev = g.device
     xt = _type(x, "x", e4m3=True)
-    if xt != MGN_E4M3 and x.dtype != g.dtype:
+    if xt != MGN_E4M3 and x.dtype is not g.dtype:
         raise ValueError(f"x: expected {g.dtype} (as g) or uint8 codes, got {x.dtype}")
-    need = mgn_gated_scan_work(T, rows, cols)
-    pg = _devt(g, g.dtype, "g")
+    head = (_arr(g, "g", g.dtype, shape, dev), _type(g, "g"), _arr(x, "x", x.dtype, shape, dev), xt,
+            None if x_scale is None else _arr(x_scale, "x_scale", torch.float32, (T, rows, rows8_blocks(cols)), dev),
+            None if starts is None else _arr(starts, "starts", torch.uint8, (T,), dev),
+            _arr(h0, "h0", torch.float32, (rows, cols), dev))
     if work is None:
-        work = _scratch(need, g.device, stream)
-    nb = 0 if work is None else work.numel() * work.element_size()
-    head = (pg, _type(g, "g"), _devt(x, x.dtype, "x", shape=shape), xt,
-            _opt(x_scale, torch.float32, "x_scale", shape=(T, rows, rows8_blocks(cols))),
-            _opt(starts, torch.uint8, "starts", shape=(T,)), _opt(h0, torch.float32, "h0", shape=(rows, cols)))
-    return shape, head, (_dev(work), nb), work
+        need = mgn_gated_scan_work(T, rows, cols)
+        if need:
+            work = _scratch(need, dev, stream)
+        return shape, dev, head, (work.data_ptr() if need else None, need), work
+    pw = _dev(work)
+    if work.device != dev:
+        raise ValueError(f"work: expected a tensor on {dev}, got one on {work.device}")
+    return shape, dev, head, (pw, work.numel() * work.element_size()), work
 
 
 def mgn_gated_scan(g, x, h=None, h_last=None, h0=None, starts=None, x_scale=None, work=None, stream=None) -> None:
@@ -483,10 +503,10 @@ def mgn_gated_scan(g, x, h=None, h_last=None, h0=None, starts=None, x_scale=None
     float32, either may be None; starts: uint8 [steps].  work: device scratch of
     mgn_gated_scan_work bytes (None: allocated)."""
     import torch
-    (T, rows, cols), head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
-    call = _call("mgn_gated_scan", stream, g, x, x_scale, starts, h0, h, h_last, keep)
-    call(*head, T, rows, cols, _opt(h, torch.float32, "h", shape=(T, rows, cols)),
-         _opt(h_last, torch.float32, "h_last", shape=(rows, cols)), *tail)
+    shape, dev, head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
+    T, rows, cols = shape
+    _run("mgn_gated_scan", dev, stream, *head, T, rows, cols, _arr(h, "h", torch.float32, shape, dev),
+         _arr(h_last, "h_last", torch.float32, (rows, cols), dev), *tail)
 
 
 def mgn_gated_scan_grad(g, x, h, dg, dx, dh=None, dh_last=None, dh0=None, h0=None, starts=None, x_scale=None,
@@ -495,13 +515,13 @@ def mgn_gated_scan_grad(g, x, h, dg, dx, dh=None, dh_last=None, dh0=None, h0=Non
     gradients dh [steps][rows][cols] and dh_last [rows][cols]: dg (g's type), dx
     (x's type; g's for 8-bit x) and dh0 (float32, or None; it may be dh_last)."""
     import torch
-    shape, head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
+    shape, dev, head, tail, keep = _scan_args(g, x, x_scale, starts, h0, work, stream)
     T, rows, cols = shape
-    call = _call("mgn_gated_scan_grad", stream, g, x, x_scale, starts, h0, h, dg, dx, dh, dh_last, dh0, keep)
-    call(*head, _devt(h, torch.float32, "h", shape=shape), _opt(dh, torch.float32, "dh", shape=shape),
-         _opt(dh_last, torch.float32, "dh_last", shape=(rows, cols)), T, rows, cols,
-         _devt(dg, g.dtype, "dg", shape=shape), _devt(dx, g.dtype, "dx", shape=shape),
-         _opt(dh0, torch.float32, "dh0", shape=(rows, cols)), *tail)
+    one, f32, dt = (rows, cols), torch.float32, g.dtype
+    _run("mgn_gated_scan_grad", dev, stream, *head, _need(_arr(h, "h", f32, shape, dev), "h"),
+         _arr(dh, "dh", f32, shape, dev), _arr(dh_last, "dh_last", f32, one, dev), T, rows, cols,
+         _need(_arr(dg, "dg", dt, shape, dev), "dg"), _need(_arr(dx, "dx", dt, shape, dev), "dx"),
+         _arr(dh0, "dh0", f32, one, dev), *tail)
 
 
 def mgn_workspace_size(model, graph: mgn_graph) -> int:
@@ -588,7 +608,7 @@ def mgn_add_latent_grads(owner, d_halo_k, recv_idx, send_rows, stream=None) -> N
 def _slots8(q, scale):
     """8-bit slots of an exchange: (q, scale, slots, cols)."""
     import torch
-    slots, cols = _rows(q, "q")
+    slots, cols = _shape(q, "q")
     return (_devt(q, torch.uint8, "q"), _devt(scale, torch.float32, "scale", shape=(slots, rows8_blocks(cols))), slots,
             cols)
 

@@ -196,7 +196,7 @@ struct ScanArgs {
   float *h_last, *dh0;
   void *dg, *dx;
   void* work;
-  int64_t steps, rows;
+  int64_t steps, rows, chunk;  // chunk: set by the launcher
   int cols;
 };
 
@@ -348,8 +348,8 @@ hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t s
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st);
 // Gated recurrence (scan.hip); steps may be 0.
 size_t scan_work_bytes(int64_t steps, int64_t rows, int cols);
-hipError_t launch_scan(const ScanArgs& a, int g_type, int x_type, hipStream_t st);
-hipError_t launch_scan_grad(const ScanArgs& a, int g_type, int x_type, hipStream_t st);
+hipError_t launch_scan(ScanArgs a, int g_type, int x_type, hipStream_t st);
+hipError_t launch_scan_grad(ScanArgs a, int g_type, int x_type, hipStream_t st);
 
 // tile sizes the host needs to know (rows per edge sub-tile, per prec/L/D)
 int edge_tile_rows(int prec, int L, int D);

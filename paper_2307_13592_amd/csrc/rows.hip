@@ -1,127 +1,179 @@
 // Node rows outside the network's MLPs: rows held in 8 bits (stored, read
 // back) and the root-mean-square norm with the residual's addition, forward
-// and backward.  A row's columns are dealt to TPR threads (16, 32 or 64 lanes
-// of one wave, or a workgroup of 256) in runs of four: thread t holds columns
-// (j TPR + t) 4 .. + 3 for j < NV, so that a row is read once, stays in
-// registers between its sum and its result, and the 128 columns that share an
-// 8-bit scale are 32 neighbouring lanes.
+// and backward.
+//
+// All are bound by memory: a row is read once and stays in registers between
+// its sum (or its blocks' largest values) and its result.  Its columns are dealt
+// to TPR threads, 4, 16, 32 or 64 lanes of one wave or a workgroup of 256 or 1024
+// (rows8.h, Cols), NV runs of V columns each; a wave takes 64 / TPR rows at a
+// time.
+#include <initializer_list>
+#include <type_traits>
+
 #include "kernels.h"
 #include "rows8.h"
 
 namespace mgn {
 namespace {
 
-constexpr int NT = 256;
+// Threads of a workgroup: a wide row's own, else 256.
+constexpr int threads(int TPR) { return TPR > 256 ? TPR : 256; }
 
-// Sum over the TPR threads of a row; every one of them gets the same value
-// (a butterfly: the order of additions does not depend on the lane).
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* lds) {
+// Sums of N values over the TPR threads of a row; every one of them gets the
+// same bits.  Rows of several waves add the waves' sums in order, through LDS:
+// one barrier a row, with two buffers in turn.
+template <int TPR, int N>
+struct RowSum {
+  static constexpr int WAVES = TPR / 64;
+  struct Lds {
+    float v[2][N][TPR > 64 ? WAVES : 1];
+  };
+  Lds& lds;
+  int turn = 0;
+  __device__ __forceinline__ explicit RowSum(Lds& l) : lds(l) {}
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-  for (int d = 1; d < (TPR < 64 ? TPR : 64); d *= 2) v += __shfl_xor(v, d);
-  if constexpr (TPR > 64) {
-    __syncthreads();  // the row before may still be reading lds
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    for (int k = 0; k < N; ++k) v[k] = group_sum<(TPR < 64 ? TPR : 64)>(v[k]);
+    if constexpr (TPR > 64) {
+      if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < N; ++k) lds.v[turn][k][threadIdx.x >> 6] = v[k];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        v[k] = lds.v[turn][k][0];
+#pragma unroll
+        for (int e = 1; e < WAVES; ++e) v[k] += lds.v[turn][k][e];
+      }
+      turn ^= 1;
+    }
   }
-  return v;
-}
+};
+
+// The rows of a wave (of a workgroup for TPR > 64): RPW at a time from `row`
+// on, the lane's own being row + sub.
+template <int TPR>
+struct Rows {
+  static constexpr int RPW = TPR > 64 ? 1 : 64 / TPR;  // rows a wave (workgroup) holds
+  static constexpr int NT = threads(TPR), RPB = TPR > 64 ? 1 : NT / TPR;  // threads, rows of a workgroup
+  int64_t row, next;
+  int sub, t;
+  __device__ __forceinline__ Rows() {
+    t = threadIdx.x % TPR;
+    sub = TPR > 64 ? 0 : (threadIdx.x & 63) / TPR;
+    row = (int64_t)blockIdx.x * RPB + (TPR > 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPW);
+    next = (int64_t)gridDim.x * RPB;
+  }
+};
 
 // --------------------------------------------------------- rows in 8 bits ---
 
-template <int TPR, int NV, bool VEC, int TI>
-__global__ __launch_bounds__(NT) void store8_kernel(Rows8Args a) {
-  const int t = threadIdx.x % TPR;
-  constexpr int RPB = NT / TPR;
+template <int TPR, int NV, int V, bool VEC, int TI>
+__global__ __launch_bounds__(threads(TPR)) void store8_kernel(Rows8Args a) {
+  using D = Cols<TPR, V, VEC>;
   const int nb = rows8_blocks(a.cols);
-  for (int64_t i = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; i < a.n; i += (int64_t)gridDim.x * RPB) {
-    const int64_t r = a.rows ? a.rows[i] : i, s = a.slots ? a.slots[i] : i;
-    if (r < 0 || r >= a.n_rows || s < 0 || s >= a.n_slots) continue;
+  Rows<TPR> w;
+  for (; w.row < a.n; w.row += w.next) {
+    const int64_t i = w.row + w.sub;
+    bool ok = i < a.n;
+    const int64_t r = ok ? (a.rows ? a.rows[i] : i) : 0, s = ok ? (a.slots ? a.slots[i] : i) : 0;
+    ok = ok && r >= 0 && r < a.n_rows && s >= 0 && s < a.n_slots;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      float v[4];
-      load_cols<TI, VEC>(a.x, r * a.cols, c, a.cols, v);
-      store_cols8<TPR, VEC>(a.q + s * a.cols, a.scale + s * nb, c, a.cols, v);
+      const int c = D::first(j, w.t);
+      float v[V];
+      load_cols<TI, D>(a.x, ok ? r * a.cols : 0, 0, c, ok ? a.cols : 0, v);
+      store_cols8<D>(a.q + (ok ? s * a.cols : 0), a.scale + (ok ? s * nb : 0), c, a.cols, v, ok);
     }
   }
 }
 
-template <int TPR, int NV, bool VEC, int TO>
-__global__ __launch_bounds__(NT) void load8_kernel(Rows8Args a) {
-  const int t = threadIdx.x % TPR;
-  constexpr int RPB = NT / TPR;
+template <int TPR, int NV, int V, bool VEC, int TO>
+__global__ __launch_bounds__(threads(TPR)) void load8_kernel(Rows8Args a) {
+  using D = Cols<TPR, V, VEC>;
   const int nb = rows8_blocks(a.cols);
-  for (int64_t i = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; i < a.n; i += (int64_t)gridDim.x * RPB) {
+  Rows<TPR> w;
+  for (; w.row < a.n; w.row += w.next) {
+    const int64_t i = w.row + w.sub;
+    if (i >= a.n) continue;
     const int64_t r = a.rows ? a.rows[i] : i, s = a.slots ? a.slots[i] : i;
     if (r < 0 || r >= a.n_rows || s < 0 || s >= a.n_slots) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      if (c >= a.cols) break;
-      float v[4];
-      load_cols8<VEC>(a.q + s * a.cols, a.scale[s * nb + c / ROWS8_BLOCK], c, a.cols, v);
+      const int c = D::first(j, w.t);
+      if (c >= a.cols) continue;
+      float v[V];
+      load_cols8<D>(a.q + s * a.cols, a.scale[s * nb + c / ROWS8_BLOCK], c, a.cols, v);
       if (a.add) {
-        float o[4];
-        load_cols<TO, VEC>(a.out, r * a.cols, c, a.cols, o);
+        float o[V];
+        load_cols<TO, D>(a.out, r * a.cols, 0, c, a.cols, o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += o[k];
+        for (int k = 0; k < V; ++k) v[k] += o[k];
       }
-      store_cols<TO, VEC>(a.out, r * a.cols, c, a.cols, v);
+      store_cols<TO, D>(a.out, r * a.cols, 0, c, a.cols, v);
     }
   }
 }
 
 // --------------------------------------------------- root-mean-square norm ---
 
-// y = t / sqrt(mean(t^2) + eps) * w for t = x + res, in fp32; t is rounded
-// once where it is stored, y once where it is stored (y is formed from the
-// unrounded t).
-template <int TPR, int NV, bool VEC, int TI, int TO>
-__global__ __launch_bounds__(NT) void rms_norm_kernel(RmsArgs a) {
-  __shared__ float lds[4];
-  const int t = threadIdx.x % TPR;
-  constexpr int RPB = NT / TPR;
-  const int nb = rows8_blocks(a.cols);
-  float w[NV][4];
+template <class D, int NV, int V>
+__device__ __forceinline__ void load_weight(const RmsArgs& a, int t, float (&w)[NV][V]) {
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = (j * TPR + t) * 4 + k;
+    for (int k = 0; k < V; ++k) {
+      const int c = D::first(j, t) + D::STRIDE * k;
       w[j][k] = a.w && c < a.cols ? a.w[c] : 1.f;
     }
+}
+
+// y = t / sqrt(mean(t^2) + eps) * w for t = x + res, in fp32; t is rounded
+// once where it is stored, y once where it is stored (y is formed from the
+// unrounded t).
+template <int TPR, int NV, int V, bool VEC, int TI, int TO>
+__global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
+  using D = Cols<TPR, V, VEC>;
+  __shared__ typename RowSum<TPR, 1>::Lds lds;
+  RowSum<TPR, 1> sum(lds);
+  const int nb = rows8_blocks(a.cols);
+  Rows<TPR> q;
+  float w[NV][V];
+  load_weight<D>(a, q.t, w);
   const float mean = 1.f / (float)a.cols;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * RPB) {
-    const int64_t base = r * a.cols;
-    float v[NV][4], s = 0.f;
+  for (; q.row < a.rows; q.row += q.next) {
+    const int64_t base = q.row * a.cols;
+    const uint32_t o = (uint32_t)(q.sub * a.cols);
+    const int cols = q.row + q.sub < a.rows ? a.cols : 0;
+    float v[NV][V], s[1] = {0.f};
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      load_cols<TI, VEC>(a.x, base, c, a.cols, v[j]);
-      if (a.res) {
-        float o[4];
-        load_cols<TI, VEC>(a.res, base, c, a.cols, o);
+    for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, v[j]);
+    if (a.res) {
+      float r[NV][V];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[j][k] += o[k];
-      }
+      for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, r[j]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) s += v[j][k] * v[j][k];
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[j][k] += r[j][k];
     }
-    s = row_sum<TPR>(s, lds);
-    const float inv = 1.f / sqrtf(s * mean + a.eps);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[0] += v[j][k] * v[j][k];
+    sum(s);
+    const float inv = rsqrtf(s[0] * mean + a.eps);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      if (a.total) store_cols<TI, VEC>(a.total, base, c, a.cols, v[j]);
-      float y[4];
+      const int c = D::first(j, q.t);
+      if (a.total) store_cols<TI, D>(a.total, base, o, c, cols, v[j]);
+      float y[V];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = v[j][k] * inv * w[j][k];
+      for (int k = 0; k < V; ++k) y[k] = v[j][k] * inv * w[j][k];
       if constexpr (TO == MGN_E4M3)
-        store_cols8<TPR, VEC>((uint8_t*)a.y + base, a.y_scale + r * nb, c, a.cols, y);
+        store_cols8<D>((uint8_t*)a.y + base + o, a.y_scale + (q.row + q.sub) * nb, c, a.cols, y, cols > 0);
       else
-        store_cols<TO, VEC>(a.y, base, c, a.cols, y);
+        store_cols<TO, D>(a.y, base, o, c, cols, y);
     }
   }
 }
@@ -130,85 +182,86 @@ __global__ __launch_bounds__(NT) void rms_norm_kernel(RmsArgs a) {
 //   dt = (w dy - u mean(u w dy)) inv + d_total;  dw += dy u.
 // Each thread sums dw of its columns over its rows in fp32; the workgroup's
 // row groups are added in order and leave one partial per column.
-template <int TPR, int NV, bool VEC, int TI>
-__global__ __launch_bounds__(NT) void rms_grad_kernel(RmsArgs a) {
-  __shared__ float lds[4];
-  __shared__ float part[NV * TPR * 4 <= 1024 ? NT * NV * 4 : 1];
-  const int t = threadIdx.x % TPR;
-  constexpr int RPB = NT / TPR;
-  float w[NV][4], dw[NV][4];
+template <int TPR, int NV, int V, bool VEC, int TI>
+__global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
+  using D = Cols<TPR, V, VEC>;
+  constexpr int NT = threads(TPR), GROUPS = NT / TPR, W = NV * TPR * V;  // row groups; columns dealt to one
+  __shared__ typename RowSum<TPR, 2>::Lds lds;
+  RowSum<TPR, 2> sums(lds);
+  __shared__ float part[GROUPS > 1 ? GROUPS * W : 1];
+  Rows<TPR> q;
+  float w[NV][V], dw[NV][V];
+  load_weight<D>(a, q.t, w);
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int c = (j * TPR + t) * 4 + k;
-      w[j][k] = a.w && c < a.cols ? a.w[c] : 1.f;
-      dw[j][k] = 0.f;
-    }
+    for (int k = 0; k < V; ++k) dw[j][k] = 0.f;
   const float mean = 1.f / (float)a.cols;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * RPB) {
-    const int64_t base = r * a.cols;
-    float v[NV][4], g[NV][4], s = 0.f, p = 0.f;
+  for (; q.row < a.rows; q.row += q.next) {
+    const int64_t base = q.row * a.cols;
+    const uint32_t o = (uint32_t)(q.sub * a.cols);
+    const int cols = q.row + q.sub < a.rows ? a.cols : 0;
+    float v[NV][V], g[NV][V], r[NV][V], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      load_cols<TI, VEC>(a.x, base, c, a.cols, v[j]);
-      load_cols<TI, VEC>(a.dy, base, c, a.cols, g[j]);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        s += v[j][k] * v[j][k];
-        p += v[j][k] * (g[j][k] * w[j][k]);
-      }
+      load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, v[j]);
+      load_cols<TI, D>(a.dy, base, o, D::first(j, q.t), cols, g[j]);
+      if (a.res) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, r[j]);
     }
-    s = row_sum<TPR>(s, lds);
-    p = row_sum<TPR>(p, lds);
-    const float inv = 1.f / sqrtf(s * mean + a.eps);
-    const float m = p * inv * mean;  // mean(u w dy)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        s[0] += v[j][k] * v[j][k];
+        s[1] += v[j][k] * (g[j][k] * w[j][k]);
+      }
+    sums(s);
+    const float inv = rsqrtf(s[0] * mean + a.eps);
+    const float m = s[1] * inv * mean;  // mean(u w dy)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + t) * 4;
-      float d[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-      if (a.res) load_cols<TI, VEC>(a.res, base, c, a.cols, o);
+      float d[V];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < V; ++k) {
         const float u = v[j][k] * inv;
-        d[k] = (g[j][k] * w[j][k] - u * m) * inv + o[k];
+        d[k] = (g[j][k] * w[j][k] - u * m) * inv;
+        if (a.res) d[k] += r[j][k];
         dw[j][k] += g[j][k] * u;
       }
-      store_cols<TI, VEC>(a.total, base, c, a.cols, d);
+      store_cols<TI, D>(a.total, base, o, D::first(j, q.t), cols, d);
     }
   }
   if (!a.part) return;
   float* dst = a.part + (int64_t)blockIdx.x * a.cols;
-  if constexpr (TPR == NT) {
+  if constexpr (GROUPS == 1) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int c = (j * TPR + t) * 4 + k;
+      for (int k = 0; k < V; ++k) {
+        const int c = D::first(j, q.t) + D::STRIDE * k;
         if (c < a.cols) dst[c] = dw[j][k];
       }
   } else {
-    constexpr int W = NV * TPR * 4;  // columns dealt to a row's threads
     const int grp = threadIdx.x / TPR;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) part[grp * W + (j * TPR + t) * 4 + k] = dw[j][k];
+      for (int k = 0; k < V; ++k) part[grp * W + D::first(j, q.t) + D::STRIDE * k] = dw[j][k];
     __syncthreads();
     for (int c = threadIdx.x; c < a.cols; c += NT) {
-      float sum = part[c];
-      for (int q = 1; q < RPB; ++q) sum += part[q * W + c];
-      dst[c] = sum;
+      float total = part[c];
+      for (int e = 1; e < GROUPS; ++e) total += part[e * W + c];
+      dst[c] = total;
     }
   }
 }
 
 // dw from the workgroups' partials, added in fp64 in a fixed order: a wave
 // per column group of 16 columns, four partial rows at a time.
-__global__ __launch_bounds__(NT) void rms_dw_kernel(const float* __restrict__ part, int parts, int cols, int accumulate,
+constexpr int DW_NT = 256;
+__global__ __launch_bounds__(DW_NT) void rms_dw_kernel(const float* __restrict__ part, int parts, int cols, int accumulate,
                                                     float* __restrict__ dw) {
-  __shared__ double lds[NT];
+  __shared__ double lds[DW_NT];
   const int c = blockIdx.x * 16 + threadIdx.x % 16, g = threadIdx.x / 16;
   double s = 0;
   if (c < cols)
@@ -221,102 +274,122 @@ __global__ __launch_bounds__(NT) void rms_dw_kernel(const float* __restrict__ pa
   }
 }
 
+// Rows at a time are dealt to at most this many workgroups, which then go
+// through them in turn.
+constexpr int ROW_GRID = 8192;
 int row_grid(int64_t rows, int rpb, int most) {
   const int64_t b = (rows + rpb - 1) / rpb;
   return (int)(b < most ? b : most);
 }
 
-constexpr int ROW_GRID = 8192;
+template <int N>
+using Int = std::integral_constant<int, N>;
 
-// Calls f(TPR, NV) with the dealing of `cols` columns as constants.
-template <class F>
-hipError_t by_cols(int cols, F f) {
-  if (cols <= 64) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-  if (cols <= 128) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
-  if (cols <= 256) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-  if (cols <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-  if (cols <= 8192) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 8>());
-  return hipErrorInvalidValue;
+// Calls f(TPR, NV, V, VEC) with the dealing of `cols` columns as constants.
+// vec: how many columns every array allows to be read at once (8, 4 or 1).  8
+// columns a thread (16 bytes of bf16) halve the instructions a row costs.
+// VMAX: the most the operands' types make use of.
+template <int VMAX, class F>
+hipError_t by_cols(int cols, int vec, F f) {
+  if (cols <= 16) return f(Int<4>(), Int<1>(), Int<4>(), std::false_type());
+  if constexpr (VMAX == 8)
+    if (vec == 8) {
+      const Int<8> v;
+      const std::true_type y;
+      if (cols <= 128) return f(Int<16>(), Int<1>(), v, y);
+      if (cols <= 256) return f(Int<32>(), Int<1>(), v, y);
+      if (cols <= 1024) return f(Int<64>(), Int<2>(), v, y);
+      if (cols <= 2048) return f(Int<256>(), Int<1>(), v, y);
+      if (cols <= 8192) return f(Int<1024>(), Int<1>(), v, y);
+      return hipErrorInvalidValue;
+    }
+  const Int<4> v;
+  const auto four = [&](auto y) {
+    if (cols <= 64) return f(Int<16>(), Int<1>(), v, y);
+    if (cols <= 128) return f(Int<32>(), Int<1>(), v, y);
+    if (cols <= 256) return f(Int<64>(), Int<1>(), v, y);
+    if (cols <= 1024) return f(Int<64>(), Int<4>(), v, y);
+    if (cols <= 2048) return f(Int<256>(), Int<2>(), v, y);
+    if (cols <= 8192) return f(Int<1024>(), Int<2>(), v, y);
+    return hipErrorInvalidValue;
+  };
+  return vec >= 4 ? four(std::true_type()) : four(std::false_type());
 }
 
-template <class F>
-hipError_t by_flag(bool v, F f) {
-  return v ? f(std::true_type()) : f(std::false_type());
+// Columns of the type that may be read at once: rows begin at multiples of
+// `cols` elements from p (null: no array).
+int vec_of(const void* p, int type, int cols) {
+  if (!p) return 8;
+  const int size = type == MGN_FP32 ? 4 : type == MGN_BF16 ? 2 : 1;
+  for (int v = 8; v >= 4; v -= 4) {
+    const int bytes = v * size < 16 ? v * size : 16;
+    if (cols % v == 0 && (uintptr_t)p % bytes == 0) return v;
+  }
+  return 1;
+}
+int least(std::initializer_list<int> v) {
+  int m = 8;
+  for (int x : v) m = x < m ? x : m;
+  return m;
 }
 
+// Calls f(TYPE, TPR, NV, V, VEC) for rows of the type.
 template <class F>
-hipError_t by_type(int type, F f) {
-  return type == MGN_BF16 ? f(std::integral_constant<int, MGN_BF16>()) : f(std::integral_constant<int, MGN_FP32>());
-}
-
-// Whether rows of `cols` columns of the type may be read four columns at a time.
-bool vec_ok(const void* p, int type, int cols) {
-  return cols % 4 == 0 && (uintptr_t)p % (type == MGN_FP32 ? 16 : type == MGN_BF16 ? 8 : 4) == 0;
+hipError_t by_rows(int type, int cols, int vec, F f) {
+  if (type == MGN_BF16)
+    return by_cols<8>(cols, vec, [&](auto t, auto n, auto v, auto y) { return f(Int<MGN_BF16>(), t, n, v, y); });
+  return by_cols<4>(cols, vec, [&](auto t, auto n, auto v, auto y) { return f(Int<MGN_FP32>(), t, n, v, y); });
 }
 
 }  // namespace
 
 hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st) {
-  const bool vec = vec_ok(a.x, type, a.cols) && vec_ok(a.q, MGN_E4M3, a.cols);
-  return by_cols(a.cols, [&](auto tpr, auto nv) {
-    return by_flag(vec, [&](auto v) {
-      return by_type(type, [&](auto ti) {
-        hipLaunchKernelGGL((store8_kernel<tpr(), nv(), v(), ti()>), dim3(row_grid(a.n, NT / tpr(), ROW_GRID)), dim3(NT), 0, st, a);
-        return hipGetLastError();
-      });
-    });
+  const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.q, MGN_E4M3, a.cols)});
+  return by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+    hipLaunchKernelGGL((store8_kernel<tpr(), nv(), v(), y(), ti()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, ROW_GRID)),
+                       dim3(Rows<tpr()>::NT), 0, st, a);
+    return hipGetLastError();
   });
 }
 
 hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st) {
-  const bool vec = vec_ok(a.out, type, a.cols) && vec_ok(a.q, MGN_E4M3, a.cols);
-  return by_cols(a.cols, [&](auto tpr, auto nv) {
-    return by_flag(vec, [&](auto v) {
-      return by_type(type, [&](auto to) {
-        hipLaunchKernelGGL((load8_kernel<tpr(), nv(), v(), to()>), dim3(row_grid(a.n, NT / tpr(), ROW_GRID)), dim3(NT), 0, st, a);
-        return hipGetLastError();
-      });
-    });
+  const int vec = least({vec_of(a.out, type, a.cols), vec_of(a.q, MGN_E4M3, a.cols)});
+  return by_rows(type, a.cols, vec, [&](auto to, auto tpr, auto nv, auto v, auto y) {
+    hipLaunchKernelGGL((load8_kernel<tpr(), nv(), v(), y(), to()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, ROW_GRID)),
+                       dim3(Rows<tpr()>::NT), 0, st, a);
+    return hipGetLastError();
   });
 }
 
 hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t st) {
-  const bool vec = vec_ok(a.x, type, a.cols) && vec_ok(a.res, type, a.cols) && vec_ok(a.total, type, a.cols) &&
-                   vec_ok(a.y, y_type, a.cols);
-  return by_cols(a.cols, [&](auto tpr, auto nv) {
-    return by_flag(vec, [&](auto v) {
-      return by_type(type, [&](auto ti) {
-        const dim3 grid(row_grid(a.rows, NT / tpr(), ROW_GRID));
-        if (y_type == MGN_E4M3)
-          hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), ti(), MGN_E4M3>), grid, dim3(NT), 0, st, a);
-        else if (y_type == MGN_BF16)
-          hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), ti(), MGN_BF16>), grid, dim3(NT), 0, st, a);
-        else
-          hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), ti(), MGN_FP32>), grid, dim3(NT), 0, st, a);
-        return hipGetLastError();
-      });
-    });
+  const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.res, type, a.cols), vec_of(a.total, type, a.cols),
+                         vec_of(a.y, y_type, a.cols)});
+  return by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+    const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, ROW_GRID));
+    if (y_type == MGN_E4M3)
+      hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), y(), ti(), MGN_E4M3>), grid, dim3(Rows<tpr()>::NT), 0, st, a);
+    else if (y_type == MGN_BF16)
+      hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), y(), ti(), MGN_BF16>), grid, dim3(Rows<tpr()>::NT), 0, st, a);
+    else
+      hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), y(), ti(), MGN_FP32>), grid, dim3(Rows<tpr()>::NT), 0, st, a);
+    return hipGetLastError();
   });
 }
 
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st) {
-  const bool vec = vec_ok(a.x, type, a.cols) && vec_ok(a.res, type, a.cols) && vec_ok(a.total, type, a.cols) &&
-                   vec_ok(a.dy, type, a.cols);
   int grid = 0;
   if (a.rows > 0) {
-    const hipError_t e = by_cols(a.cols, [&](auto tpr, auto nv) {
-      grid = row_grid(a.rows, NT / tpr(), MGN_RMS_WORK_PER_COL);
-      return by_flag(vec, [&](auto v) {
-        return by_type(type, [&](auto ti) {
-          hipLaunchKernelGGL((rms_grad_kernel<tpr(), nv(), v(), ti()>), dim3(grid), dim3(NT), 0, st, a);
-          return hipGetLastError();
-        });
-      });
+    const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.res, type, a.cols), vec_of(a.total, type, a.cols),
+                           vec_of(a.dy, type, a.cols)});
+    const hipError_t e = by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+      grid = row_grid(a.rows, Rows<tpr()>::RPB, MGN_RMS_WORK_PER_COL);
+      hipLaunchKernelGGL((rms_grad_kernel<tpr(), nv(), v(), y(), ti()>), dim3(grid), dim3(Rows<tpr()>::NT), 0, st, a);
+      return hipGetLastError();
     });
     if (e != hipSuccess) return e;
   }
   if (!dw) return hipSuccess;
-  hipLaunchKernelGGL(rms_dw_kernel, dim3((a.cols + 15) / 16), dim3(NT), 0, st, a.part, grid, a.cols, accumulate, dw);
+  hipLaunchKernelGGL(rms_dw_kernel, dim3((a.cols + 15) / 16), dim3(DW_NT), 0, st, a.part, grid, a.cols, accumulate, dw);
   return hipGetLastError();
 }
 

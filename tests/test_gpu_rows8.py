@@ -62,6 +62,9 @@ def test_every_code_reads_back():
         mgn.mgn_rows_load8(q, s, y)
         want = q.cpu().view(torch.float8_e4m3fn).float() * torch.tensor(scale)
         assert torch.equal(y.cpu().nan_to_num(nan=7e37), want.nan_to_num(nan=7e37)), scale
+        z = torch.empty(2, 128, dtype=torch.bfloat16, device="cuda")
+        mgn.mgn_rows_load8(q, s, z)
+        assert torch.equal(z.cpu().float().nan_to_num(nan=7e37), want.bfloat16().float().nan_to_num(nan=7e37)), scale
 
 
 @pytest.mark.parametrize("cols", [128, 130, 640])
