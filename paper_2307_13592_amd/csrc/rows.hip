@@ -68,9 +68,9 @@ struct Rows {
 
 // --------------------------------------------------------- rows in 8 bits ---
 
-template <int TPR, int NV, int V, bool VEC, int TI>
+template <int TPR, int NV, int V, int MODE, int TI>
 __global__ __launch_bounds__(threads(TPR)) void store8_kernel(Rows8Args a) {
-  using D = Cols<TPR, V, VEC>;
+  using D = Cols<TPR, V, MODE>;
   const int nb = rows8_blocks(a.cols);
   Rows<TPR> w;
   for (; w.row < a.n; w.row += w.next) {
@@ -82,15 +82,15 @@ __global__ __launch_bounds__(threads(TPR)) void store8_kernel(Rows8Args a) {
     for (int j = 0; j < NV; ++j) {
       const int c = D::first(j, w.t);
       float v[V];
-      load_cols<TI, D>(a.x, ok ? r * a.cols : 0, 0, c, ok ? a.cols : 0, v);
+      load_cols<TI, D>(a.x, ok ? r * a.cols : 0, 0, c, ok ? a.cols : 0, (a.n_rows - r) * a.cols, v);
       store_cols8<D>(a.q + (ok ? s * a.cols : 0), a.scale + (ok ? s * nb : 0), c, a.cols, v, ok);
     }
   }
 }
 
-template <int TPR, int NV, int V, bool VEC, int TO>
+template <int TPR, int NV, int V, int MODE, int TO>
 __global__ __launch_bounds__(threads(TPR)) void load8_kernel(Rows8Args a) {
-  using D = Cols<TPR, V, VEC>;
+  using D = Cols<TPR, V, MODE>;
   const int nb = rows8_blocks(a.cols);
   Rows<TPR> w;
   for (; w.row < a.n; w.row += w.next) {
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(threads(TPR)) void load8_kernel(Rows8Args a) {
       load_cols8<D>(a.q + s * a.cols, a.scale[s * nb + c / ROWS8_BLOCK], c, a.cols, v);
       if (a.add) {
         float o[V];
-        load_cols<TO, D>(a.out, r * a.cols, 0, c, a.cols, o);
+        load_cols<TO, D>(a.out, r * a.cols, 0, c, a.cols, (a.n_rows - r) * a.cols, o);
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] += o[k];
       }
@@ -120,20 +120,22 @@ __global__ __launch_bounds__(threads(TPR)) void load8_kernel(Rows8Args a) {
 template <class D, int NV, int V>
 __device__ __forceinline__ void load_weight(const RmsArgs& a, int t, float (&w)[NV][V]) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int j = 0; j < NV; ++j) {
+    if (a.w) {
+      load_values<D>(a.w, D::first(j, t), a.cols, w[j]);
+    } else {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int c = D::first(j, t) + D::STRIDE * k;
-      w[j][k] = a.w && c < a.cols ? a.w[c] : 1.f;
+      for (int k = 0; k < V; ++k) w[j][k] = 1.f;
     }
+  }
 }
 
 // y = t / sqrt(mean(t^2) + eps) * w for t = x + res, in fp32; t is rounded
 // once where it is stored, y once where it is stored (y is formed from the
 // unrounded t).
-template <int TPR, int NV, int V, bool VEC, int TI, int TO>
+template <int TPR, int NV, int V, int MODE, int TI, int TO>
 __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
-  using D = Cols<TPR, V, VEC>;
+  using D = Cols<TPR, V, MODE>;
   __shared__ typename RowSum<TPR, 1>::Lds lds;
   RowSum<TPR, 1> sum(lds);
   const int nb = rows8_blocks(a.cols);
@@ -143,15 +145,16 @@ __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
   const float mean = 1.f / (float)a.cols;
   for (; q.row < a.rows; q.row += q.next) {
     const int64_t base = q.row * a.cols;
+    const int64_t left = a.rows * a.cols - base;
     const uint32_t o = (uint32_t)(q.sub * a.cols);
     const int cols = q.row + q.sub < a.rows ? a.cols : 0;
     float v[NV][V], s[1] = {0.f};
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, v[j]);
+    for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, left, v[j]);
     if (a.res) {
       float r[NV][V];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, r[j]);
+      for (int j = 0; j < NV; ++j) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, left, r[j]);
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -182,9 +185,9 @@ __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
 //   dt = (w dy - u mean(u w dy)) inv + d_total;  dw += dy u.
 // Each thread sums dw of its columns over its rows in fp32; the workgroup's
 // row groups are added in order and leave one partial per column.
-template <int TPR, int NV, int V, bool VEC, int TI>
+template <int TPR, int NV, int V, int MODE, int TI>
 __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
-  using D = Cols<TPR, V, VEC>;
+  using D = Cols<TPR, V, MODE>;
   constexpr int NT = threads(TPR), GROUPS = NT / TPR, W = NV * TPR * V;  // row groups; columns dealt to one
   __shared__ typename RowSum<TPR, 2>::Lds lds;
   RowSum<TPR, 2> sums(lds);
@@ -199,14 +202,15 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
   const float mean = 1.f / (float)a.cols;
   for (; q.row < a.rows; q.row += q.next) {
     const int64_t base = q.row * a.cols;
+    const int64_t left = a.rows * a.cols - base;
     const uint32_t o = (uint32_t)(q.sub * a.cols);
     const int cols = q.row + q.sub < a.rows ? a.cols : 0;
     float v[NV][V], g[NV][V], r[NV][V], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, v[j]);
-      load_cols<TI, D>(a.dy, base, o, D::first(j, q.t), cols, g[j]);
-      if (a.res) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, r[j]);
+      load_cols<TI, D>(a.x, base, o, D::first(j, q.t), cols, left, v[j]);
+      load_cols<TI, D>(a.dy, base, o, D::first(j, q.t), cols, left, g[j]);
+      if (a.res) load_cols<TI, D>(a.res, base, o, D::first(j, q.t), cols, left, r[j]);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -256,28 +260,33 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
   }
 }
 
-// dw from the workgroups' partials, added in fp64 in a fixed order: a wave
-// per column group of 16 columns, four partial rows at a time.
-constexpr int DW_NT = 256;
-__global__ __launch_bounds__(DW_NT) void rms_dw_kernel(const float* __restrict__ part, int parts, int cols, int accumulate,
-                                                    float* __restrict__ dw) {
+// dw from the workgroups' partials, added in fp64 in a fixed order: a workgroup
+// per 16 columns, 64 of its threads to a column, each over every 64th partial.
+constexpr int DW_NT = 1024, DW_COLS = 16;
+__global__ __launch_bounds__(DW_NT) void rms_dw_kernel(const float* __restrict__ part, int parts, int cols,
+                                                       int accumulate, float* __restrict__ dw) {
+  constexpr int G = DW_NT / DW_COLS;
   __shared__ double lds[DW_NT];
-  const int c = blockIdx.x * 16 + threadIdx.x % 16, g = threadIdx.x / 16;
+  const int c = blockIdx.x * DW_COLS + threadIdx.x % DW_COLS, g = threadIdx.x / DW_COLS;
   double s = 0;
   if (c < cols)
-    for (int q = g; q < parts; q += 16) s += part[(int64_t)q * cols + c];
+#pragma unroll 8
+    for (int q = g; q < parts; q += G) s += part[(int64_t)q * cols + c];
   lds[threadIdx.x] = s;
-  __syncthreads();
-  if (g == 0 && c < cols) {
-    for (int q = 1; q < 16; ++q) s += lds[q * 16 + threadIdx.x];
-    dw[c] = (float)(accumulate ? s + dw[c] : s);
+  for (int n = G / 2; n; n /= 2) {
+    __syncthreads();
+    if (g < n) lds[threadIdx.x] += lds[threadIdx.x + n * DW_COLS];
   }
+  if (g == 0 && c < cols) dw[c] = (float)(accumulate ? lds[threadIdx.x] + dw[c] : lds[threadIdx.x]);
 }
 
 // Rows at a time are dealt to at most this many workgroups, which then go
-// through them in turn.
-constexpr int ROW_GRID = 8192;
-int row_grid(int64_t rows, int rpb, int most) {
+// through them in turn: each reads the weights once (1M x 128 fp32 rows with a
+// residual 404 us with 8,192, 354 with 32,768, 336 with one turn each; 2M x 128
+// bf16 into 8-bit rows 287, 289 and 315).  Reading 8-bit rows back needs none
+// (2M x 128 to fp32 229, 224 and 178 us).
+constexpr int64_t NORM_GRID = 32768, STORE_GRID = 8192, LOAD_GRID = 1 << 20;
+int row_grid(int64_t rows, int rpb, int64_t most) {
   const int64_t b = (rows + rpb - 1) / rpb;
   return (int)(b < most ? b : most);
 }
@@ -285,87 +294,79 @@ int row_grid(int64_t rows, int rpb, int most) {
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-// Calls f(TPR, NV, V, VEC) with the dealing of `cols` columns as constants.
-// vec: how many columns every array allows to be read at once (8, 4 or 1).  8
-// columns a thread (16 bytes of bf16) halve the instructions a row costs.
-// VMAX: the most the operands' types make use of.
-template <int VMAX, class F>
-hipError_t by_cols(int cols, int vec, F f) {
-  if (cols <= 16) return f(Int<4>(), Int<1>(), Int<4>(), std::false_type());
-  if constexpr (VMAX == 8)
-    if (vec == 8) {
+// Calls f(TPR, NV, V, MODE) with the dealing of `cols` columns of the type as
+// constants: 16 bytes a run, as few threads a row as hold it.
+template <int TYPE, class F>
+hipError_t by_cols(int cols, RowMode mode, F f) {
+  if (cols <= 16) return f(Int<4>(), Int<1>(), Int<4>(), Int<APART>());
+  const auto runs = [&](auto m) {
+    if constexpr (TYPE == MGN_BF16) {
       const Int<8> v;
-      const std::true_type y;
-      if (cols <= 128) return f(Int<16>(), Int<1>(), v, y);
-      if (cols <= 256) return f(Int<32>(), Int<1>(), v, y);
-      if (cols <= 1024) return f(Int<64>(), Int<2>(), v, y);
-      if (cols <= 2048) return f(Int<256>(), Int<1>(), v, y);
-      if (cols <= 8192) return f(Int<1024>(), Int<1>(), v, y);
-      return hipErrorInvalidValue;
+      if (cols <= 128) return f(Int<16>(), Int<1>(), v, m);
+      if (cols <= 256) return f(Int<32>(), Int<1>(), v, m);
+      if (cols <= 512) return f(Int<64>(), Int<1>(), v, m);
+      if (cols <= 1024) return f(Int<64>(), Int<2>(), v, m);
+      if (cols <= 2048) return f(Int<256>(), Int<1>(), v, m);
+      if (cols <= 8192) return f(Int<1024>(), Int<1>(), v, m);
+    } else {
+      const Int<4> v;
+      if (cols <= 64) return f(Int<16>(), Int<1>(), v, m);
+      if (cols <= 128) return f(Int<32>(), Int<1>(), v, m);
+      if (cols <= 256) return f(Int<64>(), Int<1>(), v, m);
+      if (cols <= 1024) return f(Int<64>(), Int<4>(), v, m);
+      if (cols <= 2048) return f(Int<256>(), Int<2>(), v, m);
+      if (cols <= 8192) return f(Int<1024>(), Int<2>(), v, m);
     }
-  const Int<4> v;
-  const auto four = [&](auto y) {
-    if (cols <= 64) return f(Int<16>(), Int<1>(), v, y);
-    if (cols <= 128) return f(Int<32>(), Int<1>(), v, y);
-    if (cols <= 256) return f(Int<64>(), Int<1>(), v, y);
-    if (cols <= 1024) return f(Int<64>(), Int<4>(), v, y);
-    if (cols <= 2048) return f(Int<256>(), Int<2>(), v, y);
-    if (cols <= 8192) return f(Int<1024>(), Int<2>(), v, y);
     return hipErrorInvalidValue;
   };
-  return vec >= 4 ? four(std::true_type()) : four(std::false_type());
+  return mode == STREAM ? runs(Int<STREAM>()) : mode == WHOLE ? runs(Int<WHOLE>()) : runs(Int<RUNS>());
 }
 
-// Columns of the type that may be read at once: rows begin at multiples of
-// `cols` elements from p (null: no array).
-int vec_of(const void* p, int type, int cols) {
-  if (!p) return 8;
-  const int size = type == MGN_FP32 ? 4 : type == MGN_BF16 ? 2 : 1;
-  for (int v = 8; v >= 4; v -= 4) {
-    const int bytes = v * size < 16 ? v * size : 16;
-    if (cols % v == 0 && (uintptr_t)p % bytes == 0) return v;
-  }
-  return 1;
-}
-int least(std::initializer_list<int> v) {
-  int m = 8;
-  for (int x : v) m = x < m ? x : m;
-  return m;
-}
-
-// Calls f(TYPE, TPR, NV, V, VEC) for rows of the type.
+// Calls f(TYPE, TPR, NV, V, MODE) for rows of the type.
 template <class F>
-hipError_t by_rows(int type, int cols, int vec, F f) {
+hipError_t by_rows(int type, int cols, RowMode mode, F f) {
   if (type == MGN_BF16)
-    return by_cols<8>(cols, vec, [&](auto t, auto n, auto v, auto y) { return f(Int<MGN_BF16>(), t, n, v, y); });
-  return by_cols<4>(cols, vec, [&](auto t, auto n, auto v, auto y) { return f(Int<MGN_FP32>(), t, n, v, y); });
+    return by_cols<MGN_BF16>(cols, mode, [&](auto t, auto n, auto v, auto m) { return f(Int<MGN_BF16>(), t, n, v, m); });
+  return by_cols<MGN_FP32>(cols, mode, [&](auto t, auto n, auto v, auto m) { return f(Int<MGN_FP32>(), t, n, v, m); });
 }
+
+// How a kernel that moves `bytes` reads its rows: as whole runs where they are
+// that, on 16-byte boundaries, and past the caches where it moves more than the
+// last-level cache holds (256 MB).  Above: 2M x 128 bf16 rows with a residual
+// into 8-bit rows 324 us through the caches, 287 past them.  Below, where the
+// rows may still be cached: 200k of 400k x 256 bf16 rows gathered 28.4 and 34.7.
+RowMode row_mode(int64_t bytes, int type, int cols, std::initializer_list<const void*> arrays) {
+  bool even = cols % (type == MGN_FP32 ? 4 : 8) == 0;
+  for (const void* p : arrays) even = even && (uintptr_t)p % 16 == 0;
+  return !even ? RUNS : bytes > ((int64_t)256 << 20) ? STREAM : WHOLE;
+}
+int64_t type_bytes(int type) { return type == MGN_FP32 ? 4 : type == MGN_BF16 ? 2 : 1; }
 
 }  // namespace
 
 hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st) {
-  const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.q, MGN_E4M3, a.cols)});
-  return by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
-    hipLaunchKernelGGL((store8_kernel<tpr(), nv(), v(), y(), ti()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, ROW_GRID)),
+  const RowMode mode = row_mode(a.n * a.cols * (type_bytes(type) + 1), type, a.cols, {a.x});
+  return by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+    hipLaunchKernelGGL((store8_kernel<tpr(), nv(), v(), y(), ti()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, STORE_GRID)),
                        dim3(Rows<tpr()>::NT), 0, st, a);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st) {
-  const int vec = least({vec_of(a.out, type, a.cols), vec_of(a.q, MGN_E4M3, a.cols)});
-  return by_rows(type, a.cols, vec, [&](auto to, auto tpr, auto nv, auto v, auto y) {
-    hipLaunchKernelGGL((load8_kernel<tpr(), nv(), v(), y(), to()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, ROW_GRID)),
+  const RowMode mode = row_mode(0, type, a.cols, {a.add ? a.out : nullptr});
+  return by_rows(type, a.cols, mode, [&](auto to, auto tpr, auto nv, auto v, auto y) {
+    hipLaunchKernelGGL((load8_kernel<tpr(), nv(), v(), y(), to()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, LOAD_GRID)),
                        dim3(Rows<tpr()>::NT), 0, st, a);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t st) {
-  const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.res, type, a.cols), vec_of(a.total, type, a.cols),
-                         vec_of(a.y, y_type, a.cols)});
-  return by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
-    const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, ROW_GRID));
+  const int64_t per = type_bytes(type) * (1 + (a.res != nullptr) + (a.total != nullptr)) + type_bytes(y_type);
+  const RowMode mode = row_mode(a.rows * a.cols * per, type, a.cols, {a.x, a.res});
+  return by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+    const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, NORM_GRID));
     if (y_type == MGN_E4M3)
       hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), y(), ti(), MGN_E4M3>), grid, dim3(Rows<tpr()>::NT), 0, st, a);
     else if (y_type == MGN_BF16)
@@ -379,9 +380,9 @@ hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t s
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st) {
   int grid = 0;
   if (a.rows > 0) {
-    const int vec = least({vec_of(a.x, type, a.cols), vec_of(a.res, type, a.cols), vec_of(a.total, type, a.cols),
-                           vec_of(a.dy, type, a.cols)});
-    const hipError_t e = by_rows(type, a.cols, vec, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
+      const RowMode mode = row_mode(a.rows * a.cols * type_bytes(type) * (3 + (a.res != nullptr)), type, a.cols,
+                                  {a.x, a.dy, a.res});
+    const hipError_t e = by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
       grid = row_grid(a.rows, Rows<tpr()>::RPB, MGN_RMS_WORK_PER_COL);
       hipLaunchKernelGGL((rms_grad_kernel<tpr(), nv(), v(), y(), ti()>), dim3(grid), dim3(Rows<tpr()>::NT), 0, st, a);
       return hipGetLastError();
@@ -389,7 +390,7 @@ hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accum
     if (e != hipSuccess) return e;
   }
   if (!dw) return hipSuccess;
-  hipLaunchKernelGGL(rms_dw_kernel, dim3((a.cols + 15) / 16), dim3(DW_NT), 0, st, a.part, grid, a.cols, accumulate, dw);
+  hipLaunchKernelGGL(rms_dw_kernel, dim3((a.cols + DW_COLS - 1) / DW_COLS), dim3(DW_NT), 0, st, a.part, grid, a.cols, accumulate, dw);
   return hipGetLastError();
 }
 
