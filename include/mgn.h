@@ -265,8 +265,9 @@ mgn_status mgn_rows_load8(const uint8_t* q, const float* scale, int64_t n_slots,
  * y_scale (NULL otherwise).  weight: fp32 [cols], or NULL for ones.  Sums are
  * taken in fp32 and y from the unrounded t.  total may be x or res, and y may
  * be x or res if it has their type and total is not that array too; no other
- * overlap.  A row whose squares pass the fp32 range gives zeros, a NaN or an
- * infinity in a row NaNs there.  eps > 0 and finite. */
+ * overlap.  A row whose squares pass the fp32 range gives zeros (and has no
+ * gradient), a NaN or an infinity in a row NaNs there.  eps is a positive normal
+ * number. */
 mgn_status mgn_rms_norm(const void* x, const void* res, int32_t type, int64_t rows, int32_t cols, const float* weight,
                         float eps, void* total, void* y, int32_t y_type, float* y_scale, mgn_stream stream);
 /* Its backward: total [rows][cols] is the sum that was normalised (x itself
@@ -295,10 +296,10 @@ mgn_status mgn_rms_norm_grad(const void* total, int32_t type, const float* weigh
  * entry begins a trajectory, its step takes 0 for h_{t-1}.  States are fp32: h
  * [steps][rows][cols] (NULL: not stored), h_last [rows][cols] = the last state
  * (NULL: not wanted; it may be h0, so that a rollout's step updates its state
- * in place; with no steps it is h0).  A weight f or z below 2^-126 counts as 0
- * and its term is left out whatever it multiplies: g = +inf (or the type's
- * largest value) holds a state through steps whose x is not defined, -inf
- * replaces it.
+ * in place; with no steps it is h0).  A weight f or z (or a product of
+ * successive f) below 2^-126 counts as 0 and its term is left out whatever it
+ * multiplies: g = +inf (or the type's largest value) holds a state, to a
+ * rounding, through steps whose x is not defined, -inf replaces it.
  * work: device scratch of mgn_gated_scan_work bytes, 16-byte aligned (NULL
  * when that is 0); MGN_E_NOMEM when work_bytes is less.  steps, rows >= 0,
  * 1 <= cols <= MGN_ROW_MAX_COLS.  Arrays must not overlap beyond what is
@@ -534,8 +535,9 @@ typedef enum {
   MGN_T_WEIGHT_GRAD = 7,   /* weight-gradient GEMMs and fixed-order reductions */
   MGN_T_OTHER = 8,         /* planning, loss */
   MGN_T_NODE_PROJ = 9,     /* per-node products of the edge MLP's first Linear (row-split edge kernels) */
-  MGN_T_EXCHANGE = 10,     /* halo exchange between partitions (mgn_copy_latents, mgn_add_latent_grads),
-                              timed on the owner's model */
+  MGN_T_EXCHANGE = 10,     /* halo exchange between partitions (mgn_copy_latents, mgn_add_latent_grads and
+                              their 8-bit forms), timed on the owner's model (what a lockstep step does on
+                              the holder's side, on the holder's) */
   MGN_T_COUNT = 11
 } mgn_timer;
 /* Starts (enable != 0) or stops recording; starting clears earlier records. */

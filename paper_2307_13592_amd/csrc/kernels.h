@@ -196,7 +196,8 @@ struct ScanArgs {
   float *h_last, *dh0;
   void *dg, *dx;
   void* work;
-  int64_t steps, rows, chunk;  // chunk: set by the launcher
+  int64_t steps, rows;
+  int64_t chunk, tile0;  // set by the launcher
   int cols;
 };
 

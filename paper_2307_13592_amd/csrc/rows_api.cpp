@@ -125,7 +125,7 @@ mgn_status mgn_rms_norm(const void* x, const void* res, int32_t type, int64_t ro
   const char* fn = "mgn_rms_norm";
   if (cols < 1 || cols > MGN_ROW_MAX_COLS || !size_ok(rows, cols)) return bad(fn, "bad sizes");
   if (!float_type(type) || !(float_type(y_type) || y_type == MGN_E4M3)) return bad(fn, "unknown storage type");
-  if (!(eps > 0.f) || !std::isfinite(eps)) return bad(fn, "eps must be positive");
+  if (!std::isnormal(eps) || eps < 0.f) return bad(fn, "eps must be positive (a normal number)");
   if ((y_type == MGN_E4M3) != (y_scale != nullptr) && rows > 0) return bad(fn, "y_scale goes with 8-bit rows");
   if (rows == 0) return MGN_OK;
   if (!x || !y) return bad(fn, "NULL argument");
@@ -160,7 +160,7 @@ mgn_status mgn_rms_norm_grad(const void* total, int32_t type, const float* weigh
   const char* fn = "mgn_rms_norm_grad";
   if (cols < 1 || cols > MGN_ROW_MAX_COLS || !size_ok(rows, cols)) return bad(fn, "bad sizes");
   if (!float_type(type)) return bad(fn, "unknown storage type");
-  if (!(eps > 0.f) || !std::isfinite(eps)) return bad(fn, "eps must be positive");
+  if (!std::isnormal(eps) || eps < 0.f) return bad(fn, "eps must be positive (a normal number)");
   if (rows > 0 && (!total || !dy || !dx)) return bad(fn, "NULL argument");
   if (dweight && !work) return bad(fn, "dweight needs work");
   const int64_t ts = type_size(type), n = rows * cols;

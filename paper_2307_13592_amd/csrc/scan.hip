@@ -192,7 +192,7 @@ template <int W, int V, int SEG, int TG, int TX, bool FIRST>
 __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
   __shared__ Joint<W, W == 1 ? 1 : V> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = W == 1 ? 0 : wave;
-  const Lane<V, TX> l(a, W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x);
+  const Lane<V, TX> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
   const int64_t C = l.C, i = l.i;
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
   constexpr int TD = TX == MGN_E4M3 ? TG : TX;
   __shared__ Joint<W, W == 1 ? 1 : V> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = W == 1 ? 0 : wave;
-  const Lane<V, TX> l(a, W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x);
+  const Lane<V, TX> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
   const int64_t C = l.C, i = l.i;
   const int c = blockIdx.y;
   // reversed steps u = steps - 1 - t of this chunk
@@ -409,9 +409,20 @@ constexpr int SEG4 = 4, SEG1 = 8;    // steps a wave holds with 4 columns a lane
 constexpr int64_t VEC_COLS = 65536;  // columns from which a lane takes four of them
 constexpr int64_t ALONE4 = 800, ALONE1 = 2048;  // waves from which one goes through the time axis alone
 constexpr int64_t FEW = 256;         // waves below which the time axis is cut into chunks
+constexpr int64_t LAUNCH = 1 << 20;  // tiles of one launch (a grid holds less than 2^32 threads)
 constexpr int64_t CHUNK_WGS = 512;   // workgroups of a chunked scan, at most about
 
-// How a scan is dealt.  vec: the arrays allow four columns a lane.
+// How a scan is dealt, by its columns C and steps (vec: the arrays allow four
+// columns a lane), from device times of the scan / its backward in fp32, us:
+//   four columns a lane or one: 16 x 250,000 x 128 (bf16) 787 / 1620 and 1414 /
+//     1823, C = 38,400 x 200 steps 39 / 60 and 25 / 48;
+//   a wave alone or four along time, four columns a lane: C = 241,280 x 600 steps
+//     321 / 664 and 356 / 716, C = 128,000 x 64 steps 34 / 66 and 22 / 42;
+//   four or eight, one column a lane: C = 40,960 x 400 steps 39 / 91 and 37 / 92,
+//     C = 20,480 x 400 steps 31 / 54 and 25 / 50;
+//   eight, or chunks: C = 20,480 x 400 steps 25 / 50 and 32 / 51, C = 10,240 x
+//     2,000 steps 82 / 152 and 64 / 120, C = 192 x 8,000 steps 296 / 484 and 15 / 18.
+// A wave takes all steps at once where they fit its segment.
 struct Deal {
   int V, W;
   int64_t tiles, chunk, chunks;
@@ -479,18 +490,22 @@ hipError_t launch_scan(ScanArgs a, int g_type, int x_type, hipStream_t st) {
   return by_types(g_type, x_type, [&](auto tg, auto tx) {
     return by_deal(d, [&](auto w, auto v) {
       constexpr int W = w(), V = v(), SEG = V == 4 ? SEG4 : SEG1;
-      const unsigned gx = (unsigned)(W == 1 ? (d.tiles + 3) / 4 : d.tiles);
-      if constexpr (W == 8 && V == 1) {
-        if (d.chunks > 1) {
-          hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1),
-                             dim3(threads(W)), 0, st, a);
-          const hipError_t e = hipGetLastError();
-          if (e != hipSuccess) return e;
+      const dim3 block(threads(W));
+      hipError_t e = hipSuccess;
+      for (a.tile0 = 0; a.tile0 < d.tiles && e == hipSuccess; a.tile0 += LAUNCH) {
+        const int64_t n = d.tiles - a.tile0 < LAUNCH ? d.tiles - a.tile0 : LAUNCH;
+        const unsigned gx = (unsigned)(W == 1 ? (n + 3) / 4 : n);
+        if constexpr (W == 8 && V == 1) {
+          if (d.chunks > 1) {
+            hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+          }
         }
+        hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks), block, 0, st, a);
+        e = hipGetLastError();
       }
-      hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks), dim3(threads(W)), 0,
-                         st, a);
-      return hipGetLastError();
+      return e;
     });
   });
 }
@@ -508,18 +523,22 @@ hipError_t launch_scan_grad(ScanArgs a, int g_type, int x_type, hipStream_t st) 
   return by_types(g_type, x_type, [&](auto tg, auto tx) {
     return by_deal(d, [&](auto w, auto v) {
       constexpr int W = w(), V = v(), SEG = V == 4 ? SEG4 : SEG1;
-      const unsigned gx = (unsigned)(W == 1 ? (d.tiles + 3) / 4 : d.tiles);
-      if constexpr (W == 8 && V == 1) {
-        if (d.chunks > 1) {
-          hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1),
-                             dim3(threads(W)), 0, st, a);
-          const hipError_t e = hipGetLastError();
-          if (e != hipSuccess) return e;
+      const dim3 block(threads(W));
+      hipError_t e = hipSuccess;
+      for (a.tile0 = 0; a.tile0 < d.tiles && e == hipSuccess; a.tile0 += LAUNCH) {
+        const int64_t n = d.tiles - a.tile0 < LAUNCH ? d.tiles - a.tile0 : LAUNCH;
+        const unsigned gx = (unsigned)(W == 1 ? (n + 3) / 4 : n);
+        if constexpr (W == 8 && V == 1) {
+          if (d.chunks > 1) {
+            hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+          }
         }
+        hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks), block, 0, st, a);
+        e = hipGetLastError();
       }
-      hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks),
-                         dim3(threads(W)), 0, st, a);
-      return hipGetLastError();
+      return e;
     });
   });
 }

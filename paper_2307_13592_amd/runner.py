@@ -243,6 +243,7 @@ class GatedMemory:
 
     def __init__(self, rows: int, cols: int, device: str = "cuda", gate=None):
         self.state = torch.zeros((rows, cols), dtype=torch.float32, device=device)
+        self.h0 = torch.zeros_like(self.state)  # the state that the last scan() began with
         self.gate = gate
 
     def step(self, x, g=None, x_scale=None, stream=None):
@@ -258,7 +259,8 @@ class GatedMemory:
         """Every state of a trajectory [steps][rows][cols] that continues from
         `state`, which becomes the last one."""
         h = torch.empty(g.shape, dtype=torch.float32, device=g.device)
-        self.h0 = self.state.clone()
+        none = None if x_scale is None else x_scale[:0]
+        mgn_gated_scan(g[:0], x[:0], None, self.h0, self.state, None, none, None, stream)  # h0 <- state
         mgn_gated_scan(g, x, h, self.state, self.h0, starts, x_scale, None, stream)
         return h
 

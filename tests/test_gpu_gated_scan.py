@@ -283,11 +283,11 @@ def test_arrays_aligned_to_their_type_only(T, rows, cols, typ):
         assert all(torch.allclose(p.float(), q.float(), rtol=tol, atol=tol) for p, q in zip((dg, dx, d0), want))
 
 
-def test_offsets_past_32_bits():
-    """A window of 2^32 bf16 gates: the last steps against float64 from the
-    state before them."""
-    T, rows, cols = 9, 1 << 22, 128
-    print("[scan] 9 x 4194304 x 128 bf16", flush=True)
+@pytest.mark.parametrize("T,rows,cols", [(9, 1 << 22, 128), (2, 600_001, 121)])
+def test_many_columns(T, rows, cols):
+    """Offsets past 2^32 elements, and more columns than one launch takes (four
+    and one a lane): some rows against float64."""
+    print(f"[scan] {T} x {rows} x {cols} bf16", flush=True)
     g = torch.empty(T, rows, cols, dtype=torch.bfloat16, device="cuda").normal_()
     x = torch.empty_like(g).normal_()
     h = torch.empty(T, rows, cols, device="cuda")

@@ -194,3 +194,89 @@ def test_window_from_an_8_bit_history(dtype):
         dw += w
         mag += m
     assert np.all(np.abs(ref.f64(norm.d_weight) - dw) <= mag * 64 * ref.U32 + np.abs(dw) * T * ref.U32)
+
+
+def test_captured_step_carries_its_state():
+    """A rollout's memory step recorded into a HIP graph: every replay moves
+    the state on, as eager steps do."""
+    n, cols = 500, 5
+    gate = torch.randn(n, cols, device="cuda")
+    x = torch.randn(n, cols, device="cuda")
+    a, b = GatedMemory(n, cols, gate=gate), GatedMemory(n, cols, gate=gate)
+    a.step(x)
+    b.step(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        a.step(x)
+    for k in range(4):
+        x.copy_(torch.randn(n, cols, device="cuda"))
+        g.replay()
+        b.step(x)
+        torch.cuda.synchronize()
+        assert torch.equal(a.state, b.state), k
+
+
+def test_calls_from_two_threads():
+    """Two host threads, a stream each, calling at once (a long scan with
+    scratch, and the norm's backward with its partials): everyone's own bits."""
+    import threading
+    T, rows, cols = 4000, 1, 64
+    r = torch.Generator(device="cuda")
+    r.manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=r, device="cuda")
+    sets = [dict(g=rand(T, rows, cols), x=rand(T, rows, cols), t=rand(3000, 128), dy=rand(3000, 128)) for _ in range(2)]
+
+    def run(s, stream):
+        h = torch.empty(T, rows, cols, device="cuda")
+        mgn.mgn_gated_scan(s["g"], s["x"], h=h, stream=stream)
+        dx, dw = torch.empty_like(s["t"]), torch.empty(128, device="cuda")
+        mgn.mgn_rms_norm_grad(s["t"], None, s["dy"], dx, dw, stream=stream)
+        return h, dx, dw
+
+    want = [run(s, None) for s in sets]
+    torch.cuda.synchronize()
+    got, bad = [None, None], []
+
+    def work(k):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for _ in range(20):
+                    got[k] = run(sets[k], st.cuda_stream)
+                    st.synchronize()
+                    if not all(torch.equal(p, q) for p, q in zip(got[k], want[k])):
+                        bad.append(k)
+        except Exception as e:
+            bad.append(e)
+
+    ts = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    [t.start() for t in ts]
+    [t.join() for t in ts]
+    assert not bad, bad
+
+
+def test_bindings_refuse_mismatched_tensors():
+    x = torch.zeros(4, 128, device="cuda")
+    w = torch.ones(128, device="cuda")
+    q, s = torch.zeros(4, 128, dtype=torch.uint8, device="cuda"), torch.ones(4, 1, device="cuda")
+    i = torch.zeros(4, dtype=torch.int32, device="cuda")
+    g = torch.zeros(3, 4, 128, device="cuda")
+    for call in (lambda: mgn.mgn_rms_norm(x, w, x.cpu()), lambda: mgn.mgn_rms_norm(x, w[:64], x),
+                 lambda: mgn.mgn_rms_norm(x, w, x, res=x.bfloat16()), lambda: mgn.mgn_rms_norm(x.t(), None, x.t()),
+                 lambda: mgn.mgn_rms_norm_grad(x, w, x, None), lambda: mgn.mgn_rms_norm_grad(x, w, x[:3], x),
+                 lambda: mgn.mgn_rows_store8(x, q, s, src_rows=i.long()),
+                 lambda: mgn.mgn_rows_store8(x, q, s, src_rows=i, slots=i[:3]),
+                 lambda: mgn.mgn_rows_store8(x, q, torch.ones(4, 2, device="cuda")),
+                 lambda: mgn.mgn_rows_load8(q, s, x[:, :64].contiguous()),
+                 lambda: mgn.mgn_gated_scan(g, g, h_last=x.bfloat16()), lambda: mgn.mgn_gated_scan(g, g[:2], h=g),
+                 lambda: mgn.mgn_gated_scan(g, g, h=torch.empty_like(g), starts=torch.zeros(4, dtype=torch.uint8, device="cuda")),
+                 lambda: LatentCache(4, 128).store(x, first=1)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: mgn.mgn_rms_norm(x, w, q), lambda: mgn.mgn_rms_norm(x, w, x, y_scale=s),
+                 lambda: mgn.mgn_rows_store8(x, q[:3], s[:3]), lambda: mgn.mgn_gated_scan(g, g),
+                 lambda: mgn.mgn_rows_load8(q, s, x.bfloat16(), add=True)):
+        with pytest.raises(mgn.MgnError) as e:
+            call()
+        assert e.value.status == mgn.MGN_E_ARG

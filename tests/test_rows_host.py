@@ -62,7 +62,7 @@ def test_rms_norm_refusals():
     for call in (fwd, bwd):
         for kw in (dict(cols=0), dict(cols=8193), dict(rows=-1), dict(rows=1 << 50)):
             _refused(call(**kw), "sizes")
-        for kw in (dict(eps=0.0), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF)):
+        for kw in (dict(eps=0.0), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(eps=1e-40)):
             _refused(call(**kw), "eps")
         _refused(call(t=E4M3), "type")
         _refused(call(w=HALF), "misaligned")
