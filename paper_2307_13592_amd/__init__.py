@@ -349,10 +349,11 @@ def _shape(t, name: str, dims: int = 2):
 
 def _arr(t, name: str, dtype, shape, dev):
     """Device pointer of an array of this type and shape on device `dev`
-    (None -> NULL).  One comparison per property: these calls are short."""
+    (None -> NULL); _run refuses a device that is none of the GPUs.  One
+    comparison per property: these calls are short."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous() and t.is_cuda:
+    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
         return t.data_ptr()
     _devt(t, dtype, name, shape=shape)  # says what is wrong, but for the device
     raise ValueError(f"{name}: expected a tensor on {dev}, got one on {t.device}")
@@ -369,6 +370,8 @@ def _run(fn: str, dev, stream, *args) -> None:
     without a stream given, on the current one of that device."""
     import torch
     f = getattr(lib(), fn)
+    if dev.type != "cuda":
+        raise ValueError(f"{fn}: expected device tensors, got {dev}")
     if dev.index == torch.cuda.current_device():
         st = f(*args, torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else int(stream))
     else:
