@@ -237,9 +237,9 @@ mgn_status mgn_norm_apply(const float* x, int64_t rows, int32_t cols, const doub
  * block's scale.  The scales written here are the least power of two (at least
  * 2^-126; 1 for a block of zeros) that brings the block's largest finite
  * magnitude to 448 or less, so each value is rounded once, to nearest even, and
- * rows stored, read back and stored again are the same bytes.  An infinity is
- * stored as +-448 times the scale, a NaN as a NaN; neither changes the scale of
- * its neighbours. */
+ * rows stored, read back and stored again stand for the same values.  An infinity
+ * is stored as +-448 times the scale, a NaN as a NaN; neither changes the scale
+ * of its neighbours. */
 #define MGN_ROW_MAX_COLS 8192
 #define MGN_ROWS8_BLOCK 128
 /* Stores rows in 8 bits: slot slots[i] takes row src_rows[i] of src

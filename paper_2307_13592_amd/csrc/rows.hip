@@ -4,7 +4,7 @@
 //
 // All are bound by memory: a row is read once and stays in registers between
 // its sum (or its blocks' largest values) and its result.  Its columns are dealt
-// to TPR threads, 4, 16, 32 or 64 lanes of one wave or a workgroup of 256 or 1024
+// to TPR threads, 4 to 64 lanes of one wave or a workgroup of 256 or 1024
 // (rows8.h, Cols), NV runs of V columns each; a wave takes 64 / TPR rows at a
 // time.  As few threads as hold a row at 16 bytes each: of 1M x 128 bf16 rows the
 // norm takes 79 us (6.5 TB/s) and its backward 135 (5.7), against 104 and 235
@@ -318,6 +318,8 @@ hipError_t by_cols(int cols, RowMode mode, F f) {
   const auto runs = [&](auto m) {
     if constexpr (TYPE == MGN_BF16) {
       const Int<8> v;
+      if (cols <= 32) return f(Int<4>(), Int<1>(), v, m);
+      if (cols <= 64) return f(Int<8>(), Int<1>(), v, m);
       if (cols <= 128) return f(Int<16>(), Int<1>(), v, m);
       if (cols <= 256) return f(Int<32>(), Int<1>(), v, m);
       if (cols <= 512) return f(Int<64>(), Int<1>(), v, m);
@@ -326,6 +328,7 @@ hipError_t by_cols(int cols, RowMode mode, F f) {
       if (cols <= 8192) return f(Int<1024>(), Int<1>(), v, m);
     } else {
       const Int<4> v;
+      if (cols <= 32) return f(Int<8>(), Int<1>(), v, m);
       if (cols <= 64) return f(Int<16>(), Int<1>(), v, m);
       if (cols <= 128) return f(Int<32>(), Int<1>(), v, m);
       if (cols <= 256) return f(Int<64>(), Int<1>(), v, m);

@@ -1,13 +1,13 @@
-// Rows of fp32, bf16 or 8-bit columns, four columns a lane (gfx950 / CDNA4).
+// Rows of fp32, bf16 or 8-bit columns in registers (gfx950 / CDNA4).
 //
 // 8-bit rows: the codes are e4m3 (4 exponent bits, 3 of mantissa, largest
 // finite value 448, no infinity), one byte a column, and each block of 128
 // columns of a row has one fp32 scale; a code stands for its e4m3 value times
 // the scale.  The scale is the least power of two that brings the block's
 // largest finite magnitude to 448 or less: dividing by it is exact, so a value
-// is rounded once (to nearest, ties to even), storing rows that were read back
-// gives the same bytes, and since e4m3 is a floating format a power of two
-// costs no mantissa bit against amax / 448, only up to one bit of range below.
+// is rounded once (to nearest, ties to even), rows that were read back and stored
+// again stand for the same values, and since e4m3 is a floating format a power of
+// two costs no mantissa bit against amax / 448, only up to one bit of range below.
 #pragma once
 #include <type_traits>
 

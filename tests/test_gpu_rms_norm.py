@@ -16,7 +16,7 @@ from paper_2307_13592_amd.runner import LatentCache, RmsNorm
 
 pytestmark = pytest.mark.gpu
 EPS = 1e-6
-SHAPES = [(1, 1), (3, 5), (33, 64), (1885, 77), (130, 128), (65, 129), (7, 200), (1001, 256), (5, 257), (6, 1000),
+SHAPES = [(1, 1), (3, 5), (33, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (130, 128), (65, 129), (7, 200), (1001, 256), (5, 257), (6, 1000),
           (3, 1024), (4, 1025), (2, 8192), (3, 8191)]
 
 

@@ -31,7 +31,7 @@ def _same(q, scale, x):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("n,cols", [(1, 1), (3, 5), (7, 64), (1885, 77), (33, 127), (130, 128), (65, 129), (9, 200),
+@pytest.mark.parametrize("n,cols", [(1, 1), (3, 5), (7, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (33, 127), (130, 128), (65, 129), (9, 200),
                                     (1000, 256), (5, 257), (6, 1000), (3, 1024), (4, 1025), (2, 8192), (2, 8191)])
 def test_store_and_load(n, cols, dtype):
     print(f"[rows8] {n} x {cols} {dtype}", flush=True)
@@ -44,7 +44,7 @@ def test_store_and_load(n, cols, dtype):
         mgn.mgn_rows_load8(q, s, y)
         want = torch.as_tensor(ref.values8(q, s)).to(out)
         assert torch.equal(y.cpu(), want)
-    # storing what was read back gives the same bytes
+    # what was read back and stored again stands for the same values
     y = torch.empty(n, cols, device="cuda")
     mgn.mgn_rows_load8(q, s, y)
     q2, s2 = _slots(n, cols)
