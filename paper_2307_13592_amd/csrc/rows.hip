@@ -4,7 +4,7 @@
 //
 // All are bound by memory: a row is read once and stays in registers between
 // its sum (or its blocks' largest values) and its result.  Its columns are dealt
-// to TPR threads, 4 to 64 lanes of one wave or a workgroup of 256 or 1024
+// to TPR threads, 2 to 64 lanes of one wave or a workgroup of 256 or 1024
 // (rows8.h, Cols), NV runs of V columns each; a wave takes 64 / TPR rows at a
 // time.  As few threads as hold a row at 16 bytes each: of 1M x 128 bf16 rows the
 // norm takes 79 us (6.5 TB/s) and its backward 135 (5.7), against 104 and 235
@@ -314,10 +314,11 @@ using Int = std::integral_constant<int, N>;
 // constants: 16 bytes a run, as few threads a row as hold it.
 template <int TYPE, class F>
 hipError_t by_cols(int cols, RowMode mode, F f) {
-  if (cols <= 16) return f(Int<4>(), Int<1>(), Int<4>(), Int<APART>());
+  if (mode == APART) return f(Int<4>(), Int<1>(), Int<4>(), Int<APART>());
   const auto runs = [&](auto m) {
     if constexpr (TYPE == MGN_BF16) {
       const Int<8> v;
+      if (cols <= 16) return f(Int<2>(), Int<1>(), v, m);
       if (cols <= 32) return f(Int<4>(), Int<1>(), v, m);
       if (cols <= 64) return f(Int<8>(), Int<1>(), v, m);
       if (cols <= 128) return f(Int<16>(), Int<1>(), v, m);
@@ -328,6 +329,8 @@ hipError_t by_cols(int cols, RowMode mode, F f) {
       if (cols <= 8192) return f(Int<1024>(), Int<1>(), v, m);
     } else {
       const Int<4> v;
+      if (cols <= 8) return f(Int<2>(), Int<1>(), v, m);
+      if (cols <= 16) return f(Int<4>(), Int<1>(), v, m);
       if (cols <= 32) return f(Int<8>(), Int<1>(), v, m);
       if (cols <= 64) return f(Int<16>(), Int<1>(), v, m);
       if (cols <= 128) return f(Int<32>(), Int<1>(), v, m);
@@ -349,12 +352,14 @@ hipError_t by_rows(int type, int cols, RowMode mode, F f) {
   return by_cols<MGN_FP32>(cols, mode, [&](auto t, auto n, auto v, auto m) { return f(Int<MGN_FP32>(), t, n, v, m); });
 }
 
-// How a kernel that moves `bytes` reads its rows: as whole runs where they are
-// that, on 16-byte boundaries, and past the caches where it moves more than the
-// last-level cache holds (256 MB).  Above: 2M x 128 bf16 rows with a residual
-// into 8-bit rows 324 us through the caches, 287 past them.  Below, where the
-// rows may still be cached: 200k of 400k x 256 bf16 rows gathered 28.4 and 34.7.
-RowMode row_mode(int64_t bytes, int type, int cols, std::initializer_list<const void*> arrays) {
+// How a kernel that moves `bytes` reads its arrays of `rows` rows: as whole runs
+// where they are that, on 16-byte boundaries, and past the caches where it moves
+// more than the last-level cache holds (256 MB).  Above: 2M x 128 bf16 rows with a
+// residual into 8-bit rows 324 us through the caches, 287 past them.  Below,
+// where the rows may still be cached: 200k of 400k x 256 bf16 rows gathered 28.4
+// and 34.7.
+RowMode row_mode(int64_t bytes, int type, int64_t rows, int cols, std::initializer_list<const void*> arrays) {
+  if (cols <= 16 && rows * cols < 16) return APART;
   bool even = cols % (type == MGN_FP32 ? 4 : 8) == 0;
   for (const void* p : arrays) even = even && (uintptr_t)p % 16 == 0;
   return !even ? RUNS : bytes > ((int64_t)256 << 20) ? STREAM : WHOLE;
@@ -364,7 +369,7 @@ int64_t type_bytes(int type) { return type == MGN_FP32 ? 4 : type == MGN_BF16 ? 
 }  // namespace
 
 hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st) {
-  const RowMode mode = row_mode(a.n * a.cols * (type_bytes(type) + 1), type, a.cols, {a.x});
+  const RowMode mode = row_mode(a.n * a.cols * (type_bytes(type) + 1), type, a.n_rows, a.cols, {a.x});
   return by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
     hipLaunchKernelGGL((store8_kernel<tpr(), nv(), v(), y(), ti()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, STORE_GRID)),
                        dim3(Rows<tpr()>::NT), 0, st, a);
@@ -373,7 +378,7 @@ hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st) {
 }
 
 hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st) {
-  const RowMode mode = row_mode(0, type, a.cols, {a.add ? a.out : nullptr});
+  const RowMode mode = row_mode(0, type, a.n_rows, a.cols, {a.add ? a.out : nullptr});
   return by_rows(type, a.cols, mode, [&](auto to, auto tpr, auto nv, auto v, auto y) {
     hipLaunchKernelGGL((load8_kernel<tpr(), nv(), v(), y(), to()>), dim3(row_grid(a.n, Rows<tpr()>::RPB, LOAD_GRID)),
                        dim3(Rows<tpr()>::NT), 0, st, a);
@@ -383,7 +388,7 @@ hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st) {
 
 hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t st) {
   const int64_t per = type_bytes(type) * (1 + (a.res != nullptr) + (a.total != nullptr)) + type_bytes(y_type);
-  const RowMode mode = row_mode(a.rows * a.cols * per, type, a.cols, {a.x, a.res});
+  const RowMode mode = row_mode(a.rows * a.cols * per, type, a.rows, a.cols, {a.x, a.res});
   return by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
     const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, NORM_GRID));
     if (y_type == MGN_E4M3)
@@ -399,7 +404,8 @@ hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t s
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st) {
   int grid = 0;
   if (a.rows > 0) {
-      const RowMode mode = row_mode(a.rows * a.cols * type_bytes(type) * (3 + (a.res != nullptr)), type, a.cols,
+      const RowMode mode = row_mode(a.rows * a.cols * type_bytes(type) * (3 + (a.res != nullptr)), type, a.rows,
+                                  a.cols,
                                   {a.x, a.dy, a.res});
     const hipError_t e = by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
       grid = row_grid(a.rows, Rows<tpr()>::RPB, MGN_RMS_WORK_PER_COL);

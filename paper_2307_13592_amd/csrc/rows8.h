@@ -31,9 +31,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // Mostly a thread holds runs of V neighbouring columns, read 16 bytes (fp32
 // V = 4, bf16 V = 8) at once; rows of any width and alignment, since the card's
 // vector memory accesses need none; the columns past the last whole run are
-// read in pieces of 4, 2 and 1.  Otherwise (at most 16 columns) the V = 4
-// columns of a thread lie TPR apart, neighbouring lanes reading neighbouring
-// columns.  Either way the 128 columns of an 8-bit block lie with 128 / V
+// written in pieces of 4, 2 and 1.  Otherwise (arrays of a few elements) the V =
+// 4 columns of a thread lie TPR apart, and are read one by one.  Either way the 128 columns of an 8-bit block lie with 128 / V
 // neighbouring lanes.
 enum RowMode {
   APART,   // columns TPR apart
@@ -158,7 +157,7 @@ __device__ __forceinline__ void load_values(const float* w, int c, int cols, flo
 // same for the whole wave, o the lane's; `left` elements of the array lie from
 // p + b on.  A run of 16 bytes that passes its row's end is read whole, into the
 // next row, and cut; one that would pass the array's end is read from `left`
-// back and shifted.  (A row of runs holds more than 16 elements.)
+// back and shifted.  (An array of runs holds 16 elements or more.)
 template <int TYPE, class D, int V>
 __device__ __forceinline__ void load_cols(const void* p, int64_t b, uint32_t o, int c, int cols, int64_t left,
                                           float (&v)[V]) {
@@ -173,7 +172,8 @@ __device__ __forceinline__ void load_cols(const void* p, int64_t b, uint32_t o, 
       get<V, E, D::PAST>(r + (o + c), v);
     } else {
       const int64_t most = left - V;
-      const uint32_t e = o + c, at = most < (int64_t)e ? (uint32_t)most : e, back = e - at;
+      const int32_t e = (int32_t)(o + c), at = most < (int64_t)e ? (int32_t)most : e;
+      const uint32_t back = e - at;
       uint64_t w[2];
       __builtin_memcpy(w, r + at, 16);
       if (back) {

@@ -16,7 +16,7 @@ from paper_2307_13592_amd.runner import LatentCache, RmsNorm
 
 pytestmark = pytest.mark.gpu
 EPS = 1e-6
-SHAPES = [(1, 1), (3, 5), (33, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (130, 128), (65, 129), (7, 200), (1001, 256), (5, 257), (6, 1000),
+SHAPES = [(1, 1), (3, 5), (2, 7), (1, 16), (3, 6), (900, 5), (333, 11), (64, 8), (40, 16), (9, 9), (33, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (130, 128), (65, 129), (7, 200), (1001, 256), (5, 257), (6, 1000),
           (3, 1024), (4, 1025), (2, 8192), (3, 8191)]
 
 
@@ -76,9 +76,9 @@ def test_grad(n, cols, dtype):
                                                        ref.f64(dy), ref.f64(ds) if with_ds else None, EPS)
             _near(dx, dx64, slack + np.abs(dx64) * (ref.half(dtype) + ref.U32) + 1e-37)
             # a column's sum: u within 32, one product, at most n / 1024 + 1 rows
-            # in one thread (of 1024 workgroups a row each), at most 64 row groups
+            # in one thread (of 1024 workgroups a row each), at most 128 row groups
             # of a workgroup, then fp64
-            bound = mag * (36 + n / 1024 + 1 + 64) * ref.U32 + np.abs(dw64) * ref.U32 + 1e-37
+            bound = mag * (36 + n / 1024 + 1 + 128) * ref.U32 + np.abs(dw64) * ref.U32 + 1e-37
             _near(dw, dw64, bound)
             dw2 = dw.clone()
             mgn.mgn_rms_norm_grad(t, weight, dy, dx, dw2, d_total=ds if with_ds else None, accumulate=True, eps=EPS)
@@ -170,7 +170,7 @@ def test_in_place_and_unaligned(cols, dtype):
         d2 = at(dx * 0, o)
         mgn.mgn_rms_norm_grad(at(t, o), wo, at(dy, 0), d2, dw2, d_total=at(res, 2), eps=EPS)
         _near(d2, dx64, slack + np.abs(dx64) * (h + ref.U32) + 1e-37)
-        _near(dw2, dw64, mag * (36 + n / 1024 + 1 + 64) * ref.U32 + np.abs(dw64) * ref.U32 + 1e-37)
+        _near(dw2, dw64, mag * (36 + n / 1024 + 1 + 128) * ref.U32 + np.abs(dw64) * ref.U32 + 1e-37)
 
 
 def test_no_rows():

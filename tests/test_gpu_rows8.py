@@ -31,7 +31,7 @@ def _same(q, scale, x):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("n,cols", [(1, 1), (3, 5), (7, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (33, 127), (130, 128), (65, 129), (9, 200),
+@pytest.mark.parametrize("n,cols", [(1, 1), (3, 5), (2, 7), (1, 16), (3, 6), (900, 5), (333, 11), (64, 8), (40, 16), (9, 9), (7, 64), (501, 17), (77, 21), (64, 32), (33, 48), (1885, 77), (33, 127), (130, 128), (65, 129), (9, 200),
                                     (1000, 256), (5, 257), (6, 1000), (3, 1024), (4, 1025), (2, 8192), (2, 8191)])
 def test_store_and_load(n, cols, dtype):
     print(f"[rows8] {n} x {cols} {dtype}", flush=True)
