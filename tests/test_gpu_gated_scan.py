@@ -99,6 +99,11 @@ def test_scan_and_grad(T, rows, cols, typ, x8):
 
 
 @pytest.mark.parametrize("typ,x8", [("fp32", False), ("bf16", True)])
+def test_chunks_of_several_tiles(typ, x8):
+    _check(_case(2050, 50, 128, typ, x8, starts=0.01, seed=9))
+
+
+@pytest.mark.parametrize("typ,x8", [("fp32", False), ("bf16", True)])
 @pytest.mark.parametrize("T,rows,cols", [(1, 5, 64), (20, 103, 64), (33, 1, 77), (600, 2, 128), (2050, 1, 40)])
 @pytest.mark.parametrize("starts", [0.02, 0.3, 1.1])
 def test_trajectories_in_one_window(T, rows, cols, typ, x8, starts):
@@ -215,7 +220,7 @@ def test_grad_against_differences():
         assert np.allclose(ref.f64(got[k]), num, rtol=1e-4, atol=1e-4 * np.abs(num).max()), k
 
 
-@pytest.mark.parametrize("T,rows,cols", [(1, 200, 128), (12, 40, 64), (3000, 1, 64)])
+@pytest.mark.parametrize("T,rows,cols", [(1, 200, 128), (12, 40, 64), (100, 9, 64), (40, 900, 128), (3000, 1, 64)])
 def test_state_in_place_and_windows(T, rows, cols):
     """h_last on h0, dh0 on dh_last, and a trajectory cut into windows that
     hand the state (backward: its gradient) on."""
@@ -224,6 +229,9 @@ def test_state_in_place_and_windows(T, rows, cols):
     s = c["h0"].clone()
     mgn.mgn_gated_scan(c["g"], c["x"], h_last=s, h0=s)
     assert torch.equal(s, last)
+    s, h2 = c["h0"].clone(), torch.empty_like(h)
+    mgn.mgn_gated_scan(c["g"], c["x"], h=h2, h_last=s, h0=s)
+    assert torch.equal(s, last) and torch.equal(h2, h)
     dg, dx, dh0 = _backward(c, h)
     d = c["dh_last"].clone()
     mgn.mgn_gated_scan_grad(c["g"], c["x"], h, torch.empty_like(dg), torch.empty_like(dx), dh=c["dh"], dh_last=d, dh0=d,

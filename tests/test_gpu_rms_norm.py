@@ -132,7 +132,7 @@ def test_rows_that_hold_nan_or_infinity_stay_alone(cols):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("cols", [128, 77, 2000])
+@pytest.mark.parametrize("cols", [128, 77, 2000, 5, 1501])
 def test_in_place_and_unaligned(cols, dtype):
     """Results on the arrays they may stand on (the same bits), and arrays
     aligned to their type only."""
@@ -162,14 +162,19 @@ def test_in_place_and_unaligned(cols, dtype):
     y64, t64 = ref.rms_norm(ref.f64(x), ref.f64(res), ref.f64(w), EPS)
     dx64, dw64, slack, mag = ref.rms_norm_grad(ref.f64(t), ref.f64(w), ref.f64(dy), ref.f64(res), EPS)
     h = ref.half(dtype)
+    def kept(v, o):  # what lies around an array of at()
+        all_ = v.new_empty(0).set_(v.untyped_storage(), 0, (v.numel() + 8,))
+        return bool((all_[:o] == 5).all()) and bool((all_[o + v.numel():] == 5).all())
+
     for o in (1, 2, 3):
         y2, t2, wo = at(y * 0, o), at(t * 0, (o + 1) % 4), at(w, o)
         mgn.mgn_rms_norm(at(x, o), wo, y2, res=at(res, 0), total=t2, eps=EPS)
         _near(y2, y64, np.abs(y64) * (32 * ref.U32 + h) + 1e-37)
-        assert torch.equal(t2, t)
+        assert torch.equal(t2, t) and kept(y2, o) and kept(t2, (o + 1) % 4)
         d2 = at(dx * 0, o)
         mgn.mgn_rms_norm_grad(at(t, o), wo, at(dy, 0), d2, dw2, d_total=at(res, 2), eps=EPS)
         _near(d2, dx64, slack + np.abs(dx64) * (h + ref.U32) + 1e-37)
+        assert kept(d2, o)
         _near(dw2, dw64, mag * (36 + n / 1024 + 1 + 128) * ref.U32 + np.abs(dw64) * ref.U32 + 1e-37)
 
 
@@ -184,22 +189,28 @@ def test_no_rows():
     assert bool((dw == 0).all())
 
 
-def test_more_rows_than_a_grid():
-    """3M rows of 64: rows beyond the launched workgroups' first share."""
-    x = torch.randn(3_000_001, 64, device="cuda")
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,cols", [(3_000_001, 64), (700_001, 77), (40_001, 1100), (33_001, 4100), (33_001, 4099)])
+def test_more_rows_than_a_grid(n, cols, dtype):
+    """Rows beyond the launched workgroups' first turn, and more bytes than the
+    caches hold; rows of one wave's lanes, of 256 and of 1024 threads."""
+    print(f"[rms] {n} x {cols} {dtype}", flush=True)
+    h = ref.half(dtype) + 2 * ref.U32
+    x = torch.randn(n, cols, device="cuda").to(dtype)
     y = torch.empty_like(x)
     mgn.mgn_rms_norm(x, None, y, eps=EPS)
-    want = x.double() * torch.rsqrt((x.double() ** 2).mean(1, keepdim=True) + EPS)
-    assert float(((y.double() - want).abs() - 34 * ref.U32 * want.abs()).max()) <= 1e-37
-    nz = RmsNorm(64)
-    dx = nz.grad(x, y)
-    u = want
-    m = (u * y.double()).mean(1, keepdim=True)
     inv = torch.rsqrt((x.double() ** 2).mean(1, keepdim=True) + EPS)
-    slack = (y.abs().double() + u.abs() * (u * y.double()).abs().mean(1, keepdim=True)) * inv * 92 * ref.U32
-    assert float(((dx.double() - (y.double() - u * m) * inv).abs() - slack).max()) <= 1e-37
-    dw = (y.double() * u).sum(0)
-    assert bool(((nz.d_weight.double() - dw).abs() <= dw.abs() * (53 + 3_000_001 / 1024) * ref.U32).all())
+    u = x.double() * inv
+    assert float(((y.double() - u).abs() - (32 * ref.U32 + h) * u.abs()).max()) <= 1e-37
+    nz = RmsNorm(cols)
+    dx = nz.grad(x, y)
+    g = y.double()
+    m = (u * g).mean(1, keepdim=True)
+    want = (g - u * m) * inv
+    slack = (g.abs() + u.abs() * (u * g).abs().mean(1, keepdim=True)) * inv * 92 * ref.U32
+    assert float(((dx.double() - want).abs() - slack - h * want.abs()).max()) <= 1e-37
+    dw = (g * u).sum(0)  # (all terms positive)
+    assert bool(((nz.d_weight.double() - dw).abs() <= dw.abs() * (36 + n / 1024 + 1 + 128 + 1) * ref.U32).all())
 
 
 def test_streams_and_captured_replays():

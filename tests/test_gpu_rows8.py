@@ -105,7 +105,7 @@ def test_values_where_it_can_go_wrong(cols):
     _same(q, s, x)
 
 
-@pytest.mark.parametrize("cols", [5, 64, 128, 256])
+@pytest.mark.parametrize("cols", [5, 64, 77, 128, 256, 1030])
 def test_index_lists(cols):
     """Gathered and scattered rows; pairs out of range are skipped and slots
     and rows that no pair names keep what they held."""
@@ -172,6 +172,25 @@ def test_arrays_aligned_to_their_type_only(n, cols, dtype):
         mgn.mgn_rows_load8(q, s, y)
         assert torch.equal(y, y0)
         assert bool((wide[:ox] == 9).all()) and bool((wide[ox + n * cols:] == 9).all())
+
+
+@pytest.mark.parametrize("n,cols,dtype", [(1_000_003, 128, torch.float32), (1_500_001, 256, torch.bfloat16),
+                                          (1_000_003, 77, torch.float32)])
+def test_more_than_the_caches_hold(n, cols, dtype):
+    print(f"[rows8] {n} x {cols} {dtype}", flush=True)
+    x = (torch.randn(n, cols, device="cuda") * torch.exp(torch.randn(n, 1, device="cuda"))).to(dtype)
+    q, s = _slots(n, cols)
+    mgn.mgn_rows_store8(x, q, s)
+    y = torch.empty_like(x)
+    mgn.mgn_rows_load8(q, s, y)
+    for b in range(ref.blocks(cols)):
+        blk = x[:, b * 128:(b + 1) * 128].double()
+        # (on the host: powers of two are exact there)
+        m, e = np.frexp(blk.abs().amax(1, keepdim=True).cpu().numpy())
+        p = torch.as_tensor(np.ldexp(1.0, e - 9 + (m > 0.875))).cuda()
+        assert torch.equal(s[:, b:b + 1].double(), p)
+        v = (blk / p).float().to(torch.float8_e4m3fn).double() * p
+        assert torch.equal(y[:, b * 128:(b + 1) * 128].double(), v)
 
 
 def test_offsets_past_32_bits():
