@@ -347,16 +347,16 @@ def _shape(t, name: str, dims: int = 2):
     return t.shape
 
 
-def _arr(t, name: str, dtype, shape, dev):
-    """Device pointer of an array of this type and shape on device `dev`
-    (None -> NULL); _run refuses a device that is none of the GPUs.  One
-    comparison per property: these calls are short."""
+def _arr(t, name: str, dtype, shape, dev: int):
+    """Device pointer of an array of this type and shape on GPU `dev` (None ->
+    NULL); _run refuses a dev that is none.  One comparison per property: these
+    calls are short."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
     _devt(t, dtype, name, shape=shape)  # says what is wrong, but for the device
-    raise ValueError(f"{name}: expected a tensor on {dev}, got one on {t.device}")
+    raise ValueError(f"{name}: expected a tensor on GPU {dev}, got one on {t.device}")
 
 
 def _need(p, name: str):
@@ -365,15 +365,15 @@ def _need(p, name: str):
     return p
 
 
-def _run(fn: str, dev, stream, *args) -> None:
-    """Calls the entry point fn(*args, stream) on the device of its arrays;
+def _run(fn: str, dev: int, stream, *args) -> None:
+    """Calls the entry point fn(*args, stream) on GPU `dev`, its arrays';
     without a stream given, on the current one of that device."""
     import torch
+    if dev < 0:
+        raise ValueError(f"{fn}: expected device tensors")
     f = getattr(lib(), fn)
-    if dev.type != "cuda":
-        raise ValueError(f"{fn}: expected device tensors, got {dev}")
-    if dev.index == torch.cuda.current_device():
-        st = f(*args, torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else int(stream))
+    if dev == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream))
     else:
         with torch.cuda.device(dev):
             st = f(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream))
@@ -381,12 +381,13 @@ def _run(fn: str, dev, stream, *args) -> None:
         _check(st)
 
 
-def _scratch(nbytes: int, device, stream):
+def _scratch(nbytes: int, dev: int, stream):
     """Device scratch for one call on `stream`: from torch's allocator, on that
     stream, so that it is not handed out again before the call has run (and
     belongs to a HIP graph that records the call)."""
     import torch
-    if stream is None:
+    device = torch.device("cuda", dev) if dev >= 0 else None
+    if stream is None or device is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -407,7 +408,7 @@ def mgn_rows_store8(src, q, scale, src_rows=None, slots=None, stream=None) -> No
     either, every row of src is stored."""
     import torch
     n_src, cols = _shape(src, "src")
-    n_slots, dev = _shape(q, "q")[0], src.device
+    n_slots, dev = _shape(q, "q")[0], src.get_device()
     rows, at, n = _lists(src_rows, slots, n_src, dev)
     _run("mgn_rows_store8", dev, stream, _need(_arr(src, "src", src.dtype, (n_src, cols), dev), "src"),
          _type(src, "src"), n_src, cols, rows, at, n, _arr(q, "q", torch.uint8, (n_slots, cols), dev),
@@ -421,7 +422,7 @@ def mgn_rows_load8(q, scale, dst, slots=None, dst_rows=None, add: bool = False, 
     slot is read."""
     import torch
     n_slots, cols = _shape(q, "q")
-    n_dst, dev = _shape(dst, "dst")[0], q.device
+    n_dst, dev = _shape(dst, "dst")[0], q.get_device()
     rows, at, n = _lists(dst_rows, slots, n_slots, dev)
     _run("mgn_rows_load8", dev, stream, _need(_arr(q, "q", torch.uint8, (n_slots, cols), dev), "q"),
          _need(_arr(scale, "scale", torch.float32, (n_slots, rows8_blocks(cols)), dev), "scale"), n_slots, cols, at,
@@ -435,7 +436,7 @@ def mgn_rms_norm(x, weight, y, res=None, total=None, y_scale=None, eps: float = 
     weight: float32 [cols] or None."""
     import torch
     shape = rows, cols = _shape(x, "x")
-    dev, dt = x.device, x.dtype
+    dev, dt = x.get_device(), x.dtype
     yt = _type(y, "y", e4m3=True)
     _run("mgn_rms_norm", dev, stream, _arr(x, "x", dt, shape, dev), _arr(res, "res", dt, shape, dev), _type(x, "x"),
          rows, cols, _arr(weight, "weight", torch.float32, (cols,), dev), eps, _arr(total, "total", dt, shape, dev),
@@ -451,12 +452,12 @@ def mgn_rms_norm_grad(total, weight, dy, dx, dweight=None, d_total=None, accumul
     scratch of MGN_RMS_WORK_PER_COL * cols for dweight (None: allocated)."""
     import torch
     shape = rows, cols = _shape(total, "total")
-    dev, dt = total.device, total.dtype
+    dev, dt = total.get_device(), total.dtype
     pt = _arr(total, "total", dt, shape, dev)
     if work is not None:
         pw = _devt(work, torch.float32, "work", min_numel=MGN_RMS_WORK_PER_COL * cols)
-        if work.device != dev:
-            raise ValueError(f"work: expected a tensor on {dev}, got one on {work.device}")
+        if work.get_device() != dev:
+            raise ValueError(f"work: expected a tensor on GPU {dev}, got one on {work.device}")
     elif dweight is not None:
         work = _scratch(4 * MGN_RMS_WORK_PER_COL * cols, dev, stream)
         pw = work.data_ptr()
@@ -480,7 +481,7 @@ def _scan_args(g, x, x_scale, starts, h0, work, stream):
     """Marshalled arguments the recurrence and its backward share."""
     import torch
     shape = T, rows, cols = _shape(g, "g", 3)
-    dev = g.device
+    dev = g.get_device()
     xt = _type(x, "x", e4m3=True)
     if xt != MGN_E4M3 and x.dtype is not g.dtype:
         raise ValueError(f"x: expected {g.dtype} (as g) or uint8 codes, got {x.dtype}")
@@ -494,8 +495,8 @@ def _scan_args(g, x, x_scale, starts, h0, work, stream):
             work = _scratch(need, dev, stream)
         return shape, dev, head, (work.data_ptr() if need else None, need), work
     pw = _dev(work)
-    if work.device != dev:
-        raise ValueError(f"work: expected a tensor on {dev}, got one on {work.device}")
+    if work.get_device() != dev:
+        raise ValueError(f"work: expected a tensor on GPU {dev}, got one on {work.device}")
     return shape, dev, head, (pw, work.numel() * work.element_size()), work
 
 
