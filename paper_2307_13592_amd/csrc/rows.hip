@@ -192,8 +192,10 @@ __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
 
 // Backward of one row, u = t inv (the normalised row):
 //   dt = (w dy - u mean(u w dy)) inv + d_total;  dw += dy u.
+// (Where w dy lies along t, as in a row of one column, the difference cancels to a
+// share eps inv^2 of its terms, and carries their rounding.)
 // Each thread sums dw of its columns over its rows in fp32; the workgroup's
-// row groups are added in order and leave one partial per column, of at most
+// row groups are added in order, in fp64, and leave one partial per column, of at most
 // MGN_RMS_WORK_PER_COL workgroups (1M x 128 fp32 rows with d_total 360 us, 5.7
 // TB/s; with twice as many workgroups 417).  Unaligned rows (100,003 x 77 bf16)
 // take 15 us, 3.1 TB/s: their stores share lines, so that 1.5 times the bytes
@@ -266,9 +268,9 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
       for (int k = 0; k < V; ++k) part[grp * W + D::first(j, q.t) + D::STRIDE * k] = dw[j][k];
     __syncthreads();
     for (int c = threadIdx.x; c < a.cols; c += NT) {
-      float total = part[c];
+      double total = part[c];
       for (int e = 1; e < GROUPS; ++e) total += part[e * W + c];
-      dst[c] = total;
+      dst[c] = (float)total;
     }
   }
 }
@@ -297,11 +299,13 @@ __global__ __launch_bounds__(DW_NT) void rms_dw_kernel(const float* __restrict__
 // Rows at a time are dealt to at most this many workgroups, which then go
 // through them in turn: each reads the weights once (1M x 128 fp32 rows with a
 // residual 404 us with 8,192, 354 with 32,768, 336 with one turn each; 2M x 128
-// bf16 into 8-bit rows 287, 289 and 315).  Storing gathered rows prefers few
-// (200k x 256 bf16 28.7 us with 8,192, 30.3 with 32,768); reading 8-bit rows back
-// needs no turns (2M x 128 to fp32 224 us with 32,768 workgroups, 178 - 206 with
-// as many as there are rows to deal).
-constexpr int64_t NORM_GRID = 32768, STORE_GRID = 8192, LOAD_GRID = 1 << 20;
+// bf16 into 8-bit rows 287, 289 and 315).  Rows that are no whole runs, whose
+// weights cost more, prefer 8,192 (500k x 77 bf16 45 us, 61 with 32,768; 300k x
+// 300 bf16 78 and 89; 500k x 77 fp32 with a residual 131 and 129).  Storing
+// gathered rows prefers few (200k x 256 bf16 28.7 us with 8,192, 30.3 with
+// 32,768); reading 8-bit rows back needs no turns (2M x 128 to fp32 224 us with
+// 32,768 workgroups, 178 - 206 with as many as there are rows to deal).
+constexpr int64_t NORM_GRID = 32768, NORM_GRID_RUNS = 8192, STORE_GRID = 8192, LOAD_GRID = 1 << 20;
 int row_grid(int64_t rows, int rpb, int64_t most) {
   const int64_t b = (rows + rpb - 1) / rpb;
   return (int)(b < most ? b : most);
@@ -390,7 +394,7 @@ hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t s
   const int64_t per = type_bytes(type) * (1 + (a.res != nullptr) + (a.total != nullptr)) + type_bytes(y_type);
   const RowMode mode = row_mode(a.rows * a.cols * per, type, a.rows, a.cols, {a.x, a.res});
   return by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
-    const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, NORM_GRID));
+    const dim3 grid(row_grid(a.rows, Rows<tpr()>::RPB, mode == RUNS ? NORM_GRID_RUNS : NORM_GRID));
     if (y_type == MGN_E4M3)
       hipLaunchKernelGGL((rms_norm_kernel<tpr(), nv(), v(), y(), ti(), MGN_E4M3>), grid, dim3(Rows<tpr()>::NT), 0, st, a);
     else if (y_type == MGN_BF16)
