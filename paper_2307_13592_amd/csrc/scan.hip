@@ -23,8 +23,7 @@
 // 1,885 x 128 fp32 backward 660 us (5.3; 943 waves).  With few by the launches
 // and a load's latency in each of them: 8,192 steps of 192 columns 15 us, backward
 // 18.  Loading a wave's next segment ahead of the join was slower (registers:
-// 400 steps of 10,240 columns backward 26 -> 36 us).  Accesses of four columns a
-// lane bypass the caches (16 x 250,000 x 128 793 -> 751 us, backward 1624 -> 1551).
+// 400 steps of 10,240 columns backward 26 -> 36 us).
 #include "kernels.h"
 #include "rows8.h"
 
@@ -48,13 +47,19 @@ __device__ __forceinline__ float term(float weight, float v) { return weight == 
 __device__ __forceinline__ float step(float p, float y, float q) { return p == 0.f ? q : fmaf(p, y, q); }
 
 // V neighbouring elements from element b + o on: b is the same for the whole
-// wave (an address in scalar registers), o the lane's 32-bit offset.
-template <int T, int V>
+// wave (an address in scalar registers), o the lane's 32-bit offset.  PAST: past
+// the caches.
+template <bool PAST, class U>
+__device__ __forceinline__ U read(const void* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load((const U*)p);
+  else return *(const U*)p;
+}
+template <int T, int V, bool PAST = false>
 __device__ __forceinline__ void loadv(const void* p, int64_t b, uint32_t o, float (&v)[V]) {
   if constexpr (T == MGN_BF16) {
     const uint16_t* r = (const uint16_t*)p + b;
     if constexpr (V == 4) {
-      const uint64_t w = __builtin_nontemporal_load(reinterpret_cast<const uint64_t*>(r + o));
+      const uint64_t w = read<PAST, uint64_t>(r + o);
       const uint2 u{(uint32_t)w, (uint32_t)(w >> 32)};
       v[0] = __uint_as_float(u.x << 16);
       v[1] = __uint_as_float(u.x & 0xffff0000u);
@@ -66,7 +71,7 @@ __device__ __forceinline__ void loadv(const void* p, int64_t b, uint32_t o, floa
   } else {
     const float* r = (const float*)p + b;
     if constexpr (V == 4) {
-      const floatx4 u = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(r + o));
+      const floatx4 u = read<PAST, floatx4>(r + o);
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = u[k];
     } else {
@@ -91,7 +96,7 @@ __device__ __forceinline__ void storev(void* p, int64_t b, uint32_t o, const flo
 }
 
 // Where a lane's columns lie (i + o, i the same for its wave), and its view of x.
-template <int V, int TX>
+template <int V, int TX, bool PAST>
 struct Lane {
   int64_t i, C, s0, scn;  // 8-bit x: scale of column i, scales of a step
   uint32_t o, so;
@@ -116,13 +121,13 @@ struct Lane {
       const float* s = a.x_scale + (t * scn + s0);
       float u[4];
       uint32_t codes;
-      if constexpr (V == 4) codes = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(q + o));
+      if constexpr (V == 4) codes = read<PAST, uint32_t>(q + o);
       else codes = q[o];
       values8(codes, s[so], u);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = u[k];
     } else {
-      loadv<TX, V>(a.x, t * C + i, o, v);
+      loadv<TX, V, PAST>(a.x, t * C + i, o, v);
     }
   }
 };
@@ -196,11 +201,11 @@ constexpr int threads(int W) { return W == 1 ? 256 : 64 * W; }
 // FIRST: the first launch of a chunked scan, (p, q) of the chunk blockIdx.y
 // into entry blockIdx.y + 1 (and, with the first chunk, the state that enters
 // the scan into entry 0).
-template <int W, int V, int SEG, int TG, int TX, bool FIRST>
+template <int W, int V, int SEG, int TG, int TX, bool FIRST, bool PAST>
 __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
   __shared__ Joint<W, W == 1 ? 1 : V> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = W == 1 ? 0 : wave;
-  const Lane<V, TX> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
+  const Lane<V, TX, PAST> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
   const int64_t C = l.C, i = l.i;
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
@@ -230,7 +235,7 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
 #pragma unroll
       for (int k = 0; k < V; ++k) f[s][k] = INFINITY, q[s][k] = 0.f;
       if (l.ok && t0 + s < te) {
-        loadv<TG, V>(a.g, (t0 + s) * C + i, l.o, f[s]);
+        loadv<TG, V, PAST>(a.g, (t0 + s) * C + i, l.o, f[s]);
         l.x(a, t0 + s, q[s]);
       }
     }
@@ -287,12 +292,12 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
 }
 
 // The same in reversed time: a wave's step s is time te - 1 - (its position).
-template <int W, int V, int SEG, int TG, int TX, bool FIRST>
+template <int W, int V, int SEG, int TG, int TX, bool FIRST, bool PAST>
 __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
   constexpr int TD = TX == MGN_E4M3 ? TG : TX;
   __shared__ Joint<W, W == 1 ? 1 : V> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = W == 1 ? 0 : wave;
-  const Lane<V, TX> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
+  const Lane<V, TX, PAST> l(a, a.tile0 + (W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x));
   const int64_t C = l.C, i = l.i;
   const int c = blockIdx.y;
   // reversed steps u = steps - 1 - t of this chunk
@@ -327,11 +332,11 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
       }
       if (l.ok && u0 + s < ue) {
         const int64_t t = a.steps - 1 - (u0 + s);
-        loadv<TG, V>(a.g, t * C + i, l.o, f[s]);
-        if (a.dh) loadv<MGN_FP32, V>(a.dh, t * C + i, l.o, d[s]);
+        loadv<TG, V, PAST>(a.g, t * C + i, l.o, f[s]);
+        if (a.dh) loadv<MGN_FP32, V, PAST>(a.dh, t * C + i, l.o, d[s]);
         if constexpr (!FIRST) {
           l.x(a, t, z[s]);
-          if (t > 0) loadv<MGN_FP32, V>(a.h, (t - 1) * C + i, l.o, m[s]);
+          if (t > 0) loadv<MGN_FP32, V, PAST>(a.h, (t - 1) * C + i, l.o, m[s]);
           else if (a.h0) loadv<MGN_FP32, V>(a.h0, i, l.o, m[s]);
         }
       }
@@ -476,7 +481,15 @@ hipError_t by_deal(const Deal& d, F f) {
 }
 
 bool at(const void* p, int bytes) { return (uintptr_t)p % bytes == 0; }
-int quad(int type) { return type == MGN_FP32 ? 16 : type == MGN_BF16 ? 8 : 4; }
+int bytes(int type) { return type == MGN_FP32 ? 4 : type == MGN_BF16 ? 2 : 1; }
+int quad(int type) { return 4 * bytes(type); }
+// A scan of four columns a lane that moves more than the last-level cache holds
+// reads past it: 16 steps of 250,000 x 128 bf16 793 us through it, 752 past it, its
+// backward 1624 and 1551; below, 20 steps of 5,000 x 64 bf16 19 and 26 us, its
+// backward 26 and 34, both in turn on 16 x 10,000 x 128 fp32 113 and 131.  It
+// writes past it at any size (16 x 10,000 x 128 fp32, both in turn: 113 us, 129
+// otherwise; 20 x 5,000 x 64 bf16 52 and 45).
+constexpr int64_t CACHE = (int64_t)256 << 20;
 
 }  // namespace
 
@@ -494,6 +507,7 @@ hipError_t launch_scan(ScanArgs a, int g_type, int x_type, hipStream_t st) {
   const bool vec = (x_type == MGN_E4M3 ? a.cols : C) % 4 == 0 && at(a.g, quad(g_type)) && at(a.x, quad(x_type)) &&
                    at(a.h0, 16) && at(a.h, 16) && at(a.h_last, 16);
   const Deal d = deal(a.steps, C, vec);
+  const bool past = a.steps * C * (bytes(g_type) + bytes(x_type) + (a.h ? 4 : 0)) > CACHE;
   a.chunk = d.chunk;
   return by_types(g_type, x_type, [&](auto tg, auto tx) {
     return by_deal(d, [&](auto w, auto v) {
@@ -505,12 +519,20 @@ hipError_t launch_scan(ScanArgs a, int g_type, int x_type, hipStream_t st) {
         const unsigned gx = (unsigned)(W == 1 ? (n + 3) / 4 : n);
         if constexpr (W == 8 && V == 1) {
           if (d.chunks > 1) {
-            hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
+            hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), true, false>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
           }
         }
-        hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks), block, 0, st, a);
+        const dim3 grid(gx, (unsigned)d.chunks);
+        if constexpr (V == 4) {
+          if (past)
+            hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false, true>), grid, block, 0, st, a);
+          else
+            hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false, false>), grid, block, 0, st, a);
+        } else {
+          hipLaunchKernelGGL((scan_kernel<W, V, SEG, tg(), tx(), false, false>), grid, block, 0, st, a);
+        }
         e = hipGetLastError();
       }
       return e;
@@ -527,6 +549,7 @@ hipError_t launch_scan_grad(ScanArgs a, int g_type, int x_type, hipStream_t st) 
                    at(a.h0, 16) && at(a.h, 16) && at(a.dh, 16) && at(a.dh_last, 16) && at(a.dg, quad(g_type)) &&
                    at(a.dx, quad(d_type)) && at(a.dh0, 16);
   const Deal d = deal(a.steps, C, vec);
+  const bool past = a.steps * C * (bytes(g_type) + bytes(x_type) + bytes(g_type) + bytes(d_type) + (a.dh ? 8 : 4)) > CACHE;
   a.chunk = d.chunk;
   return by_types(g_type, x_type, [&](auto tg, auto tx) {
     return by_deal(d, [&](auto w, auto v) {
@@ -538,12 +561,20 @@ hipError_t launch_scan_grad(ScanArgs a, int g_type, int x_type, hipStream_t st) 
         const unsigned gx = (unsigned)(W == 1 ? (n + 3) / 4 : n);
         if constexpr (W == 8 && V == 1) {
           if (d.chunks > 1) {
-            hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), true>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
+            hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), true, false>), dim3(gx, (unsigned)d.chunks - 1), block, 0, st, a);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
           }
         }
-        hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false>), dim3(gx, (unsigned)d.chunks), block, 0, st, a);
+        const dim3 grid(gx, (unsigned)d.chunks);
+        if constexpr (V == 4) {
+          if (past)
+            hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false, true>), grid, block, 0, st, a);
+          else
+            hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false, false>), grid, block, 0, st, a);
+        } else {
+          hipLaunchKernelGGL((scan_grad_kernel<W, V, SEG, tg(), tx(), false, false>), grid, block, 0, st, a);
+        }
         e = hipGetLastError();
       }
       return e;

@@ -291,25 +291,38 @@ def test_arrays_aligned_to_their_type_only(T, rows, cols, typ):
         assert all(torch.allclose(p.float(), q.float(), rtol=tol, atol=tol) for p, q in zip((dg, dx, d0), want))
 
 
-@pytest.mark.parametrize("T,rows,cols", [(9, 1 << 22, 128), (2, 600_001, 121)])
-def test_many_columns(T, rows, cols):
-    """Offsets past 2^32 elements, and more columns than one launch takes (four
-    and one a lane): some rows against float64."""
-    print(f"[scan] {T} x {rows} x {cols} bf16", flush=True)
-    g = torch.empty(T, rows, cols, dtype=torch.bfloat16, device="cuda").normal_()
-    x = torch.empty_like(g).normal_()
+@pytest.mark.parametrize("T,rows,cols,typ,x8", [(9, 1 << 22, 128, "bf16", False), (2, 600_001, 121, "bf16", False),
+                                                (700, 1000, 128, "fp32", False), (400, 2000, 128, "bf16", True),
+                                                (40, 40_001, 128, "fp32", False), (40, 40_001, 128, "fp32", True),
+                                                (40, 60_001, 128, "bf16", True)])
+def test_large_windows(T, rows, cols, typ, x8):
+    """Offsets past 2^32 elements, more columns than one launch takes (four
+    and one a lane), and windows that the caches do not hold in every form and
+    type: some rows against float64."""
+    print(f"[scan] {T} x {rows} x {cols} {typ} x8={x8}", flush=True)
+    dt = torch.float32 if typ == "fp32" else torch.bfloat16
+    g = torch.empty(T, rows, cols, dtype=dt, device="cuda").normal_()
+    if x8:
+        c = LatentCache(T * rows, cols)
+        c.store(torch.empty(T * rows, cols, device="cuda").normal_())
+        x, xs = c.window(0, T, rows)
+    else:
+        x, xs = torch.empty_like(g).normal_(), None
     h = torch.empty(T, rows, cols, device="cuda")
-    mgn.mgn_gated_scan(g, x, h=h)
+    mgn.mgn_gated_scan(g, x, h=h, x_scale=xs)
     at = [0, 1, rows // 2, rows - 1]
-    h64, e = ref.scan(ref.f64(g[:, at]), ref.f64(x[:, at]), None, None)
+    x64 = ref.values8(x[:, at], xs[:, at]) if x8 else ref.f64(x[:, at])
+    h64, e = ref.scan(ref.f64(g[:, at]), x64, None, None)
     _near("h", h[:, at], h64, e)
     dg, dx = torch.empty_like(g), torch.empty_like(g)
     dl = torch.randn(rows, cols, device="cuda")
-    mgn.mgn_gated_scan_grad(g, x, h, dg, dx, dh_last=dl)
-    a, b, _, ea, eb, _ = ref.scan_grad(ref.f64(g[:, at]), ref.f64(x[:, at]), ref.f64(h[:, at]), None, None, None,
-                                       ref.f64(dl[at]))
-    _near("dg", dg[:, at], a, ea + np.abs(a) * (ref.U16 + ref.U32))
-    _near("dx", dx[:, at], b, eb + np.abs(b) * (ref.U16 + ref.U32))
+    dh = torch.empty_like(h).normal_() if T * rows < 1 << 24 else None
+    mgn.mgn_gated_scan_grad(g, x, h, dg, dx, dh=dh, dh_last=dl, x_scale=xs)
+    a, b, _, ea, eb, _ = ref.scan_grad(ref.f64(g[:, at]), x64, ref.f64(h[:, at]), None, None,
+                                       None if dh is None else ref.f64(dh[:, at]), ref.f64(dl[at]))
+    u = ref.half(dt) + ref.U32
+    _near("dg", dg[:, at], a, ea + np.abs(a) * u)
+    _near("dx", dx[:, at], b, eb + np.abs(b) * u)
 
 
 @pytest.mark.parametrize("T,rows,cols", [(6, 50, 128), (5000, 1, 64)])
