@@ -43,6 +43,9 @@ __device__ __forceinline__ void gates(float g, float& f, float& z) {
 }
 
 __device__ __forceinline__ float term(float weight, float v) { return weight == 0.f ? 0.f : weight * v; }
+// The factor of two joined stretches of time: 0 where either is, whatever the
+// other one (a NaN gate too ends at a start or at a state that is replaced).
+__device__ __forceinline__ float joined(float p, float f) { return p == 0.f || f == 0.f ? 0.f : p * f; }
 // p y + q, without y where p is 0
 __device__ __forceinline__ float step(float p, float y, float q) { return p == 0.f ? q : fmaf(p, y, q); }
 
@@ -157,7 +160,7 @@ __device__ __forceinline__ void chunk_entry(const ScanArgs& a, int c, int64_t i,
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         q[k] = step(pe[k], q[k], qe[k]);
-        p[k] *= pe[k];
+        p[k] = joined(p[k], pe[k]);
       }
     }
 #pragma unroll
@@ -256,7 +259,7 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
         if (fresh) f[s][k] = 0.f;
         if constexpr (W > 1 || FIRST) {
           r[k] = step(f[s][k], r[k], q[s][k]);
-          p[k] *= f[s][k];
+          p[k] = joined(p[k], f[s][k]);
         }
       }
     }
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
 #pragma unroll
       for (int e = 0; e < W; ++e)
 #pragma unroll
-        for (int k = 0; k < V; ++k) pt[k] *= lds.v[par][e][0][threadIdx.x & 63][k];
+        for (int k = 0; k < V; ++k) pt[k] = joined(pt[k], lds.v[par][e][0][threadIdx.x & 63][k]);
     } else {
 #pragma unroll
       for (int s = 0; s < SEG; ++s) {
@@ -362,7 +365,7 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
         if (fresh) f[s][k] = 0.f;
         if constexpr (W > 1 || FIRST) {
           r[k] = term(f[s][k], r[k] + d[s][k]);
-          p[k] *= f[s][k];
+          p[k] = joined(p[k], f[s][k]);
         }
       }
     }
@@ -372,7 +375,7 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
 #pragma unroll
       for (int e = 0; e < W; ++e)
 #pragma unroll
-        for (int k = 0; k < V; ++k) pt[k] *= lds.v[par][e][0][threadIdx.x & 63][k];
+        for (int k = 0; k < V; ++k) pt[k] = joined(pt[k], lds.v[par][e][0][threadIdx.x & 63][k]);
     } else {
 #pragma unroll
       for (int s = 0; s < SEG; ++s) {
