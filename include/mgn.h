@@ -296,10 +296,11 @@ mgn_status mgn_rms_norm_grad(const void* total, int32_t type, const float* weigh
  * entry begins a trajectory, its step takes 0 for h_{t-1}.  States are fp32: h
  * [steps][rows][cols] (NULL: not stored), h_last [rows][cols] = the last state
  * (NULL: not wanted; it may be h0, so that a rollout's step updates its state
- * in place; with no steps it is h0).  A weight f or z (or a product of
- * successive f) below 2^-126 counts as 0 and its term is left out whatever it
- * multiplies: g = +inf (or the type's largest value) holds a state, to a
- * rounding, through steps whose x is not defined, -inf replaces it.
+ * in place; with no steps it is h0).  A weight f or z below 2^-126 counts as 0
+ * and its term is left out whatever it multiplies: g = +inf (or the type's
+ * largest value) holds a state, to a rounding, through steps whose x is not
+ * defined, -inf replaces it.  A state that is NaN or infinite lasts until a start
+ * or a gate that counts as 0; a finite one may keep 2^-149 of itself for as long.
  * work: device scratch of mgn_gated_scan_work bytes, 16-byte aligned (NULL
  * when that is 0); MGN_E_NOMEM when work_bytes is less.  steps, rows >= 0,
  * 1 <= cols <= MGN_ROW_MAX_COLS.  Arrays must not overlap beyond what is

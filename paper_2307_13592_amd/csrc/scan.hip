@@ -44,8 +44,14 @@ __device__ __forceinline__ void gates(float g, float& f, float& z) {
 
 __device__ __forceinline__ float term(float weight, float v) { return weight == 0.f ? 0.f : weight * v; }
 // The factor of two joined stretches of time: 0 where either is, whatever the
-// other one (a NaN gate too ends at a start or at a state that is replaced).
-__device__ __forceinline__ float joined(float p, float f) { return p == 0.f || f == 0.f ? 0.f : p * f; }
+// other one (a NaN gate too ends at a start or at a state that is replaced),
+// and nowhere else: a product that passes below fp32 stays at the smallest
+// number, 2^-149, so that a NaN or infinite state lasts as it does step by step
+// (a finite one y is then off by at most 2^-149 |y|, as by that number's rounding).
+__device__ __forceinline__ float joined(float p, float f) {
+  const float v = p * f;
+  return p == 0.f || f == 0.f ? 0.f : v == 0.f ? 1.40129846e-45f : v;
+}
 // p y + q, without y where p is 0
 __device__ __forceinline__ float step(float p, float y, float q) { return p == 0.f ? q : fmaf(p, y, q); }
 

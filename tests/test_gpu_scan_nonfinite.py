@@ -82,3 +82,61 @@ def test_nan_gate_ends_with_its_trajectory(T, rows, cols, reset):
         assert torch.equal(out["h"].view(T, C)[~hit], clean["h"].view(T, C)[~hit])
         assert bool(out["last"].isfinite().all()) and bool(out["dh0"].isfinite().all())
         _against_definition(c, out, col + [C // 3])
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("T,rows,cols", DEALS + [(8192, 3, 64), (8192, 1, 1)])
+def test_nonfinite_states_last(T, rows, cols, value):
+    """A state (backward: a gradient) that is NaN or infinite stays so, however
+    far its finite part would have decayed, to the next start or gate of -inf."""
+    print(f"[scan] a state of {value} lasts: T={T} {rows} x {cols}", flush=True)
+    C = rows * cols
+    col = [0, C // 2, C - 1]
+    for where in ("x", "h0"):
+        c = _inputs(T, rows, cols, seed=4)
+        clean = _run(c)
+        if where == "x":
+            c["x"].view(T, C)[1, col] = value
+            c["dh"].view(T, C)[T - 2, col] = value
+        else:
+            c["h0"].view(C)[col] = value
+            c["dh_last"].view(C)[col] = value
+        out = _run(c)
+        first = 1 if where == "x" else 0
+        bad = out["h"].view(T, C)[first:, col]
+        assert bool(bad.isnan().all()) if value != value else bool((bad == value).all())
+        assert not bool(out["dh0"].view(C)[col].isfinite().any())
+        keep = torch.ones(C, dtype=torch.bool, device="cuda")
+        keep[col] = False
+        for k in ("h", "dg", "dx"):
+            assert torch.equal(out[k].view(T, C)[:, keep], clean[k].view(T, C)[:, keep]), k
+        _against_definition(c, out, col)
+        # and with a start and a replaced state far behind
+        a, b = T // 3, T - T // 3
+        c["starts"][a] = 1
+        c["g"].view(T, C)[b, col] = -float("inf")
+        out = _run(c)
+        assert bool(out["h"].view(T, C)[a:].isfinite().all()) and bool(out["dh0"].isfinite().all())
+        _against_definition(c, out, col)
+
+
+def test_nan_gate_leaves_neighbours_alone():
+    c = _inputs(1000, 3, 64, seed=9)
+    clean = _run(c)
+    c["g"][17, 1, 5] = float("nan")
+    out = _run(c)
+    for k in ("h", "dg", "dx"):
+        keep = torch.ones_like(out[k], dtype=torch.bool)
+        keep[:, 1, 5] = False
+        assert torch.equal(out[k][keep], clean[k][keep]), k
+    _against_definition(c, out, [69, 0])
+
+
+@pytest.mark.parametrize("T,rows,cols", [(1000, 3, 64), (2050, 50, 128), (40, 600, 128)])
+def test_large_states_decay(T, rows, cols):
+    """A finite state of 1e30 leaves no more than the smallest number's share
+    behind (2^-149 of it, below half a step of states near 1e-6)."""
+    c = _inputs(T, rows, cols, seed=5, gate=-1.0)
+    c["h0"].mul_(1e30)
+    c["dh_last"].mul_(1e30)
+    _against_definition(c, _run(c), [0, 1, rows * cols // 2, rows * cols - 1])
