@@ -236,7 +236,18 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
       }
     sums(s);
     const float inv = rsqrtf(s[0] * mean + a.eps);
-    const float m = s[1] * inv * mean;  // mean(u w dy)
+    float m = s[1] * inv * mean;  // mean(u w dy)
+    if (inv == 0.f) {
+      // squares past the fp32 range: no gradient through the norm.  The second
+      // sum may have passed it too; m is 0 for a finite row, NaN for others.
+      s[0] = s[1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[0] += v[j][k] - v[j][k];
+      sums(s);
+      m = s[0];
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float d[V];
