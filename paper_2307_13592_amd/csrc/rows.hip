@@ -194,26 +194,45 @@ __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
 //   dt = (w dy - u mean(u w dy)) inv + d_total;  dw += dy u.
 // (Where w dy lies along t, as in a row of one column, the difference cancels to a
 // share eps inv^2 of its terms, and carries their rounding.)
-// Each thread sums dw of its columns over its rows in fp32; the workgroup's
-// row groups are added in order, in fp64, and leave one partial per column, of at most
+// dw is a long sum over rows: a thread adds its columns' products over DW_ROWS
+// rows in fp32 and these in fp64, in LDS (rows of a whole workgroup in fp64 at
+// once; fp64 registers for all cost 100,000 x 999 bf16 118 -> 160 us).  The
+// workgroup's row groups are added in order, in fp64, and leave one partial per
+// column, rounded to fp32 (at most half a step of it), of at most
 // MGN_RMS_WORK_PER_COL workgroups (1M x 128 fp32 rows with d_total 360 us, 5.7
 // TB/s; with twice as many workgroups 417).  Unaligned rows (100,003 x 77 bf16)
 // take 15 us, 3.1 TB/s: their stores share lines, so that 1.5 times the bytes
 // are written, and six rounds of rows a wave leave the last one part empty.
+constexpr int DW_ROWS = 16;
 template <int TPR, int NV, int V, int MODE, int TI>
 __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
   using D = Cols<TPR, V, MODE>;
   constexpr int NT = threads(TPR), GROUPS = NT / TPR, W = NV * TPR * V;  // row groups; columns dealt to one
   __shared__ typename RowSum<TPR, 2>::Lds lds;
   RowSum<TPR, 2> sums(lds);
-  __shared__ float part[GROUPS > 1 ? GROUPS * W : 1];
+  // [row group][column]: each thread adds to its own places only
+  __shared__ double part[GROUPS > 1 ? GROUPS * W : 1];
+  double* const mine = part + threadIdx.x / TPR * W;
   Rows<TPR> q;
-  float w[NV][V], dw[NV][V];
+  float w[NV][V];
+  std::conditional_t<(GROUPS > 1), float, double> dw[NV][V];
+  int turn = 0;
   load_weight<D>(a, q.t, w);
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int k = 0; k < V; ++k) dw[j][k] = 0.f;
+    for (int k = 0; k < V; ++k) {
+      dw[j][k] = 0;
+      if constexpr (GROUPS > 1) mine[D::first(j, q.t) + D::STRIDE * k] = 0;
+    }
+  const auto add = [&] {
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) mine[D::first(j, q.t) + D::STRIDE * k] += dw[j][k], dw[j][k] = 0;
+    }
+  };
   const float mean = 1.f / (float)a.cols;
   for (; q.row < a.rows; q.row += q.next) {
     const int64_t base = q.row * a.cols;
@@ -260,6 +279,7 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
       }
       store_cols<TI, D>(a.total, base, o, D::first(j, q.t), cols, d);
     }
+    if (++turn % DW_ROWS == 0) add();
   }
   if (!a.part) return;
   float* dst = a.part + (int64_t)blockIdx.x * a.cols;
@@ -269,14 +289,10 @@ __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const int c = D::first(j, q.t) + D::STRIDE * k;
-        if (c < a.cols) dst[c] = dw[j][k];
+        if (c < a.cols) dst[c] = (float)dw[j][k];
       }
   } else {
-    const int grp = threadIdx.x / TPR;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int k = 0; k < V; ++k) part[grp * W + D::first(j, q.t) + D::STRIDE * k] = dw[j][k];
+    add();
     __syncthreads();
     for (int c = threadIdx.x; c < a.cols; c += NT) {
       double total = part[c];
