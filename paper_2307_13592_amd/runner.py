@@ -256,17 +256,22 @@ class GatedMemory:
         return self.state
 
     def scan(self, g, x, starts=None, x_scale=None, stream=None):
-        """Every state of a trajectory [steps][rows][cols] that continues from
-        `state`, which becomes the last one."""
+        """Every state h of a trajectory [steps][rows][cols] that continues from
+        `state`, which becomes the last one; h.h0 is the state it began with."""
         h = torch.empty(g.shape, dtype=torch.float32, device=g.device)
+        h0 = torch.empty_like(self.state)
         none = None if x_scale is None else x_scale[:0]
-        mgn_gated_scan(g[:0], x[:0], None, self.h0, self.state, None, none, None, stream)  # h0 <- state
-        mgn_gated_scan(g, x, h, self.state, self.h0, starts, x_scale, None, stream)
+        mgn_gated_scan(g[:0], x[:0], None, h0, self.state, None, none, None, stream)  # h0 <- state
+        mgn_gated_scan(g, x, h, self.state, h0, starts, x_scale, None, stream)
+        self.h0 = h.h0 = h0
         return h
 
-    def grad(self, g, x, h, dh=None, dh_last=None, starts=None, x_scale=None, stream=None):
-        """(dg, dx, dh0) of the last scan()."""
+    def grad(self, g, x, h, dh=None, dh_last=None, starts=None, x_scale=None, stream=None, h0=None):
+        """(dg, dx, dh0) of the scan() that returned h.  h0: the state which that
+        began with; without it h.h0, and for an h that carries none (a copy) that
+        of the last scan()."""
         dg, dx = torch.empty_like(g), torch.empty_like(g)
         dh0 = torch.empty_like(self.state)
-        mgn_gated_scan_grad(g, x, h, dg, dx, dh, dh_last, dh0, self.h0, starts, x_scale, None, stream)
+        h0 = getattr(h, "h0", self.h0) if h0 is None else h0
+        mgn_gated_scan_grad(g, x, h, dg, dx, dh, dh_last, dh0, h0, starts, x_scale, None, stream)
         return dg, dx, dh0
