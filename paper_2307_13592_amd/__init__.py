@@ -8,6 +8,7 @@ kernels of libmgn.so; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -381,15 +382,23 @@ def _run(fn: str, dev: int, stream, *args) -> None:
         _check(st)
 
 
+def _on(stream, device):
+    """Context in which torch allocates on `stream` (None: the current one): what
+    a call on that stream writes must come from there, or the allocator could
+    hand it out while work queued elsewhere still uses it."""
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device))
+
+
 def _scratch(nbytes: int, dev: int, stream):
     """Device scratch for one call on `stream`: from torch's allocator, on that
     stream, so that it is not handed out again before the call has run (and
     belongs to a HIP graph that records the call)."""
     import torch
     device = torch.device("cuda", dev) if dev >= 0 else None
-    if stream is None or device is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
+    with _on(None if device is None else stream, device):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 

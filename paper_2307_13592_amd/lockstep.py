@@ -17,7 +17,7 @@ import numpy as np
 import torch
 
 from . import (mgn_halo_masks, mgn_lockstep_backward, mgn_lockstep_backward8, mgn_lockstep_forward,
-               mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step)
+               mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step, _on)
 from .runner import LatentCache, Session
 
 
@@ -86,8 +86,9 @@ class Lockstep:
         rows = sum(s.out.shape[0] if m is None else int(m.count_nonzero().item()) for s, m in zip(S, masks))
         shares, d_outs = [], []
         for s, t, m in zip(S, targets, masks):
-            loss = torch.empty(2, dtype=torch.float32, device=self.device)
-            d_out = torch.empty_like(s.out)
+            with _on(stream, self.device):
+                loss = torch.empty(2, dtype=torch.float32, device=self.device)
+                d_out = torch.empty_like(s.out)
             mgn_mse_grad_global(s.out, t, m, max(rows, 1), loss, d_out, stream)
             shares.append(loss[0])
             d_outs.append(d_out)

@@ -10,7 +10,7 @@ from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_d
                mgn_graph_validate, mgn_mse_grad, mgn_param_count, mgn_set_params, mgn_set_recompute,
                mgn_norm_accumulate, mgn_norm_apply, MGN_NORM_WORK_PER_COL, mgn_rollout_update, mgn_set_h1_stash,
                mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
-               mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks)
+               mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on)
 
 
 class Session:
@@ -116,14 +116,16 @@ class Session:
             if history is not None:
                 history.store(self.out, first=t * n, stream=stream)
             else:
-                outs.append(self.out.clone())
+                with _on(stream, self.device):
+                    outs.append(self.out.clone())
             p = self.out if memory is None else memory.step(self.out, stream=stream)
             mgn_rollout_update(p, self.node_feat, col0, stream)
         return outs if history is None else history
 
     def mse(self, target, mask=None, stream=None):
-        loss = torch.empty(2, dtype=torch.float32, device=self.device)
-        d_out = torch.empty_like(self.out)
+        with _on(stream, self.device):
+            loss = torch.empty(2, dtype=torch.float32, device=self.device)
+            d_out = torch.empty_like(self.out)
         mgn_mse_grad(self.out, target, mask, loss, d_out, stream)
         return loss, d_out
 
@@ -157,7 +159,8 @@ class Normalizer:
         mgn_norm_accumulate(x, self.stats, self.work, stream)
 
     def apply(self, x, out=None, stream=None):
-        out = torch.empty_like(x) if out is None else out
+        with _on(stream, x.device):
+            out = torch.empty_like(x) if out is None else out
         mgn_norm_apply(x, self.stats, out, self.eps, stream)
         return out
 
@@ -214,8 +217,9 @@ class RmsNorm:
     def apply(self, x, res=None, dtype=None, stream=None):
         """(y, t): y the norm of t = x + res (of x without a residual) in
         `dtype` (x's by default)."""
-        y = torch.empty_like(x, dtype=x.dtype if dtype is None else dtype)
-        total = x if res is None else torch.empty_like(x)
+        with _on(stream, x.device):
+            y = torch.empty_like(x, dtype=x.dtype if dtype is None else dtype)
+            total = x if res is None else torch.empty_like(x)
         mgn_rms_norm(x, self.weight, y, res, None if res is None else total, None, self.eps, stream)
         return y, total
 
@@ -223,14 +227,16 @@ class RmsNorm:
         """The norm of x + res in 8 bits, into the cache's slots from `first`
         on; returns the sum."""
         q, scale = cache._span(first, x.shape[0])
-        total = x if res is None else torch.empty_like(x)
+        with _on(stream, x.device):
+            total = x if res is None else torch.empty_like(x)
         mgn_rms_norm(x, self.weight, q, res, None if res is None else total, scale, self.eps, stream)
         return total
 
     def grad(self, total, dy, d_total=None, accumulate: bool = False, stream=None):
         """dL/dt from dy and the gradient that reaches t otherwise; d_weight
         takes (accumulate: adds) dL/dweight."""
-        dx = torch.empty_like(total)
+        with _on(stream, total.device):
+            dx = torch.empty_like(total)
         mgn_rms_norm_grad(total, self.weight, dy, dx, self.d_weight, d_total, accumulate, None, self.eps, stream)
         return dx
 
@@ -258,8 +264,9 @@ class GatedMemory:
     def scan(self, g, x, starts=None, x_scale=None, stream=None):
         """Every state h of a trajectory [steps][rows][cols] that continues from
         `state`, which becomes the last one; h.h0 is the state it began with."""
-        h = torch.empty(g.shape, dtype=torch.float32, device=g.device)
-        h0 = torch.empty_like(self.state)
+        with _on(stream, g.device):
+            h = torch.empty(g.shape, dtype=torch.float32, device=g.device)
+            h0 = torch.empty_like(self.state)
         none = None if x_scale is None else x_scale[:0]
         mgn_gated_scan(g[:0], x[:0], None, h0, self.state, None, none, None, stream)  # h0 <- state
         mgn_gated_scan(g, x, h, self.state, h0, starts, x_scale, None, stream)
@@ -270,8 +277,9 @@ class GatedMemory:
         """(dg, dx, dh0) of the scan() that returned h.  h0: the state which that
         began with; without it h.h0, and for an h that carries none (a copy) that
         of the last scan()."""
-        dg, dx = torch.empty_like(g), torch.empty_like(g)
-        dh0 = torch.empty_like(self.state)
+        with _on(stream, g.device):
+            dg, dx = torch.empty_like(g), torch.empty_like(g)
+            dh0 = torch.empty_like(self.state)
         h0 = getattr(h, "h0", self.h0) if h0 is None else h0
         mgn_gated_scan_grad(g, x, h, dg, dx, dh, dh_last, dh0, h0, starts, x_scale, None, stream)
         return dg, dx, dh0

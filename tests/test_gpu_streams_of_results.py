@@ -1,0 +1,62 @@
+"""Arrays that a call allocates for its results belong to the stream the call
+runs on: torch's allocator then hands their memory out again behind the call
+only, and no work queued on another stream still uses it."""
+import numpy as np
+import pytest
+import torch
+
+from parity import local_inputs
+from paper_2307_13592_amd.runner import GatedMemory, LatentCache, Normalizer, RmsNorm, Session
+from synth import meshes
+
+pytestmark = pytest.mark.gpu
+
+
+def _stream_of(t):
+    """The stream whose memory a tensor holds."""
+    p = t.untyped_storage().data_ptr()
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= p < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not in the allocator's memory")
+
+
+def _owned(side, *ts):
+    assert [_stream_of(t) for t in ts] == [side.cuda_stream] * len(ts)
+
+
+def test_norm_memory_and_normalizer():
+    side = torch.cuda.Stream()
+    x, res, g = torch.randn(50, 64, device="cuda"), torch.randn(50, 64, device="cuda"), torch.randn(9, 50, 64, device="cuda")
+    nz, mem, cache, std = RmsNorm(64), GatedMemory(50, 64), LatentCache(50, 64), Normalizer(64)
+    torch.cuda.synchronize()
+    st = dict(stream=side.cuda_stream)
+    y, t = nz.apply(x, res, **st)
+    h = mem.scan(g, g, **st)
+    out = [y, t, nz.store(x, cache, res=res, **st), nz.grad(t, y, **st), h, h.h0, *mem.grad(g, g, h, g, **st)]
+    std.accumulate(x, **st)
+    out.append(std.apply(x, **st))
+    _owned(side, *out)
+    side.synchronize()
+    assert [_stream_of(v) for v in (x, nz.apply(x, res)[0])] == [torch.cuda.current_stream().cuda_stream] * 2
+
+
+def test_rollout_and_loss():
+    mesh = meshes.delaunay_box(8, 7, 6, seed=3)
+    c = local_inputs(mesh, 0, 64, 2, 2, 6, part=np.zeros(mesh.n_nodes, np.int32))
+    s = Session(64, 2, 2, "fp32", c["g"], c["nf"], c["ef"], c["halo"], c["params"], inference=True)
+    try:
+        nf = s.node_feat.clone()
+        want = s.rollout(3)
+        loss = s.mse(nf[:, :5].contiguous())
+        s.node_feat.copy_(nf)
+        target = nf[:, :5].contiguous()
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        got = s.rollout(3, stream=side.cuda_stream)
+        loss2 = s.mse(target, stream=side.cuda_stream)
+        _owned(side, *got, *loss2)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*want, *loss), (*got, *loss2)))
+    finally:
+        s.close()
