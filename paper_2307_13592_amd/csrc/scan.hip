@@ -43,15 +43,15 @@ __device__ __forceinline__ void gates(float g, float& f, float& z) {
 }
 
 __device__ __forceinline__ float term(float weight, float v) { return weight == 0.f ? 0.f : weight * v; }
-// The factor of two joined stretches of time: 0 where either is, whatever the
-// other one (a NaN gate too ends at a start or at a state that is replaced),
-// and nowhere else: a product that passes below fp32 stays at the smallest
-// number, 2^-149, so that a NaN or infinite state lasts as it does step by step
-// (a finite one y is then off by at most 2^-149 |y|, as by that number's rounding).
-__device__ __forceinline__ float joined(float p, float f) {
-  const float v = p * f;
-  return p == 0.f || f == 0.f ? 0.f : v == 0.f ? 1.40129846e-45f : v;
-}
+// The factor p of a stretch of time: 0 where one of its gates is (cut), and
+// nowhere else: a product that passes below fp32 stays at the smallest number,
+// 2^-149, so that a NaN or infinite state lasts as it does step by step (a finite
+// one y is then off by at most 2^-149 |y|, as by that number's rounding).  A NaN
+// gate needs no trace in p: the stretch's q is NaN from it to the next cut.
+constexpr float LEAST = 1.40129846e-45f;
+__device__ __forceinline__ float factor(float p, bool cut) { return cut ? 0.f : fmaxf(p, LEAST); }
+// That of two joined stretches.
+__device__ __forceinline__ float joined(float p, float f) { return f == 0.f ? 0.f : fmaxf(p * f, fminf(p, LEAST)); }
 // p y + q, without y where p is 0
 __device__ __forceinline__ float step(float p, float y, float q) { return p == 0.f ? q : fmaf(p, y, q); }
 
@@ -252,8 +252,9 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
     // wave reads that array, which another wave's last step may write
     const bool head = !FIRST && w == 0 && t == ts && !chunked<W, V>();
     float p[V], r[V];
+    bool cut[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) p[k] = head ? 0.f : 1.f, r[k] = head ? y[k] : 0.f;
+    for (int k = 0; k < V; ++k) p[k] = 1.f, cut[k] = head, r[k] = head ? y[k] : 0.f;
 #pragma unroll
     for (int s = 0; s < SEG; ++s) {
       const bool fresh = a.starts && t0 + s < te && a.starts[t0 + s];
@@ -265,10 +266,13 @@ __global__ __launch_bounds__(threads(W)) void scan_kernel(ScanArgs a) {
         if (fresh) f[s][k] = 0.f;
         if constexpr (W > 1 || FIRST) {
           r[k] = step(f[s][k], r[k], q[s][k]);
-          p[k] = joined(p[k], f[s][k]);
+          p[k] *= f[s][k];
+          cut[k] = cut[k] || f[s][k] == 0.f;
         }
       }
     }
+#pragma unroll
+    for (int k = 0; k < V; ++k) p[k] = factor(p[k], cut[k]);
     float end[V];
     if constexpr (W > 1) join<W, V>(lds, par, w, p, r, y, end);
     if constexpr (FIRST) {
@@ -354,8 +358,9 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
     // wave reads that array, which another wave's last step may write
     const bool head = !FIRST && w == 0 && u == us && !chunked<W, V>();
     float p[V], r[V];
+    bool cut[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) p[k] = head ? 0.f : 1.f, r[k] = head ? y[k] : 0.f;
+    for (int k = 0; k < V; ++k) p[k] = 1.f, cut[k] = head, r[k] = head ? y[k] : 0.f;
 #pragma unroll
     for (int s = 0; s < SEG; ++s) {
       const bool fresh = a.starts && u0 + s < ue && a.starts[a.steps - 1 - (u0 + s)];
@@ -371,10 +376,13 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
         if (fresh) f[s][k] = 0.f;
         if constexpr (W > 1 || FIRST) {
           r[k] = term(f[s][k], r[k] + d[s][k]);
-          p[k] = joined(p[k], f[s][k]);
+          p[k] *= f[s][k];
+          cut[k] = cut[k] || f[s][k] == 0.f;
         }
       }
     }
+#pragma unroll
+    for (int k = 0; k < V; ++k) p[k] = factor(p[k], cut[k]);
     float end[V];
     if constexpr (W > 1) join<W, V>(lds, par, w, p, r, y, end);
     if constexpr (FIRST) {
