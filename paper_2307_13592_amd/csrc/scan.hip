@@ -369,8 +369,10 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
         float zz;
         gates(f[s][k], f[s][k], zz);
         if constexpr (!FIRST) {
-          // m: f z (h_{t-1} - x), what dg takes of D; z: what dx takes
-          m[s][k] = term(f[s][k] * zz, (fresh ? 0.f : m[s][k]) - z[s][k]);
+          // m: f z (h_{t-1} - x), what dg takes of D, -0 where f or z is 0 and
+          // the term left out; z: what dx takes
+          const float fz = f[s][k] * zz;
+          m[s][k] = fz == 0.f ? -0.f : fmaf(fz, (fresh ? 0.f : m[s][k]) - z[s][k], 0.f);
           z[s][k] = zz;
         }
         if (fresh) f[s][k] = 0.f;
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(threads(W)) void scan_grad_kernel(ScanArgs a) {
           for (int k = 0; k < V; ++k) {
             const float D = d[s][k] + y[k];
             dx[k] = term(z[s][k], D);
-            dg[k] = term(m[s][k], D);
+            dg[k] = __float_as_uint(m[s][k]) == 0x80000000u ? 0.f : m[s][k] * D;
             y[k] = term(f[s][k], D);
           }
           if (l.ok) {

@@ -140,3 +140,23 @@ def test_large_states_decay(T, rows, cols):
     c["h0"].mul_(1e30)
     c["dh_last"].mul_(1e30)
     _against_definition(c, _run(c), [0, 1, rows * cols // 2, rows * cols - 1])
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T,rows,cols", DEALS)
+def test_gradients_that_are_not_finite_where_state_and_input_agree(T, rows, cols, value):
+    """h_{t-1} = x: dg is 0 times the gradient D, 0 for a finite D and NaN for
+    others, unless the step holds or replaces its state."""
+    C = rows * cols
+    c = _inputs(T, rows, cols, seed=6)
+    col = [0, C // 2, C - 1]
+    c["x"].view(T, C)[:, col] = 0
+    c["h0"].view(C)[col] = 0
+    c["dh"].view(T, C)[T - 1, col] = value
+    c["g"].view(T, C)[T - 1, 0] = float("inf")  # held
+    c["g"].view(T, C)[T // 2, C // 2] = -float("inf")  # replaced
+    out = _run(c)
+    dg = out["dg"].view(T, C)
+    assert float(dg[T - 1, 0]) == 0 and bool(dg[T - 1, col[1:]].isnan().all())
+    assert not dg[:T // 2 + 1, C // 2].any()
+    _against_definition(c, out, col + [C // 3])
