@@ -227,8 +227,9 @@ mgn_status mgn_norm_apply(const float* x, int64_t rows, int32_t cols, const doub
  * Device arrays of rows [n][cols], 1 <= cols <= MGN_ROW_MAX_COLS, contiguous
  * and aligned to their type (fp32 4 bytes, bf16 2); row counts are 64-bit.
  * Asynchronous on `stream`, no allocation, no atomics; the same inputs, in
- * arrays of the same alignment, give the same bits.  MGN_E_ARG for sizes or types outside what is stated, a NULL or
- * misaligned pointer, or arrays that overlap where it is not allowed.
+ * arrays of the same alignment, give the same bits.  MGN_E_ARG for sizes or
+ * types outside what is stated, a NULL or misaligned pointer, or arrays that
+ * overlap where it is not allowed.
  *
  * 8-bit rows are codes q [slots][cols] (one e4m3 byte a column: 4 exponent
  * bits, 3 of mantissa, largest value 448, no infinity) and scale
@@ -265,19 +266,21 @@ mgn_status mgn_rows_load8(const uint8_t* q, const float* scale, int64_t n_slots,
  * y_scale (NULL otherwise).  weight: fp32 [cols], or NULL for ones.  Sums are
  * taken in fp32 and y from the unrounded t.  total may be x or res, and y may
  * be x or res if it has their type and total is not that array too; no other
- * overlap.  A row whose squares pass the fp32 range gives zeros (and has no
- * gradient), a NaN or an infinity in a row NaNs there.  eps is a positive normal
- * number. */
+ * overlap.  A finite row whose squares pass the fp32 range gives zeros (and has
+ * no gradient through the norm), a NaN or an infinity in a row NaNs there.  eps
+ * is a positive normal number. */
 mgn_status mgn_rms_norm(const void* x, const void* res, int32_t type, int64_t rows, int32_t cols, const float* weight,
                         float eps, void* total, void* y, int32_t y_type, float* y_scale, mgn_stream stream);
-/* Its backward: total [rows][cols] is the sum that was normalised (x itself
- * without a residual), dy = dL/dy (8-bit rows: of the values before their
- * rounding), d_total (NULL: none) a gradient that reaches total on another way
- * (the residual stream).  dx receives the whole gradient of total, which is
- * that of x and of res alike; it may be dy, d_total or total.  All of `type`.
- * dweight (fp32 [cols], NULL: not wanted) is overwritten, or added to when
- * accumulate != 0; work is a device scratch array of MGN_RMS_WORK_PER_COL * cols
- * floats, overwritten (NULL allowed without dweight). */
+/* Its backward at total [rows][cols], the sum as it was stored (in MGN_BF16 the
+ * forward's y is of the sum before that rounding) or x itself without a residual.
+ * dy = dL/dy (8-bit rows: of the values before their rounding), d_total (NULL:
+ * none) a gradient that reaches total on another way (the residual stream).  dx
+ * receives the whole gradient of total, which is that of x and of res alike; it
+ * may be dy, d_total or total.  All of `type`, whatever y's type was.  dweight
+ * (fp32 [cols], NULL: not wanted) is overwritten, or added to when accumulate !=
+ * 0; its rows are added in fp64 but for groups of 16 and one partial a workgroup.
+ * work is a device scratch array of MGN_RMS_WORK_PER_COL * cols floats,
+ * overwritten (NULL allowed without dweight). */
 #define MGN_RMS_WORK_PER_COL 1024
 mgn_status mgn_rms_norm_grad(const void* total, int32_t type, const float* weight, float eps, const void* dy,
                              const void* d_total, int64_t rows, int32_t cols, void* dx, float* dweight,

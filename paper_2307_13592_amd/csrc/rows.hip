@@ -435,8 +435,7 @@ hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t s
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st) {
   int grid = 0;
   if (a.rows > 0) {
-      const RowMode mode = row_mode(a.rows * a.cols * type_bytes(type) * (3 + (a.res != nullptr)), type, a.rows,
-                                  a.cols,
+    const RowMode mode = row_mode(a.rows * a.cols * type_bytes(type) * (3 + (a.res != nullptr)), type, a.rows, a.cols,
                                   {a.x, a.dy, a.res});
     const hipError_t e = by_rows(type, a.cols, mode, [&](auto ti, auto tpr, auto nv, auto v, auto y) {
       grid = row_grid(a.rows, Rows<tpr()>::RPB, MGN_RMS_WORK_PER_COL);

@@ -32,8 +32,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // V = 4, bf16 V = 8) at once; rows of any width and alignment, since the card's
 // vector memory accesses need none; the columns past the last whole run are
 // written in pieces of 4, 2 and 1.  Otherwise (arrays of a few elements) the V =
-// 4 columns of a thread lie TPR apart, and are read one by one.  Either way the 128 columns of an 8-bit block lie with 128 / V
-// neighbouring lanes.
+// 4 columns of a thread lie TPR apart, and are read one by one.  Either way the
+// 128 columns of an 8-bit block lie with 128 / V neighbouring lanes.
 enum RowMode {
   APART,   // columns TPR apart
   RUNS,    // runs

@@ -30,9 +30,12 @@
 namespace mgn {
 namespace {
 
-// f and z of a gate logit, both with a small relative error: e = exp(-|g|),
-// 1 / (1 + e) and e / (1 + e).  A weight below the smallest normal number is 0,
-// and a term with a weight of 0 is left out whatever it multiplies.
+// f and z of a gate logit: e = exp(-|g|), 1 / (1 + e) and e / (1 + e).  The
+// exponent's product rounds once, so that the small weight is off by about |g|
+// half-steps of itself (less than 90: no smaller weight is left), and the large
+// one by a few; a more exact exponential would move a term that weighs e^-|g| of
+// the others.  A weight below the smallest normal number is 0, and a term with a
+// weight of 0 is left out whatever it multiplies.
 __device__ __forceinline__ void gates(float g, float& f, float& z) {
   const float e = __expf(-fabsf(g));
   const float big = __builtin_amdgcn_rcpf(1.f + e);

@@ -106,7 +106,8 @@ class Session:
         increments fed back are then its states, h <- f h + (1 - f) p.
         history: a LatentCache of at least steps * n_owned slots; the outputs
         are then kept there in 8 bits (step t in slots t n_owned ..), and the
-        cache is returned."""
+        cache is returned.  (A row of a few columns has a scale of 4 bytes of its
+        own: five columns take 9 bytes, against 20 in float32 and 10 in bfloat16.)"""
         n = self.out.shape[0]
         outs = []
         if history is not None and (history.cols != self.out.shape[1] or history.slots < steps * n):
@@ -167,8 +168,8 @@ class Normalizer:
 
 class LatentCache:
     """`slots` rows of `cols` columns held in 8 bits on the device (codes q,
-    one scale per 128 columns): packed halo rows, or the history of a rollout
-    or of a trajectory's node latents."""
+    one scale per 128 columns, cols + 4 ceil(cols / 128) bytes a row): packed halo
+    rows, or the history of a rollout or of a trajectory's node latents."""
 
     def __init__(self, slots: int, cols: int, device: str = "cuda"):
         self.slots, self.cols = slots, cols
