@@ -278,7 +278,7 @@ mgn_status mgn_rms_norm(const void* x, const void* res, int32_t type, int64_t ro
  * receives the whole gradient of total, which is that of x and of res alike; it
  * may be dy, d_total or total.  All of `type`, whatever y's type was.  dweight
  * (fp32 [cols], NULL: not wanted) is overwritten, or added to when accumulate !=
- * 0; its rows are added in fp64 but for groups of 16 and one partial a workgroup.
+ * 0; its rows are added in fp64 but for groups of 8 and one partial a workgroup.
  * work is a device scratch array of MGN_RMS_WORK_PER_COL * cols floats,
  * overwritten (NULL allowed without dweight). */
 #define MGN_RMS_WORK_PER_COL 1024

@@ -7,8 +7,10 @@
 // to TPR threads, 2 to 64 lanes of one wave or a workgroup of 256 or 1024
 // (rows8.h, Cols), NV runs of V columns each; a wave takes 64 / TPR rows at a
 // time.  As few threads as hold a row at 16 bytes each: of 1M x 128 bf16 rows the
-// norm takes 79 us (6.5 TB/s) and its backward 135 (5.7), against 104 and 235
+// norm takes 80 us (6.4 TB/s) and its backward 140 (5.5), against 104 and 235
 // with four columns a thread.
+// Times here are of calls queued one behind the other on two to four sets of
+// arrays; single launches under a kernel trace take some per cent longer.
 #include <initializer_list>
 #include <type_traits>
 
@@ -72,9 +74,9 @@ struct Rows {
 // Storing takes each block's largest finite magnitude over its lanes (DPP), the
 // scale from its bits and the codes from the card's conversion; reading back is
 // that conversion and one product.  Bound by HBM: 2M x 128 fp32 rows stored in
-// 236 us (5.5 TB/s) and read back in 206 (6.3); 100k of 2M such rows gathered by
-// an index list, 512 bytes at a random place each, 14 us (4.6 TB/s), and read
-// back into random rows 11 (5.8).
+// 236 us (5.5 TB/s) and read back in 175 - 208 (6.2 and more); 100k of 2M such
+// rows gathered by an index list, 512 bytes at a random place each, 14 us (4.5
+// TB/s), and read back into random rows 11 (5.8).
 
 template <int TPR, int NV, int V, int MODE, int TI>
 __global__ __launch_bounds__(threads(TPR)) void store8_kernel(Rows8Args a) {
@@ -140,8 +142,8 @@ __device__ __forceinline__ void load_weight(const RmsArgs& a, int t, float (&w)[
 
 // y = t / sqrt(mean(t^2) + eps) * w for t = x + res, in fp32; t is rounded
 // once where it is stored, y once where it is stored (y is formed from the
-// unrounded t).  1M x 128 fp32 rows with a residual: 352 us, 5.8 TB/s; 2M x 128
-// bf16 rows with one into 8-bit rows: 284 us, 6.3 TB/s.
+// unrounded t).  1M x 128 fp32 rows with a residual: 357 us, 5.7 TB/s; 2M x 128
+// bf16 rows with one into 8-bit rows: 286 us, 6.3 TB/s.
 template <int TPR, int NV, int V, int MODE, int TI, int TO>
 __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
   using D = Cols<TPR, V, MODE>;
@@ -199,11 +201,14 @@ __global__ __launch_bounds__(threads(TPR)) void rms_norm_kernel(RmsArgs a) {
 // once; fp64 registers for all cost 100,000 x 999 bf16 118 -> 160 us).  The
 // workgroup's row groups are added in order, in fp64, and leave one partial per
 // column, rounded to fp32 (at most half a step of it), of at most
-// MGN_RMS_WORK_PER_COL workgroups (1M x 128 fp32 rows with d_total 360 us, 5.7
-// TB/s; with twice as many workgroups 417).  Unaligned rows (100,003 x 77 bf16)
-// take 15 us, 3.1 TB/s: their stores share lines, so that 1.5 times the bytes
-// are written, and six rounds of rows a wave leave the last one part empty.
-constexpr int DW_ROWS = 16;
+// MGN_RMS_WORK_PER_COL workgroups.  Of 1M x 128 fp32 rows dw is off by 7.5e-8 of
+// itself (its products alone 5.3e-8, groups of 16 and 4 rows 8.8e-8 and 6.8e-8,
+// all of a thread's rows in fp32 2.0e-7); with d_total 357 us, 5.7 TB/s (twice as
+// many workgroups 377 - 427; groups of 4 rows up to 2 % longer on bf16 rows).
+// Unaligned rows (100,003 x 77 bf16) take 16 us, 2.9 TB/s: their stores share
+// lines, so that 1.5 times the bytes are written, and six rounds of rows a wave
+// leave the last one part empty.
+constexpr int DW_ROWS = 8;
 template <int TPR, int NV, int V, int MODE, int TI>
 __global__ __launch_bounds__(threads(TPR)) void rms_grad_kernel(RmsArgs a) {
   using D = Cols<TPR, V, MODE>;
@@ -325,13 +330,14 @@ __global__ __launch_bounds__(DW_NT) void rms_dw_kernel(const float* __restrict__
 
 // Rows at a time are dealt to at most this many workgroups, which then go
 // through them in turn: each reads the weights once (1M x 128 fp32 rows with a
-// residual 404 us with 8,192, 354 with 32,768, 336 with one turn each; 2M x 128
-// bf16 into 8-bit rows 287, 289 and 315).  Rows that are no whole runs, whose
-// weights cost more, prefer 8,192 (500k x 77 bf16 45 us, 61 with 32,768; 300k x
-// 300 bf16 78 and 89; 500k x 77 fp32 with a residual 131 and 129).  Storing
-// gathered rows prefers few (200k x 256 bf16 28.7 us with 8,192, 30.3 with
-// 32,768); reading 8-bit rows back needs no turns (2M x 128 to fp32 224 us with
-// 32,768 workgroups, 178 - 206 with as many as there are rows to deal).
+// residual 380 us with 8,192, 357 with 32,768, 332 with one turn each; 2M x 128
+// bf16 into 8-bit rows 287, 286 and 293; 500k x 256 fp32 into 8-bit rows 117, 113
+// and 140).  Rows that are no whole runs, whose weights cost more, prefer 8,192
+// (500k x 77 bf16 44 us, 55 with 32,768; 300k x 300 bf16 77 and 86; 500k x 77 fp32
+// with a residual 130 and 127).  Storing gathered rows prefers few (200k x 256
+// bf16 28.4 us with 8,192, 30.8 with 32,768); reading 8-bit rows back needs no
+// turns (2M x 128 to fp32 209 - 220 us with 32,768 workgroups, 175 - 208 with as
+// many as there are rows to deal).
 constexpr int64_t NORM_GRID = 32768, NORM_GRID_RUNS = 8192, STORE_GRID = 8192, LOAD_GRID = 1 << 20;
 int row_grid(int64_t rows, int rpb, int64_t most) {
   const int64_t b = (rows + rpb - 1) / rpb;
@@ -386,9 +392,9 @@ hipError_t by_rows(int type, int cols, RowMode mode, F f) {
 // How a kernel that moves `bytes` reads its arrays of `rows` rows: as whole runs
 // where they are that, on 16-byte boundaries, and past the caches where it moves
 // more than the last-level cache holds (256 MB).  Above: 2M x 128 bf16 rows with a
-// residual into 8-bit rows 324 us through the caches, 287 past them.  Below,
+// residual into 8-bit rows 313 us through the caches, 286 past them.  Below,
 // where the rows may still be cached: 200k of 400k x 256 bf16 rows gathered 28.4
-// and 34.7.
+// and 34.2.
 RowMode row_mode(int64_t bytes, int type, int64_t rows, int cols, std::initializer_list<const void*> arrays) {
   if (cols <= 16 && rows * cols < 16) return APART;
   bool even = cols % (type == MGN_FP32 ? 4 : 8) == 0;

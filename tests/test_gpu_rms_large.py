@@ -89,5 +89,5 @@ def test_backward_with_d_total(n, cols, dtype):
         assert bool(((dx[p].double() - want).abs() <= slack).all())
         sums += torch.stack([(g * u).sum(0), (g * u).abs().sum(0)])
         del v, g, u, wg, want, slack
-    # u within 32 half-steps, a product, 16 rows in fp32, a partial, the result
-    assert bool(((dw.double() - sums[0]).abs() <= sums[1] * (32 + 1 + 16 + 1) * ref.U32 + sums[0].abs() * ref.U32).all())
+    # u within 32 half-steps, a product, 8 rows in fp32, a partial, the result
+    assert bool(((dw.double() - sums[0]).abs() <= sums[1] * (32 + 1 + 8 + 1) * ref.U32 + sums[0].abs() * ref.U32).all())
