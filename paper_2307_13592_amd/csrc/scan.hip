@@ -18,11 +18,11 @@
 // read twice (mostly from the caches: such arrays are small), but no workgroup
 // waits for another.
 //
-// Bound by HBM with many columns: 16 steps of 250,000 x 128 bf16 752 us (5.8
-// TB/s), 20 of 100,003 x 64 backward from an 8-bit history 346 us (5.6), 600 of
-// 1,885 x 128 fp32 backward 660 us (5.3; 943 waves).  With few by the launches
+// Bound by HBM with many columns: 16 steps of 250,000 x 128 bf16 734 - 760 us
+// (5.7 TB/s), 20 of 100,003 x 64 backward from an 8-bit history 347 us (5.6), 600
+// of 1,885 x 128 fp32 backward 664 us (5.2; 943 waves).  With few by the launches
 // and a load's latency in each of them: 8,192 steps of 192 columns 15 us, backward
-// 18.  Loading a wave's next segment ahead of the join was slower (registers:
+// 19.  Loading a wave's next segment ahead of the join was slower (registers:
 // 400 steps of 10,240 columns backward 26 -> 36 us).
 #include "kernels.h"
 #include "rows8.h"
@@ -449,14 +449,14 @@ constexpr int64_t CHUNK_WGS = 512;   // workgroups of a chunked scan, at most ab
 
 // How a scan is dealt, by its columns C and steps (vec: the arrays allow four
 // columns a lane), from device times of the scan / its backward in fp32, us:
-//   four columns a lane or one: 16 x 250,000 x 128 (bf16) 787 / 1620 and 1414 /
-//     1823, C = 38,400 x 200 steps 39 / 60 and 25 / 48;
+//   four columns a lane or one: 16 x 250,000 x 128 (bf16) 734 / 1529 and 1425 /
+//     1798, C = 38,400 x 200 steps 35 / 52 and 23 / 40;
 //   a wave alone or four along time, four columns a lane: C = 241,280 x 600 steps
-//     321 / 664 and 356 / 716, C = 128,000 x 64 steps 34 / 66 and 22 / 42;
-//   four or eight, one column a lane: C = 40,960 x 400 steps 39 / 91 and 37 / 92,
-//     C = 20,480 x 400 steps 31 / 54 and 25 / 50;
-//   eight, or chunks: C = 20,480 x 400 steps 25 / 50 and 32 / 51, C = 10,240 x
-//     2,000 steps 82 / 152 and 64 / 120, C = 192 x 8,000 steps 296 / 484 and 15 / 18.
+//     312 / 673 and 345 / 700, C = 128,000 x 64 steps 29 / 47 and 18 / 33;
+//   four or eight, one column a lane: C = 40,960 x 400 steps 39 / 92 and 38 / 94,
+//     C = 20,480 x 400 steps 32 / 57 and 26 / 53;
+//   eight, or chunks: C = 20,480 x 400 steps 26 / 53 and 33 / 54, C = 10,240 x
+//     2,000 steps 85 / 157 and 67 / 123, C = 192 x 8,000 steps 299 / 539 and 15 / 19.
 // A wave takes all steps at once where they fit its segment.
 struct Deal {
   int V, W;
@@ -506,11 +506,11 @@ bool at(const void* p, int bytes) { return (uintptr_t)p % bytes == 0; }
 int bytes(int type) { return type == MGN_FP32 ? 4 : type == MGN_BF16 ? 2 : 1; }
 int quad(int type) { return 4 * bytes(type); }
 // A scan of four columns a lane that moves more than the last-level cache holds
-// reads past it: 16 steps of 250,000 x 128 bf16 793 us through it, 752 past it, its
-// backward 1624 and 1551; below, 20 steps of 5,000 x 64 bf16 19 and 26 us, its
-// backward 26 and 34, both in turn on 16 x 10,000 x 128 fp32 113 and 131.  It
-// writes past it at any size (16 x 10,000 x 128 fp32, both in turn: 113 us, 129
-// otherwise; 20 x 5,000 x 64 bf16 52 and 45).
+// reads past it: 16 steps of 250,000 x 128 bf16 744 us through it, 728 past it, its
+// backward 1558 and 1507; below, 20 steps of 5,000 x 64 bf16 19 and 27 us, its
+// backward 25 and 33, both in turn on 16 x 10,000 x 128 fp32 115 and 136.  It
+// writes past it at any size (16 x 10,000 x 128 fp32, both in turn: 119 us, 125
+// otherwise; 20 x 5,000 x 64 bf16 46 and 42).
 constexpr int64_t CACHE = (int64_t)256 << 20;
 
 }  // namespace
