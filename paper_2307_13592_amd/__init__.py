@@ -389,6 +389,8 @@ def _on(stream, device):
     import torch
     if stream is None:
         return contextlib.nullcontext()
+    if int(stream) == 0:  # (torch takes no handle of 0 for a stream)
+        return torch.cuda.stream(torch.cuda.default_stream(device))
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device))
 
 

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2307_13592_amd as mgn
 from parity import local_inputs
 from paper_2307_13592_amd.runner import GatedMemory, LatentCache, Normalizer, RmsNorm, Session
 from synth import meshes
@@ -39,6 +40,23 @@ def test_norm_memory_and_normalizer():
     _owned(side, *out)
     side.synchronize()
     assert [_stream_of(v) for v in (x, nz.apply(x, res)[0])] == [torch.cuda.current_stream().cuda_stream] * 2
+
+
+def test_the_default_stream_by_its_handle():
+    """stream=0 is the default stream, also while another one is current:
+    results and scratch come from there."""
+    x = torch.randn(50, 64, device="cuda")
+    g = torch.randn(3000, 1, 64, device="cuda")
+    nz, mem = RmsNorm(64), GatedMemory(1, 64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        y = nz.apply(x, x, stream=0)[0]
+        h = mem.scan(g, g, stream=0)
+        dx = nz.grad(x, y, stream=0)
+        scratch = mgn._scratch(mgn.mgn_gated_scan_work(3000, 1, 64), x.get_device(), 0)
+    assert [_stream_of(t) for t in (y, h, h.h0, dx, scratch)] == [0] * 5
+    torch.cuda.synchronize()
+    assert torch.equal(y, nz.apply(x, x)[0]) and torch.equal(dx, nz.grad(x, y))
 
 
 def test_rollout_and_loss():
