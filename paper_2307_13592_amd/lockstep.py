@@ -99,10 +99,11 @@ class Lockstep:
         parameter gradient."""
         S = self.sessions
         ds = []
-        for d in d_outs:
-            if not isinstance(d, torch.Tensor):
-                d = torch.as_tensor(np.ascontiguousarray(d, np.float32)).to(self.device)
-            ds.append(d.contiguous())
+        with _on(stream, self.device):
+            for d in d_outs:
+                if not isinstance(d, torch.Tensor):
+                    d = torch.as_tensor(np.ascontiguousarray(d, np.float32)).to(self.device)
+                ds.append(d.contiguous())
         args = ([s.model for s in S], ds, self.d_params, [s.d_halo for s in S], self.links)
         if self.grads8:
             mgn_lockstep_backward8(*args, self.packed.q, self.packed.scale, False, stream)

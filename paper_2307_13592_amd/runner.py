@@ -90,9 +90,11 @@ class Session:
         return self.out
 
     def backward(self, d_out, accumulate: bool = False, stream=None):
-        if not isinstance(d_out, torch.Tensor):
-            d_out = torch.as_tensor(np.ascontiguousarray(d_out, np.float32)).to(self.device)
-        mgn_backward(self.model, d_out.contiguous(), self.d_params, accumulate, self.d_halo, stream)
+        with _on(stream, self.device):
+            if not isinstance(d_out, torch.Tensor):
+                d_out = torch.as_tensor(np.ascontiguousarray(d_out, np.float32)).to(self.device)
+            d_out = d_out.contiguous()
+        mgn_backward(self.model, d_out, self.d_params, accumulate, self.d_halo, stream)
         return self.d_params, self.d_halo
 
     def sgd(self, lr: float, grad=None, stream=None):

@@ -7,6 +7,7 @@ import torch
 
 import paper_2307_13592_amd as mgn
 from parity import local_inputs
+from paper_2307_13592_amd import runner
 from paper_2307_13592_amd.runner import GatedMemory, LatentCache, Normalizer, RmsNorm, Session
 from synth import meshes
 
@@ -76,5 +77,31 @@ def test_rollout_and_loss():
         _owned(side, *got, *loss2)
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*want, *loss), (*got, *loss2)))
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("host", [False, True])
+def test_converted_gradients(monkeypatch, host):
+    """dL/dout that a call has to convert (an array of the host, or not
+    contiguous) is copied on the call's stream, into that stream's memory."""
+    mesh = meshes.delaunay_box(8, 7, 6, seed=3)
+    c = local_inputs(mesh, 0, 64, 2, 2, 6, part=np.zeros(mesh.n_nodes, np.int32))
+    s = Session(64, 2, 2, "fp32", c["g"], c["nf"], c["ef"], c["halo"], c["params"])
+    try:
+        d = torch.as_tensor(c["d_out"]).cuda()
+        s.forward()
+        want = s.backward(d)[0].clone()
+        wide = torch.zeros(d.shape[0], 2 * d.shape[1], device="cuda")
+        wide[:, ::2] = d
+        seen, call = [], runner.mgn_backward
+        monkeypatch.setattr(runner, "mgn_backward", lambda m, g, *a: (seen.append(g), call(m, g, *a)))
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        s.forward(side.cuda_stream)
+        got = s.backward(c["d_out"] if host else wide[:, ::2], stream=side.cuda_stream)[0]
+        _owned(side, *seen)
+        side.synchronize()
+        assert len(seen) == 1 and torch.equal(got, want)
     finally:
         s.close()
