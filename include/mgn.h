@@ -323,6 +323,132 @@ mgn_status mgn_gated_scan_grad(const void* g, int32_t g_type, const void* x, int
                                const float* dh_last, int64_t steps, int64_t rows, int32_t cols, void* dg, void* dx,
                                float* dh0, void* work, size_t work_bytes, mgn_stream stream);
 
+/* ---- layer norm of node rows, with the residual's addition ----
+ *
+ *   t = x + res;  y = (t - mean(t)) / sqrt(mean((t - mean(t))^2) + eps) * weight + bias.
+ * Arguments, types, sums and in-place forms as mgn_rms_norm; weight, bias: fp32
+ * [cols], NULL for ones and for zeros.  A finite row whose squared deviations pass
+ * the fp32 range gives its bias (and has no gradient through the norm), a NaN or an
+ * infinity in a row NaNs there. */
+mgn_status mgn_layer_norm(const void* x, const void* res, int32_t type, int64_t rows, int32_t cols, const float* weight,
+                          const float* bias, float eps, void* total, void* y, int32_t y_type, float* y_scale,
+                          mgn_stream stream);
+/* Its backward, as mgn_rms_norm_grad; dweight and dbias (fp32 [cols], NULL: not
+ * wanted) are overwritten or added to.  work: device scratch of
+ * MGN_LAYER_WORK_PER_COL * cols floats (NULL allowed without dweight and dbias). */
+#define MGN_LAYER_WORK_PER_COL 2048
+mgn_status mgn_layer_norm_grad(const void* total, int32_t type, const float* weight, float eps, const void* dy,
+                               const void* d_total, int64_t rows, int32_t cols, void* dx, float* dweight, float* dbias,
+                               int32_t accumulate, float* work, mgn_stream stream);
+
+/* ---- along time: short causal convolution ----
+ *
+ * Every column of every row takes a weighted sum of its last `width` inputs,
+ *   v_t = bias + sum_{k < width} weight[width - 1 - k] x_{t-k},
+ *   y_t = v_t, or with silu != 0 v_t sigmoid(v_t),
+ * 1 <= width <= MGN_CONV_MAX_WIDTH.  x, y [steps][rows][cols] of one storage type
+ * (MGN_FP32 or MGN_BF16); weight fp32 [cols][width] (the last entry weighs the
+ * step's own input), bias fp32 [cols] (NULL: zeros).  past [width - 1][rows][cols]
+ * of x's type holds the inputs before the first step, oldest first (NULL: zeros);
+ * past_out (NULL: not wanted) takes those that a next window's steps see.  It may
+ * be past, so that a rollout's step updates it in place.  starts [steps] (NULL:
+ * none): a nonzero entry begins a trajectory, and no step from it on sees an input
+ * before it, whatever that holds (past_out holds zeros for such).  Sums in fp32, y
+ * rounded once.  Sizes, alignment and overlaps as mgn_gated_scan. */
+#define MGN_CONV_MAX_WIDTH 8
+mgn_status mgn_causal_conv(const void* x, int32_t type, const float* weight, int32_t width, const float* bias,
+                           const uint8_t* starts, const void* past, int64_t steps, int64_t rows, int32_t cols,
+                           int32_t silu, void* y, void* past_out, mgn_stream stream);
+/* Its backward, from the forward's arguments and dy (x's type): dx (x's type),
+ * d_past (fp32 [width - 1][rows][cols], NULL: not wanted) = dL/dpast, given
+ * d_past_out (the same, NULL: zeros) = dL/dpast_out.  dweight [cols][width] and
+ * dbias [cols] (fp32, NULL: not wanted) are overwritten, or added to when accumulate
+ * != 0.  work: device scratch of MGN_CONV_PARTS * cols * (width + 1) floats (NULL
+ * allowed without dweight and dbias).  No arrays may overlap. */
+#define MGN_CONV_PARTS 1024
+mgn_status mgn_causal_conv_grad(const void* x, int32_t type, const float* weight, int32_t width, const float* bias,
+                                const uint8_t* starts, const void* past, const void* dy, const float* d_past_out,
+                                int64_t steps, int64_t rows, int32_t cols, int32_t silu, void* dx, float* dweight,
+                                float* dbias, int32_t accumulate, float* d_past, float* work, mgn_stream stream);
+
+/* ---- along time: selective state space scan ----
+ *
+ * Every column of every row carries n states, 1 <= n <= MGN_STATES_MAX, with a step
+ * size, an input and an output vector that each step brings:
+ *   delta_t = dt_t + dt_bias, with softplus != 0 log(1 + e^(dt_t + dt_bias));
+ *   h_t[k] = exp(delta_t A[k]) h_{t-1}[k] + delta_t x_t B_t[k],  h_{-1} = h0;
+ *   y_t = (sum_k C_t[k] h_t[k] + D x_t) * (z_t sigmoid(z_t)).
+ * x, dt, z (NULL: no factor) [steps][rows][cols] and B, C [steps][rows][n] (shared
+ * by a row's columns) of one storage type (MGN_FP32 or MGN_BF16); A fp32 [cols][n],
+ * D (NULL: zeros) and dt_bias (NULL: zeros) fp32 [cols]; all of them finite.  starts
+ * as mgn_gated_scan.  States are fp32 [rows][cols][n] and stay so.  A step of size 0
+ * (softplus of -infinity, say) leaves the states as they were whatever x and B hold. */
+#define MGN_STATES_MAX 64
+#define MGN_MARK_STEPS 8
+typedef struct {
+  int64_t steps, rows;
+  int32_t cols, n;
+  int32_t type;
+  int32_t softplus;
+  const void *x, *dt, *B, *C, *z;
+  const float *A, *D, *dt_bias;
+  const uint8_t* starts;
+} mgn_ssm;
+/* The scan: y as x; h_last (NULL: not wanted) the last states, which may stand on
+ * h0 (NULL: zeros), so that a rollout's step updates its states in place (with no
+ * steps it is h0).  marks (NULL: not wanted; what the backward needs)
+ * [ceil(steps / MGN_MARK_STEPS)][rows][cols][n]: the states before every
+ * MGN_MARK_STEPS-th step.  work: device scratch of mgn_selective_scan_work bytes,
+ * 16-byte aligned (NULL when that is 0); MGN_E_NOMEM when work_bytes is less.
+ * Sizes, alignment and overlaps as mgn_gated_scan. */
+mgn_status mgn_selective_scan_work(int64_t steps, int64_t rows, int32_t cols, int32_t n, size_t* bytes);
+mgn_status mgn_selective_scan(const mgn_ssm* s, const float* h0, void* y, float* h_last, float* marks, void* work,
+                              size_t work_bytes, mgn_stream stream);
+/* Its backward, from the forward's arguments, its marks, dy (x's type) and dh_last
+ * (fp32 [rows][cols][n] = dL/dh_last, NULL: zeros): dx, ddt, dB, dC and (with z) dz
+ * in x's type; dA, dD and d_bias fp32, each NULL if not wanted, overwritten or added
+ * to when accumulate != 0; dh0 (NULL: not wanted; it may be dh_last) = dL/dh0.
+ * A step of size 0 gives x and B no gradient, nor dt where its softplus is level. */
+typedef struct {
+  void *dx, *ddt, *dB, *dC, *dz;
+  float *dA, *dD, *d_bias;
+  int32_t accumulate;
+} mgn_ssm_grads;
+mgn_status mgn_selective_scan_grad_work(int64_t steps, int64_t rows, int32_t cols, int32_t n, size_t* bytes);
+mgn_status mgn_selective_scan_grad(const mgn_ssm* s, const float* marks, const void* dy, const float* dh_last,
+                                   const mgn_ssm_grads* grads, float* dh0, void* work, size_t work_bytes,
+                                   mgn_stream stream);
+
+/* ---- global gradient norm and clipping ----
+ *
+ * norm = sqrt of the sum of g^2 over all elements of many tensors, and
+ * out = g * min(1, max_norm / norm) for each of them: what an update wants between
+ * the backward and mgn_sgd_step.  A list is made once for a program's tensors (it
+ * holds their addresses and lengths, in host memory; the tensors stay the caller's
+ * and must live as long as the list is used).  Lengths may be 0; grad and out (grad
+ * itself, or NULL, to scale in place) have the type MGN_FP32 or MGN_BF16 and need
+ * its alignment.  MGN_E_ARG for tensors of which one is written and overlaps
+ * another, unless out is grad. */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int32_t type;
+} mgn_grad;
+typedef struct mgn_grads mgn_grads;
+mgn_status mgn_grads_create(const mgn_grad* tensors, int64_t count, mgn_grads** out);
+void mgn_grads_destroy(mgn_grads* list);
+/* Bytes of device scratch that the calls below need (16-byte aligned). */
+mgn_status mgn_grads_work(const mgn_grads* list, size_t* bytes);
+/* norm[0] (device fp32) = the norm; squares and sums are taken in fp64. */
+mgn_status mgn_grad_norm(const mgn_grads* list, float* norm, void* work, size_t work_bytes, mgn_stream stream);
+/* Scales to max_norm (positive and finite).  given == 0: norm[0] takes the tensors'
+ * own norm; else it is read: that of all the parts of a job, say.  A norm that is NaN
+ * or infinite scales nothing.  Tensors that are not scaled are copied to their
+ * out. */
+mgn_status mgn_grad_clip(const mgn_grads* list, float max_norm, int32_t given, float* norm, void* work,
+                         size_t work_bytes, mgn_stream stream);
+
 /* Device workspace mgn_forward/mgn_backward need for graph g (bytes) under
  * the model's checkpointing setting.  For a forward-only fp32 plan with a halo
  * this includes 4 * latent bytes per halo node that mgn_forward can do without

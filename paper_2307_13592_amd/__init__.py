@@ -33,7 +33,10 @@ EXPORTS = ["mgn_create", "mgn_destroy", "mgn_last_error", "mgn_param_count", "mg
            "mgn_mse_grad_global", "mgn_timing_enable", "mgn_timing_read", "mgn_forward_noalloc",
            "mgn_rows_store8", "mgn_rows_load8", "mgn_rms_norm", "mgn_rms_norm_grad", "mgn_gated_scan_work",
            "mgn_gated_scan", "mgn_gated_scan_grad", "mgn_pack_latents8", "mgn_add_latent_grads8",
-           "mgn_lockstep_forward8", "mgn_lockstep_backward8"]
+           "mgn_lockstep_forward8", "mgn_lockstep_backward8",
+           "mgn_layer_norm", "mgn_layer_norm_grad", "mgn_causal_conv", "mgn_causal_conv_grad",
+           "mgn_selective_scan_work", "mgn_selective_scan", "mgn_selective_scan_grad_work", "mgn_selective_scan_grad",
+           "mgn_grads_create", "mgn_grads_destroy", "mgn_grads_work", "mgn_grad_norm", "mgn_grad_clip"]
 TIMERS = ["encode", "edge_fwd", "node_fwd", "decode", "edge_bwd", "node_bwd", "input_grad", "weight_grad",
           "other", "node_proj", "exchange"]
 
@@ -60,6 +63,23 @@ class mgn_graph(C.Structure):
                 ("send", C.c_void_p), ("trow_ptr", C.c_void_p), ("tedge", C.c_void_p)]
 
 
+class mgn_ssm(C.Structure):
+    _fields_ = [("steps", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int32), ("n", C.c_int32), ("type", C.c_int32),
+                ("softplus", C.c_int32), ("x", C.c_void_p), ("dt", C.c_void_p), ("B", C.c_void_p), ("C", C.c_void_p),
+                ("z", C.c_void_p), ("A", C.c_void_p), ("D", C.c_void_p), ("dt_bias", C.c_void_p),
+                ("starts", C.c_void_p)]
+
+
+class mgn_ssm_grads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("ddt", C.c_void_p), ("dB", C.c_void_p), ("dC", C.c_void_p), ("dz", C.c_void_p),
+                ("dA", C.c_void_p), ("dD", C.c_void_p), ("d_bias", C.c_void_p), ("accumulate", C.c_int32)]
+
+
+class mgn_grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
+
+
+_byref = C.byref  # (C is also a name of the selective scan's)
 _lib = None
 
 
@@ -117,6 +137,20 @@ def lib() -> C.CDLL:
             "mgn_pack_latents8": (C.c_int, [vp, vp, i64, vp, vp, i32, vp]),
             "mgn_add_latent_grads8": (C.c_int, [vp, vp, vp, i32, vp, i64, vp]),
             "mgn_lockstep_forward8": (C.c_int, [i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i64, i32, vp]),
+            "mgn_layer_norm": (C.c_int, [vp, vp, i32, i64, i32, vp, vp, C.c_float, vp, vp, i32, vp, vp]),
+            "mgn_layer_norm_grad": (C.c_int, [vp, i32, vp, C.c_float, vp, vp, i64, i32, vp, vp, vp, i32, vp, vp]),
+            "mgn_causal_conv": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, i64, i64, i32, i32, vp, vp, vp]),
+            "mgn_causal_conv_grad": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, vp, i64, i64, i32, i32, vp, vp, vp, i32,
+                                               vp, vp, vp]),
+            "mgn_selective_scan_work": (C.c_int, [i64, i64, i32, i32, vp]),
+            "mgn_selective_scan": (C.c_int, [vp, vp, vp, vp, vp, vp, C.c_size_t, vp]),
+            "mgn_selective_scan_grad_work": (C.c_int, [i64, i64, i32, i32, vp]),
+            "mgn_selective_scan_grad": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]),
+            "mgn_grads_create": (C.c_int, [vp, i64, vp]),
+            "mgn_grads_destroy": (None, [vp]),
+            "mgn_grads_work": (C.c_int, [vp, vp]),
+            "mgn_grad_norm": (C.c_int, [vp, vp, vp, C.c_size_t, vp]),
+            "mgn_grad_clip": (C.c_int, [vp, C.c_float, i32, vp, vp, C.c_size_t, vp]),
             "mgn_lockstep_backward8": (C.c_int, [i32, vp, vp, vp, C.c_int, vp, vp, i32, vp, vp, i64, i32, vp]),
             "mgn_mse_grad": (C.c_int, [vp, vp, vp, i64, i32, vp, vp, vp]),
             "mgn_mse_grad_global": (C.c_int, [vp, vp, vp, i64, i32, i64, vp, vp, vp]),
@@ -537,6 +571,253 @@ def mgn_gated_scan_grad(g, x, h, dg, dx, dh=None, dh_last=None, dh0=None, h0=Non
          _arr(dh, "dh", f32, shape, dev), _arr(dh_last, "dh_last", f32, one, dev), T, rows, cols,
          _need(_arr(dg, "dg", dt, shape, dev), "dg"), _need(_arr(dx, "dx", dt, shape, dev), "dx"),
          _arr(dh0, "dh0", f32, one, dev), *tail)
+
+
+MGN_LAYER_WORK_PER_COL = 2048
+MGN_CONV_MAX_WIDTH, MGN_CONV_PARTS = 8, 1024
+MGN_STATES_MAX, MGN_MARK_STEPS = 64, 8
+
+
+def _given(work, name: str, nbytes: int, dev: int, stream):
+    """Pointer and bytes of a call's scratch, and the tensor that holds it: the
+    caller's, or one of nbytes."""
+    if work is None:
+        work = _scratch(nbytes, dev, stream) if nbytes else None
+        return (work.data_ptr() if nbytes else None), nbytes, work
+    p = _dev(work)
+    if work.get_device() != dev:
+        raise ValueError(f"{name}: expected a tensor on GPU {dev}, got one on {work.device}")
+    return p, work.numel() * work.element_size(), work
+
+
+def mgn_layer_norm(x, weight, bias, y, res=None, total=None, y_scale=None, eps: float = 1e-5, stream=None) -> None:
+    """y = (t - mean(t)) / sqrt(var(t) + eps) * weight + bias for t = x + res, rows
+    of device tensors.  x, res, total: float32 or bfloat16, one type; total takes t.
+    y: float32, bfloat16, or uint8 for 8-bit rows with their scales in y_scale.
+    weight, bias: float32 [cols] or None."""
+    import torch
+    shape = rows, cols = _shape(x, "x")
+    dev, dt, f32 = x.get_device(), x.dtype, torch.float32
+    yt = _type(y, "y", e4m3=True)
+    _run("mgn_layer_norm", dev, stream, _arr(x, "x", dt, shape, dev), _arr(res, "res", dt, shape, dev), _type(x, "x"),
+         rows, cols, _arr(weight, "weight", f32, (cols,), dev), _arr(bias, "bias", f32, (cols,), dev), eps,
+         _arr(total, "total", dt, shape, dev), _arr(y, "y", y.dtype, shape, dev), yt,
+         None if y_scale is None else _arr(y_scale, "y_scale", f32, (rows, rows8_blocks(cols)), dev))
+
+
+def mgn_layer_norm_grad(total, weight, dy, dx, dweight=None, dbias=None, d_total=None, accumulate: bool = False,
+                        work=None, eps: float = 1e-5, stream=None) -> None:
+    """Backward of mgn_layer_norm: dx (the gradient of x and of res), dweight and
+    dbias (float32 [cols], overwritten or added to) from the normalised sum `total`,
+    dy and the gradient d_total that reaches the sum otherwise.  work: float32
+    scratch of MGN_LAYER_WORK_PER_COL * cols for dweight and dbias (None:
+    allocated)."""
+    import torch
+    shape = rows, cols = _shape(total, "total")
+    dev, dt, f32 = total.get_device(), total.dtype, torch.float32
+    pt = _arr(total, "total", dt, shape, dev)
+    sums = dweight is not None or dbias is not None
+    if work is not None:
+        _devt(work, f32, "work", min_numel=MGN_LAYER_WORK_PER_COL * cols)
+    pw, _, keep = _given(work, "work", 4 * MGN_LAYER_WORK_PER_COL * cols if sums else 0, dev, stream)
+    _run("mgn_layer_norm_grad", dev, stream, pt, _type(total, "total"), _arr(weight, "weight", f32, (cols,), dev), eps,
+         _need(_arr(dy, "dy", dt, shape, dev), "dy"), _arr(d_total, "d_total", dt, shape, dev), rows, cols,
+         _need(_arr(dx, "dx", dt, shape, dev), "dx"), _arr(dweight, "dweight", f32, (cols,), dev),
+         _arr(dbias, "dbias", f32, (cols,), dev), 1 if accumulate else 0, pw)
+
+
+def _conv_args(x, weight, bias, past, starts):
+    """Marshalled arguments the convolution and its backward share."""
+    import torch
+    shape = T, rows, cols = _shape(x, "x", 3)
+    dev, f32 = x.get_device(), torch.float32
+    if weight is None or weight.dim() != 2:
+        raise ValueError("weight: expected [cols][width]")
+    width = weight.shape[1]
+    if not 1 <= width <= MGN_CONV_MAX_WIDTH:
+        raise ValueError(f"weight: expected 1 .. {MGN_CONV_MAX_WIDTH} weights a column")
+    before = (width - 1, rows, cols)
+    return shape, dev, width, before, (
+        _arr(x, "x", x.dtype, shape, dev), _type(x, "x"), _arr(weight, "weight", f32, (cols, width), dev), width,
+        _arr(bias, "bias", f32, (cols,), dev), None if starts is None else _arr(starts, "starts", torch.uint8, (T,), dev),
+        _arr(past, "past", x.dtype, before, dev))
+
+
+def mgn_causal_conv(x, weight, y, bias=None, past=None, past_out=None, starts=None, silu: bool = False,
+                    stream=None) -> None:
+    """v_t = bias + sum_k weight[:, width - 1 - k] x_{t-k} along the first axis of
+    device tensors [steps][rows][cols], y = v or (silu) v sigmoid(v).  x, y: float32
+    or bfloat16; weight: float32 [cols][width]; bias: float32 [cols] or None; past,
+    past_out [width - 1][rows][cols] of x's type: the inputs before the first step
+    and those that the next window's steps see (past_out may be past), either None;
+    starts: uint8 [steps]."""
+    shape, dev, width, before, head = _conv_args(x, weight, bias, past, starts)
+    T, rows, cols = shape
+    _run("mgn_causal_conv", dev, stream, *head, T, rows, cols, 1 if silu else 0,
+         _need(_arr(y, "y", x.dtype, shape, dev), "y"), _arr(past_out, "past_out", x.dtype, before, dev))
+
+
+def mgn_causal_conv_grad(x, weight, dy, dx, dweight=None, dbias=None, bias=None, past=None, d_past=None,
+                         d_past_out=None, starts=None, silu: bool = False, accumulate: bool = False, work=None,
+                         stream=None) -> None:
+    """Backward of mgn_causal_conv from its arguments, dy and d_past_out (float32
+    [width - 1][rows][cols], or None): dx (x's type), dweight, dbias (float32,
+    overwritten or added to) and d_past (float32), each of them or None.  work:
+    float32 scratch of MGN_CONV_PARTS * cols * (width + 1) for dweight and dbias
+    (None: allocated)."""
+    import torch
+    shape, dev, width, before, head = _conv_args(x, weight, bias, past, starts)
+    T, rows, cols = shape
+    f32, floats = torch.float32, MGN_CONV_PARTS * cols * (width + 1)
+    sums = dweight is not None or dbias is not None
+    if work is not None:
+        _devt(work, f32, "work", min_numel=floats)
+    pw, _, keep = _given(work, "work", 4 * floats if sums else 0, dev, stream)
+    _run("mgn_causal_conv_grad", dev, stream, *head, _need(_arr(dy, "dy", x.dtype, shape, dev), "dy"),
+         _arr(d_past_out, "d_past_out", f32, before, dev), T, rows, cols, 1 if silu else 0,
+         _need(_arr(dx, "dx", x.dtype, shape, dev), "dx"), _arr(dweight, "dweight", f32, (cols, width), dev),
+         _arr(dbias, "dbias", f32, (cols,), dev), 1 if accumulate else 0, _arr(d_past, "d_past", f32, before, dev), pw)
+
+
+@functools.lru_cache(maxsize=256)
+def mgn_selective_scan_work(steps: int, rows: int, cols: int, n: int) -> int:
+    """Bytes of device scratch mgn_selective_scan needs."""
+    b = C.c_size_t()
+    _check(lib().mgn_selective_scan_work(int(steps), int(rows), int(cols), int(n), C.byref(b)))
+    return int(b.value)
+
+
+@functools.lru_cache(maxsize=256)
+def mgn_selective_scan_grad_work(steps: int, rows: int, cols: int, n: int) -> int:
+    """Bytes of device scratch mgn_selective_scan_grad needs."""
+    b = C.c_size_t()
+    _check(lib().mgn_selective_scan_grad_work(int(steps), int(rows), int(cols), int(n), C.byref(b)))
+    return int(b.value)
+
+
+def _ssm_args(x, dt, A, B, C_, D, dt_bias, z, starts, softplus):
+    """The scan's shape, device and argument record."""
+    import torch
+    shape = T, rows, cols = _shape(x, "x", 3)
+    dev, ty, f32 = x.get_device(), x.dtype, torch.float32
+    if A is None or A.dim() != 2 or not 1 <= A.shape[1] <= MGN_STATES_MAX:
+        raise ValueError(f"A: expected [cols][n], 1 <= n <= {MGN_STATES_MAX}")
+    n = A.shape[1]
+    return shape, dev, n, mgn_ssm(
+        T, rows, cols, n, _type(x, "x"), 1 if softplus else 0, _arr(x, "x", ty, shape, dev),
+        _need(_arr(dt, "dt", ty, shape, dev), "dt"), _need(_arr(B, "B", ty, (T, rows, n), dev), "B"),
+        _need(_arr(C_, "C", ty, (T, rows, n), dev), "C"), _arr(z, "z", ty, shape, dev), _arr(A, "A", f32, (cols, n), dev),
+        _arr(D, "D", f32, (cols,), dev), _arr(dt_bias, "dt_bias", f32, (cols,), dev),
+        None if starts is None else _arr(starts, "starts", torch.uint8, (T,), dev))
+
+
+def mgn_selective_marks(x, A, stream=None):
+    """The array that mgn_selective_scan leaves its states in for the backward:
+    float32 [ceil(steps / MGN_MARK_STEPS)][rows][cols][n]."""
+    import torch
+    T, rows, cols = _shape(x, "x", 3)
+    with _on(stream, x.device):
+        return torch.empty((-(-T // MGN_MARK_STEPS), rows, cols, A.shape[1]), dtype=torch.float32, device=x.device)
+
+
+def mgn_selective_scan(x, dt, A, B, C, y, D=None, dt_bias=None, z=None, h0=None, h_last=None, marks=None, starts=None,
+                       softplus: bool = False, work=None, stream=None) -> None:
+    """The selective scan along the first axis of device tensors [steps][rows][cols]:
+      h_t = exp(delta A) h_{t-1} + delta x B_t,  delta = dt + dt_bias (softplus: its
+      softplus),  y = (sum over the states of C_t h_t + D x) z sigmoid(z).
+    x, dt, z (or None), y and B, C [steps][rows][n]: float32 or bfloat16, one type; A
+    float32 [cols][n]; D, dt_bias float32 [cols] or None; h0, h_last (it may be h0)
+    float32 [rows][cols][n] or None; marks of mgn_selective_marks, for the backward;
+    starts: uint8 [steps].  work: device scratch of mgn_selective_scan_work bytes
+    (None: allocated)."""
+    import torch
+    shape, dev, n, s = _ssm_args(x, dt, A, B, C, D, dt_bias, z, starts, softplus)
+    T, rows, cols = shape
+    f32, state = torch.float32, (rows, cols, n)
+    pw, nb, keep = _given(work, "work", mgn_selective_scan_work(T, rows, cols, n) if work is None else 0, dev, stream)
+    _run("mgn_selective_scan", dev, stream, _byref(s), _arr(h0, "h0", f32, state, dev),
+         _need(_arr(y, "y", x.dtype, shape, dev), "y"), _arr(h_last, "h_last", f32, state, dev),
+         _arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), pw, nb)
+
+
+def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=None, d_bias=None, dz=None, D=None,
+                            dt_bias=None, z=None, dh_last=None, dh0=None, starts=None, softplus: bool = False,
+                            accumulate: bool = False, work=None, stream=None) -> None:
+    """Backward of mgn_selective_scan from its arguments, its marks, dy and dh_last
+    (float32 [rows][cols][n], or None): dx, ddt, dB, dC and (with z) dz in x's type;
+    dA, dD, d_bias (float32, overwritten or added to, each of them or None); dh0
+    (float32, or None; it may be dh_last).  work: device scratch of
+    mgn_selective_scan_grad_work bytes (None: allocated)."""
+    import torch
+    shape, dev, n, s = _ssm_args(x, dt, A, B, C, D, dt_bias, z, starts, softplus)
+    T, rows, cols = shape
+    f32, ty, state, pair = torch.float32, x.dtype, (rows, cols, n), (T, rows, n)
+    g = mgn_ssm_grads(_need(_arr(dx, "dx", ty, shape, dev), "dx"), _need(_arr(ddt, "ddt", ty, shape, dev), "ddt"),
+                      _need(_arr(dB, "dB", ty, pair, dev), "dB"), _need(_arr(dC, "dC", ty, pair, dev), "dC"),
+                      _arr(dz, "dz", ty, shape, dev), _arr(dA, "dA", f32, (cols, n), dev),
+                      _arr(dD, "dD", f32, (cols,), dev), _arr(d_bias, "d_bias", f32, (cols,), dev),
+                      1 if accumulate else 0)
+    pw, nb, keep = _given(work, "work", mgn_selective_scan_grad_work(T, rows, cols, n) if work is None else 0, dev,
+                          stream)
+    _run("mgn_selective_scan_grad", dev, stream, _byref(s),
+         _need(_arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), "marks"),
+         _need(_arr(dy, "dy", ty, shape, dev), "dy"), _arr(dh_last, "dh_last", f32, state, dev), _byref(g),
+         _arr(dh0, "dh0", f32, state, dev), pw, nb)
+
+
+class mgn_grad_list:
+    """Device tensors (float32 or bfloat16, contiguous, on one GPU) whose global norm
+    mgn_grad_norm and mgn_grad_clip take; outs: where the clipped ones go (None: in
+    place).  The list holds the tensors; it is made once for a program's gradients."""
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = [None] * len(grads) if outs is None else list(outs)
+        if len(outs) != len(grads):
+            raise ValueError("outs: expected one for each of grads")
+        self._list = None
+        self.tensors, self.dev = (grads, outs), grads[0].get_device() if grads else -1
+        rec = (mgn_grad * max(len(grads), 1))()
+        for k, (g, o) in enumerate(zip(grads, outs)):
+            ty = _type(g, f"grads[{k}]")
+            rec[k] = mgn_grad(_arr(g, f"grads[{k}]", g.dtype, g.shape, self.dev),
+                              _arr(o, f"outs[{k}]", g.dtype, g.shape, self.dev), g.numel(), ty)
+        p = C.c_void_p()
+        _check(lib().mgn_grads_create(rec, len(grads), C.byref(p)))
+        self._list = p
+        n = C.c_size_t()
+        _check(lib().mgn_grads_work(p, C.byref(n)))
+        self.work_bytes = int(n.value)
+
+    def __del__(self):
+        if getattr(self, "_list", None):
+            lib().mgn_grads_destroy(self._list)
+            self._list = None
+
+
+def _grads(grads, norm, work, stream):
+    import torch
+    keep = grads = grads if isinstance(grads, mgn_grad_list) else mgn_grad_list(grads)
+    dev = grads.dev if grads.dev >= 0 else norm.get_device()
+    pn = _need(_arr(norm, "norm", torch.float32, (1,), dev), "norm")
+    pw, nb, scratch = _given(work, "work", grads.work_bytes if work is None else 0, dev, stream)
+    return dev, grads._list, pn, (pw, nb), (keep, scratch)
+
+
+def mgn_grad_norm(grads, norm, work=None, stream=None) -> None:
+    """norm (float32 [1], device) = sqrt of the sum of squares over all elements of
+    grads, an mgn_grad_list or a sequence of tensors.  work: device scratch of the
+    list's work_bytes (None: allocated)."""
+    dev, p, pn, tail, keep = _grads(grads, norm, work, stream)
+    _run("mgn_grad_norm", dev, stream, p, pn, *tail)
+
+
+def mgn_grad_clip(grads, max_norm: float, norm, given: bool = False, work=None, stream=None) -> None:
+    """Scales grads (an mgn_grad_list, into its outs; or a sequence of tensors, in
+    place) by min(1, max_norm / norm); norm (float32 [1], device) takes the tensors'
+    own or, given, is read."""
+    dev, p, pn, tail, keep = _grads(grads, norm, work, stream)
+    _run("mgn_grad_clip", dev, stream, p, float(max_norm), 1 if given else 0, pn, *tail)
 
 
 def mgn_workspace_size(model, graph: mgn_graph) -> int:

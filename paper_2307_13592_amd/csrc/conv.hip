@@ -1,0 +1,435 @@
+// Short causal convolution along time, each column with its own taps (gfx950):
+//   v_t = b + sum_k w[W - 1 - k] x_{t-k},  y_t = v_t or v_t sigmoid(v_t),
+// over the W - 1 steps before t that belong to its trajectory, and its backward
+//   d_t = dy_t act'(v_t),  dx_t = sum_k w[W - 1 - k] d_{t+k},
+//   dw[W - 1 - k] = sum d_t x_{t-k},  db = sum d_t.
+//
+// A lane holds V neighbouring columns of a row and goes through time with the last
+// W - 1 inputs in registers, STEPS steps' loads in flight together, so that each
+// input is read once.  A workgroup takes as many rows as it has lanes for and, with
+// many rows, all steps of them; with fewer the time axis is cut into segments,
+// which read the W - 1 steps around them again (the neighbours', from the caches).
+// The backward adds w d_t to the gradients of the W inputs that step t saw, and
+// passes on the oldest: it needs each d once, and the pre-activation is formed
+// again from the inputs that it holds.
+#include <type_traits>
+
+#include "kernels.h"
+#include "rows8.h"
+
+namespace mgn {
+namespace {
+
+constexpr int NT = 256, MAX_W = MGN_CONV_MAX_WIDTH;
+
+// V neighbouring elements; V = 1, or a run of 4 or 8 on its own boundary.
+template <int TYPE, int V>
+__device__ __forceinline__ void load(const void* p, int64_t i, float (&v)[V]) {
+  get<V>((const Elem<TYPE>*)p + i, v);
+}
+template <int TYPE, int V>
+__device__ __forceinline__ void store(void* p, int64_t i, const float (&v)[V]) {
+  put<V>((Elem<TYPE>*)p + i, v);
+}
+
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+// A thread's place: its columns from c on, and its rows r, r + rows_wg * gridDim.x, ...
+template <int V>
+struct Place {
+  int c, r, per;  // per: rows of a workgroup
+  bool ok;
+  __device__ __forceinline__ explicit Place(const ConvArgs& a) {
+    per = NT / a.lanes;
+    r = threadIdx.x / a.lanes;
+    c = ((int)blockIdx.y * a.lanes + threadIdx.x % a.lanes) * V;
+    ok = r < per && c < a.cols;
+  }
+};
+
+// Steps since the last start at or before step t, at most W: how far back step t
+// + 1's predecessors go.
+template <int W>
+__device__ __forceinline__ int age_at(const uint8_t* starts, int64_t t) {
+  int n = W;
+  if (starts)
+    for (int k = W - 1; k >= 0; --k)
+      if (t - k >= 0 && starts[t - k]) n = k;
+  return n;
+}
+
+template <int W, int V>
+__device__ __forceinline__ void load_taps(const ConvArgs& a, int c, bool ok, float (&w)[W][V], float (&b)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) b[k] = a.b && ok ? a.b[c + k] : 0.f;
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+#pragma unroll
+    for (int k = 0; k < V; ++k) w[j][k] = ok ? a.w[(int64_t)(c + k) * W + j] : 0.f;
+}
+
+// Inputs t0 - (W - 1) .. t0 - 1 of a row, oldest first.
+template <int TYPE, int W, int V>
+__device__ __forceinline__ void load_before(const ConvArgs& a, int64_t t0, int64_t C, int64_t i, bool ok, float (*xs)[V]) {
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) {
+    const int64_t t = t0 - (W - 1) + j;
+#pragma unroll
+    for (int k = 0; k < V; ++k) xs[j][k] = 0.f;
+    if (ok && t >= 0) load<TYPE, V>(a.x, t * C + i, xs[j]);
+    else if (ok && a.past) load<TYPE, V>(a.past, (t + W - 1) * C + i, xs[j]);
+  }
+}
+
+// The weighted inputs of the step whose own input is xs[W - 1]; of those before it
+// the last `age` count, the others are left out whatever they are.
+template <int W, int V>
+__device__ __forceinline__ void taps(const float (*xs)[V], const float (&w)[W][V], const float (&b)[V], int age, float (&v)[V]) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = b[k];
+  if (age >= W - 1) {
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = fmaf(w[j][k], xs[j][k], v[k]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (W - 1 - j <= age)
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = fmaf(w[j][k], xs[j][k], v[k]);
+  }
+}
+
+template <int TYPE, int W, int V, int STEPS>
+__global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
+  const Place<V> p(a);
+  const int64_t C = a.rows * a.cols;
+  float w[W][V], b[V];
+  load_taps<W, V>(a, p.c, p.ok, w, b);
+  for (int64_t item = blockIdx.x; item < a.groups * a.segs; item += gridDim.x) {
+    const int64_t s = item / a.groups, r = (item - s * a.groups) * p.per + p.r;
+    const int64_t t0 = s * a.seg, t1 = s + 1 == a.segs ? a.steps : t0 + a.seg;
+    const bool ok = p.ok && r < a.rows;
+    const int64_t i = ok ? r * a.cols + p.c : 0;
+    float xs[W - 1 + STEPS][V];
+    load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
+    int age = age_at<W>(a.starts, t0 - 1);
+    for (int64_t t = t0; t < t1; t += STEPS) {
+      bool fresh[STEPS];
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) {
+        fresh[e] = a.starts && t + e < t1 && a.starts[t + e];
+#pragma unroll
+        for (int k = 0; k < V; ++k) xs[W - 1 + e][k] = 0.f;
+        if (ok && t + e < t1) load<TYPE, V>(a.x, (t + e) * C + i, xs[W - 1 + e]);
+      }
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) {
+        if (t + e >= t1) break;
+        age = fresh[e] ? 0 : age < W ? age + 1 : W;
+        float v[V];
+        taps<W, V>(xs + e, w, b, age, v);
+        if (a.silu) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) v[k] *= sigmoid(v[k]);
+        }
+        if (ok) store<TYPE, V>(a.y, (t + e) * C + i, v);
+      }
+      const int n = t1 - t < STEPS ? (int)(t1 - t) : STEPS;  // the last W - 1 inputs to the front
+      if (n == STEPS) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+          for (int k = 0; k < V; ++k) xs[j][k] = xs[STEPS + j][k];
+      } else {
+#pragma unroll
+        for (int e = 1; e < STEPS; ++e)
+          if (e == n)
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+              for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k];
+      }
+    }
+    if (a.past_out && ok && s + 1 == a.segs) {
+      // what the next window's steps see: nothing from before the last start
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) {
+        float v[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = W - 2 - j <= age ? xs[j][k] : 0.f;
+        store<TYPE, V>(a.past_out, j * C + i, v);
+      }
+    }
+  }
+}
+
+// The backward; a.y is dx.  A thread's sums of dw and db go over all its items, in
+// fp32 over STEPS steps and in fp64 over these.
+template <int TYPE, int W, int V, int STEPS>
+__global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
+  const Place<V> p(a);
+  const int64_t C = a.rows * a.cols;
+  float w[W][V], b[V];
+  load_taps<W, V>(a, p.c, p.ok, w, b);
+  double dw[W][V], db[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    db[k] = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j][k] = 0;
+  }
+  for (int64_t item = blockIdx.x; item < a.groups * a.segs; item += gridDim.x) {
+    const int64_t s = item / a.groups, r = (item - s * a.groups) * p.per + p.r;
+    const int64_t t0 = s * a.seg, t1 = s + 1 == a.segs ? a.steps : t0 + a.seg;
+    const int64_t te = s + 1 == a.segs ? t1 : t1 + (W - 1);  // the next segment's steps that saw this one's inputs
+    const bool ok = p.ok && r < a.rows;
+    const int64_t i = ok ? r * a.cols + p.c : 0;
+    float xs[W - 1 + STEPS][V], g[W - 1 + STEPS][V];  // g[j]: gradient of the input of xs[j]
+    load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) g[j][k] = 0.f;
+    int age = age_at<W>(a.starts, t0 - 1);
+    // the gradient of input t, complete
+    const auto out = [&](int64_t t, const float (&v)[V]) {
+      if (!ok || t >= t1) return;
+      if (t >= t0) store<TYPE, V>(a.y, t * C + i, v);
+      else if (t < 0 && a.d_past) store<MGN_FP32, V>(a.d_past, (t + W - 1) * C + i, v);
+    };
+    for (int64_t t = t0; t < te; t += STEPS) {
+      float d[STEPS][V];
+      bool fresh[STEPS];
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) {
+        fresh[e] = a.starts && t + e < te && a.starts[t + e];
+#pragma unroll
+        for (int k = 0; k < V; ++k) xs[W - 1 + e][k] = d[e][k] = g[W - 1 + e][k] = 0.f;
+        if (ok && t + e < te) {
+          load<TYPE, V>(a.x, (t + e) * C + i, xs[W - 1 + e]);
+          load<TYPE, V>(a.dy, (t + e) * C + i, d[e]);
+        }
+      }
+      float sw[W][V], sb[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        sb[k] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) sw[j][k] = 0.f;
+      }
+      const int n = te - t < STEPS ? (int)(te - t) : STEPS;
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) {
+        if (e >= n) break;
+        age = fresh[e] ? 0 : age < W ? age + 1 : W;
+        if (a.silu) {
+          float v[V];
+          taps<W, V>(xs + e, w, b, age, v);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float f = sigmoid(v[k]);
+            d[e][k] *= f * fmaf(v[k], 1.f - f, 1.f);
+          }
+        }
+        const bool mine = t + e < t1;
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+          if (W - 1 - j <= age)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+              g[e + j][k] = fmaf(w[j][k], d[e][k], g[e + j][k]);
+              if (mine) sw[j][k] = fmaf(d[e][k], xs[e + j][k], sw[j][k]);
+            }
+        if (mine)
+#pragma unroll
+          for (int k = 0; k < V; ++k) sb[k] += d[e][k];
+        out(t + e - (W - 1), g[e]);
+      }
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        db[k] += sb[k];
+#pragma unroll
+        for (int j = 0; j < W; ++j) dw[j][k] += sw[j][k];
+      }
+#pragma unroll
+      for (int e = 1; e <= STEPS; ++e)
+        if (e == n)
+#pragma unroll
+          for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+            for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k], g[j][k] = g[e + j][k];
+    }
+    if (s + 1 == a.segs) {
+      // the inputs that steps after the last one see
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) {
+        if (a.d_past_out && ok && W - 2 - j <= age) {
+          float v[V];
+          load<MGN_FP32, V>(a.d_past_out, j * C + i, v);
+#pragma unroll
+          for (int k = 0; k < V; ++k) g[j][k] += v[k];
+        }
+        out(t1 - (W - 1) + j, g[j]);
+      }
+    }
+  }
+  if (!a.part) return;
+  // the workgroup's rows, one behind the other, in fp64
+  __shared__ double lds[NT];
+  const int64_t width = (int64_t)a.cols * (W + 1);
+  float* const dst = a.part + blockIdx.x * width;
+  const auto total = [&](double v, int64_t at) {
+    lds[threadIdx.x] = p.ok ? v : 0;
+    __syncthreads();
+    if (p.ok && p.r == 0) {
+      for (int e = 1; e < p.per; ++e) v += lds[e * a.lanes + threadIdx.x];
+      dst[at] = (float)v;
+    }
+    __syncthreads();
+  };
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) total(dw[j][k], (int64_t)(p.c + k) * W + j);
+    total(db[k], (int64_t)a.cols * W + p.c + k);
+  }
+}
+
+// past_out where no steps come: past, or zeros.
+__global__ __launch_bounds__(NT) void past_copy_kernel(const uint8_t* in, uint8_t* out, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < n; i += (int64_t)gridDim.x * NT) out[i] = in ? in[i] : 0;
+}
+hipError_t copy_bytes(const void* in, void* out, int64_t n, hipStream_t st) {
+  if (n <= 0) return hipSuccess;
+  const int64_t b = (n + NT - 1) / NT;
+  hipLaunchKernelGGL(past_copy_kernel, dim3((unsigned)(b < 8192 ? b : 8192)), dim3(NT), 0, st, (const uint8_t*)in, (uint8_t*)out, n);
+  return hipGetLastError();
+}
+// past_out from the last W - 1 of `steps` inputs, where it lies on the array that
+// the first segment reads.
+template <int TYPE>
+__global__ __launch_bounds__(NT) void past_tail_kernel(ConvArgs a, int W) {
+  const int64_t C = a.rows * a.cols, n = (W - 1) * C;
+  int age = MAX_W;
+  if (a.starts)
+    for (int k = W - 2; k >= 0; --k)
+      if (a.starts[a.steps - 1 - k]) age = k;
+  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < n; i += (int64_t)gridDim.x * NT) {
+    const int64_t j = i / C;
+    Elem<TYPE> v = 0;
+    if (W - 2 - j <= age) v = ((const Elem<TYPE>*)a.x)[(a.steps - (W - 1)) * C + i];
+    ((Elem<TYPE>*)a.past_out)[i] = v;
+  }
+}
+
+constexpr int64_t FWD_WGS = 4096;   // workgroups that a forward launch wants
+constexpr int64_t MOST_WGS = 1 << 20;
+constexpr int64_t LEAST_SEG = 32;   // steps of a segment
+
+int64_t type_size(int type) { return type == MGN_FP32 ? 4 : 2; }
+bool at(const void* p, int64_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+// How the rows and steps are dealt for V columns a lane and about `want` workgroups.
+void deal(ConvArgs& a, int V, int64_t want) {
+  const int per_row = (a.cols + V - 1) / V;
+  a.tiles = (per_row + NT - 1) / NT;
+  a.lanes = (per_row + a.tiles - 1) / a.tiles;
+  const int per = NT / a.lanes;
+  a.groups = (a.rows + per - 1) / per;
+  const int64_t have = a.groups * a.tiles, most = a.steps / LEAST_SEG;
+  a.segs = (want + have - 1) / have;
+  a.segs = a.segs < most ? a.segs : most;
+  if (a.segs < 1) a.segs = 1;
+  a.seg = (a.steps + a.segs - 1) / a.segs;
+  a.segs = (a.steps + a.seg - 1) / a.seg;
+  if (a.segs > 1 && a.steps - (a.segs - 1) * a.seg < MAX_W) --a.segs;  // the last one takes its few steps too
+}
+
+template <int W>
+using Int = std::integral_constant<int, W>;
+template <class F>
+hipError_t by_width(int width, F f) {
+  switch (width) {
+    case 1: return f(Int<1>());
+    case 2: return f(Int<2>());
+    case 3: return f(Int<3>());
+    case 4: return f(Int<4>());
+    case 5: return f(Int<5>());
+    case 6: return f(Int<6>());
+    case 7: return f(Int<7>());
+    case 8: return f(Int<8>());
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+int64_t conv_work_floats(int cols, int width) { return (int64_t)MGN_CONV_PARTS * cols * (width + 1); }
+
+hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
+  const int64_t C = a.rows * a.cols;
+  if (C <= 0) return hipSuccess;
+  const int64_t past_bytes = (width - 1) * C * type_size(type);
+  if (a.steps <= 0)
+    return a.past_out && a.past_out != a.past ? copy_bytes(a.past, a.past_out, past_bytes, st) : hipSuccess;
+  const int run = type == MGN_BF16 ? 8 : 4;
+  const bool vec = a.cols % run == 0 && at(a.x, 16) && at(a.y, 16) && at(a.past, 16) && at(a.past_out, 16);
+  deal(a, vec ? run : 1, FWD_WGS);
+  const bool tail = a.past_out && a.past_out == a.past && a.segs > 1;
+  ConvArgs m = a;
+  if (tail) m.past_out = nullptr;
+  const int64_t items = a.groups * a.segs;
+  const dim3 grid((unsigned)(items < MOST_WGS ? items : MOST_WGS), (unsigned)a.tiles);
+  const hipError_t e = by_width(width, [&](auto w) {
+    if (type == MGN_BF16) {
+      if (vec) hipLaunchKernelGGL((conv_kernel<MGN_BF16, w(), 8, 4>), grid, dim3(NT), 0, st, m);
+      else hipLaunchKernelGGL((conv_kernel<MGN_BF16, w(), 1, 8>), grid, dim3(NT), 0, st, m);
+    } else {
+      if (vec) hipLaunchKernelGGL((conv_kernel<MGN_FP32, w(), 4, 4>), grid, dim3(NT), 0, st, m);
+      else hipLaunchKernelGGL((conv_kernel<MGN_FP32, w(), 1, 8>), grid, dim3(NT), 0, st, m);
+    }
+    return hipGetLastError();
+  });
+  if (e != hipSuccess || !tail || width < 2) return e;
+  const int64_t b = ((width - 1) * C + NT - 1) / NT;
+  const dim3 tg((unsigned)(b < 8192 ? b : 8192));
+  if (type == MGN_BF16) hipLaunchKernelGGL((past_tail_kernel<MGN_BF16>), tg, dim3(NT), 0, st, a, width);
+  else hipLaunchKernelGGL((past_tail_kernel<MGN_FP32>), tg, dim3(NT), 0, st, a, width);
+  return hipGetLastError();
+}
+
+hipError_t launch_conv_grad(ConvArgs a, int type, int width, float* dw, float* db, int accumulate, hipStream_t st) {
+  const int64_t C = a.rows * a.cols;
+  int64_t parts = 0;
+  if (C > 0 && a.steps <= 0 && a.d_past)
+    if (const hipError_t e = copy_bytes(a.d_past_out, a.d_past, (width - 1) * C * 4, st); e != hipSuccess) return e;
+  if (C > 0 && a.steps > 0) {
+    const int run = 4;
+    const bool vec = a.cols % run == 0 && at(a.x, run * type_size(type)) && at(a.y, run * type_size(type)) &&
+                     at(a.dy, run * type_size(type)) && at(a.past, run * type_size(type)) && at(a.d_past, 16) &&
+                     at(a.d_past_out, 16);
+    deal(a, vec ? run : 1, MGN_CONV_PARTS);
+    const int64_t items = a.groups * a.segs;
+    parts = items < MGN_CONV_PARTS ? items : MGN_CONV_PARTS;
+    const dim3 grid((unsigned)parts, (unsigned)a.tiles);
+    const hipError_t e = by_width(width, [&](auto w) {
+      constexpr int STEPS = w() > 4 ? 2 : 4;
+      if (type == MGN_BF16) {
+        if (vec) hipLaunchKernelGGL((conv_grad_kernel<MGN_BF16, w(), 4, STEPS>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((conv_grad_kernel<MGN_BF16, w(), 1, 8>), grid, dim3(NT), 0, st, a);
+      } else {
+        if (vec) hipLaunchKernelGGL((conv_grad_kernel<MGN_FP32, w(), 4, STEPS>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((conv_grad_kernel<MGN_FP32, w(), 1, 8>), grid, dim3(NT), 0, st, a);
+      }
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+  }
+  if (!dw && !db) return hipSuccess;
+  return launch_col_sums(ColSums{a.part, parts, (int64_t)a.cols * (width + 1), {dw, db, nullptr},
+                                 {(int64_t)a.cols * width, a.cols}, accumulate}, st);
+}
+
+}  // namespace mgn

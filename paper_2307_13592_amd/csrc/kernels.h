@@ -186,6 +186,71 @@ struct RmsArgs {
   int cols;
   float eps;
 };
+// Layer norm of rows (layer.hip): as RmsArgs.
+struct LayerArgs {
+  const void *x, *res, *dy;
+  const float *w, *b;
+  void *total, *y;
+  float *y_scale, *part;
+  int64_t rows;
+  int cols;
+  float eps;
+};
+// Sums over the rows of part [parts][cols] into up to three arrays that share
+// the columns: the first len[0] columns are dst[0]'s, the next len[1] dst[1]'s,
+// the others dst[2]'s (any of them NULL: not wanted).
+struct ColSums {
+  const float* part;
+  int64_t parts, cols;
+  float* dst[3];
+  int64_t len[2];
+  int accumulate;
+};
+// Short causal convolution (conv.hip): [steps][rows][cols] arrays, weight
+// [cols][width], what came before [width - 1][rows][cols].
+struct ConvArgs {
+  const void *x, *past, *dy;
+  const float *w, *b, *d_past_out;
+  const uint8_t* starts;
+  void *y, *past_out;  // the backward's y: dx
+  float *d_past, *part;
+  int64_t steps, rows;
+  int64_t seg, segs, groups;  // set by the launcher
+  int cols, lanes, tiles;     // (the last two likewise)
+  int silu;
+};
+// Selective scan (ssm.hip, ssm_grad.hip): x, dt, z, y and their gradients
+// [steps][rows][cols], B, C [steps][rows][n], A [cols][n], states
+// [rows][cols][n], marks one state every MGN_MARK_STEPS steps.
+struct SsmArgs {
+  const void *x, *dt, *B, *C, *z, *dy;
+  const float *A, *D, *bias, *h0, *dh_last;
+  const uint8_t* starts;
+  void *y, *dx, *ddt, *dB, *dC, *dz;
+  float *h_last, *marks, *dh0;
+  float* state;  // chunks of the time axis: the state (the carry) that enters each
+  float* sums;   // and its sum of delta
+  float* bc;     // dB, dC of column tiles, where there are several
+  float* part;   // dA, dD, d_bias of a workgroup's items
+  int64_t steps, rows;
+  int64_t chunk, chunks;  // set by the launcher, as what follows
+  int64_t group0;         // first group of 4 columns of a launch
+  int64_t slots;          // backward: row groups that go through the rows in turn
+  int cols, n, softplus;
+  int tiles;  // backward: column tiles of a row
+};
+// A list of tensors (clip.hip), at most GRAD_TABLE of them a launch: tiles of
+// GRAD_TILE elements, tensor k's being first[k] .. first[k + 1] - 1.
+constexpr int GRAD_TABLE = 128;
+constexpr int64_t GRAD_TILE = 8192;
+struct GradTable {
+  const void* g[GRAD_TABLE];
+  void* out[GRAD_TABLE];
+  int64_t n[GRAD_TABLE];
+  uint32_t first[GRAD_TABLE + 1];
+  uint32_t bf16[GRAD_TABLE / 32];  // a bit for each tensor
+  int count;
+};
 // Gated recurrence (scan.hip): [steps][rows][cols] arrays, states [rows][cols].
 struct ScanArgs {
   const void *g, *x;
@@ -347,6 +412,33 @@ hipError_t launch_rows_store8(const Rows8Args& a, int type, hipStream_t st);
 hipError_t launch_rows_load8(const Rows8Args& a, int type, hipStream_t st);
 hipError_t launch_rms_norm(const RmsArgs& a, int type, int y_type, hipStream_t st);
 hipError_t launch_rms_norm_grad(const RmsArgs& a, int type, float* dw, int accumulate, hipStream_t st);
+hipError_t launch_col_sums(const ColSums& a, hipStream_t st);
+hipError_t launch_layer_norm(const LayerArgs& a, int type, int y_type, hipStream_t st);
+hipError_t launch_layer_norm_grad(const LayerArgs& a, int type, float* dw, float* db, int accumulate, hipStream_t st);
+// Global norm of the tensors of `n` tables and their clipping (clip.hip).  work
+// holds grad_work_doubles(n).  given: *norm is read, not written.  max_norm < 0:
+// the norm alone.
+int64_t grad_work_doubles(int64_t n);
+hipError_t launch_grads(const GradTable* t, int64_t n, float max_norm, bool given, float* norm, double* work,
+                        hipStream_t st);
+// Selective scan (ssm.hip, ssm_grad.hip); steps may be 0.
+size_t ssm_work_bytes(int64_t steps, int64_t rows, int cols, int n);
+hipError_t launch_ssm(SsmArgs a, int type, void* work, hipStream_t st);
+size_t ssm_grad_work_bytes(int64_t steps, int64_t rows, int cols, int n);
+hipError_t launch_ssm_grad(SsmArgs a, int type, float* dA, float* dD, float* d_bias, int accumulate, void* work,
+                           hipStream_t st);
+// How a time axis is cut where the columns are few: steps of a chunk.
+int64_t ssm_chunk(int64_t steps, int64_t rows, int cols, int64_t want);
+// Joins the chunks of a scan: entry c of state takes what enters chunk c (its own
+// end, from 0, before), from `first` on (NULL: zeros); reverse: from the last chunk
+// on.
+hipError_t launch_ssm_join(const SsmArgs& a, const float* first, bool reverse, hipStream_t st);
+hipError_t launch_state_copy(const float* in, float* out, int64_t n, hipStream_t st);
+// Short causal convolution (conv.hip); steps may be 0.  The backward: w_grad
+// (db likewise) may be NULL; part holds conv_work_floats.
+int64_t conv_work_floats(int cols, int width);
+hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st);
+hipError_t launch_conv_grad(ConvArgs a, int type, int width, float* dw, float* db, int accumulate, hipStream_t st);
 // Gated recurrence (scan.hip); steps may be 0.
 size_t scan_work_bytes(int64_t steps, int64_t rows, int cols);
 hipError_t launch_scan(ScanArgs a, int g_type, int x_type, hipStream_t st);

@@ -515,6 +515,8 @@ constexpr int64_t CACHE = (int64_t)256 << 20;
 
 }  // namespace
 
+hipError_t launch_state_copy(const float* in, float* out, int64_t n, hipStream_t st) { return copy_state(in, out, n, st); }
+
 size_t scan_work_bytes(int64_t steps, int64_t rows, int cols) {
   const int64_t C = rows * cols;
   if (steps <= 0 || C <= 0) return 0;

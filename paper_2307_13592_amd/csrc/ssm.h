@@ -1,0 +1,102 @@
+// Device parts that the selective scan and its backward share (gfx950).
+//
+// A wave holds 16 groups of 4 neighbouring columns, one to each 4 of its lanes.
+// For what is done once a column (delta, the products with x, the gate, y) lane q
+// of the four holds column q; the states of the group's 4 columns are dealt by
+// their index, lane q taking states q NL .. q NL + NL - 1 of all four.  So a lane
+// reads 4 NL numbers of A and only NL of B and of C, four columns use each of these,
+// and the sums over the states end in the lane of their column after two exchanges
+// between neighbouring lanes.
+#pragma once
+#include <type_traits>
+
+#include "kernels.h"
+#include "rows8.h"
+
+namespace mgn {
+
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+
+// a b, 0 where a is 0 whatever b holds.
+__device__ __forceinline__ float mul_or_0(float a, float b) { return a == 0.f ? 0.f : a * b; }
+// Whether any lane of the wave says so.
+__device__ __forceinline__ bool any(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
+
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+// log(1 + e^v), to a few half-steps of itself at any v: with e = e^-|v| the
+// logarithm of 1 + e is 2 atanh(s), s = e / (2 + e), an odd series in s <= 1 / 3
+// (five terms, fitted in s^2 to 5e-9 of the sum).
+__device__ __forceinline__ float softplus(float v) {
+  const float e = __expf(-fabsf(v));
+  const float s = e * __builtin_amdgcn_rcpf(2.f + e), w = s * s;
+  float p = fmaf(w, 0.28161454f, 0.27964345f);
+  p = fmaf(w, p, 0.40024651f);
+  p = fmaf(w, p, 0.6666632f);
+  p = fmaf(w, p, 2.f);
+  return v != v ? v : fmaf(s, p, fmaxf(v, 0.f));
+}
+
+// v of lane J of each four.
+template <int J>
+__device__ __forceinline__ float quad(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), J * 0x55, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void quads(float v, float (&u)[4]) {
+  u[0] = quad<0>(v), u[1] = quad<1>(v), u[2] = quad<2>(v), u[3] = quad<3>(v);
+}
+// Sum over the four lanes of v[q], in lane q.
+__device__ __forceinline__ float quad_sums(const float (&v)[4]) {
+  const bool b0 = threadIdx.x & 1, b1 = threadIdx.x & 2;
+  const float r0 = (b0 ? v[1] : v[0]) + mirror<1>(b0 ? v[0] : v[1]);
+  const float r1 = (b0 ? v[3] : v[2]) + mirror<1>(b0 ? v[2] : v[3]);
+  return (b1 ? r1 : r0) + mirror<2>(b1 ? r0 : r1);
+}
+
+template <int TYPE>
+__device__ __forceinline__ float load1(const void* p, int64_t i) {
+  float v[1];
+  get<1>((const Elem<TYPE>*)p + i, v);
+  return v[0];
+}
+template <int TYPE>
+__device__ __forceinline__ void store1(void* p, int64_t i, float v) {
+  put<1>((Elem<TYPE>*)p + i, &v);
+}
+
+// NL of the n numbers at p + i, from number s on; FULL: all of them are there.
+template <int TYPE, int NL, bool FULL>
+__device__ __forceinline__ void load_n(const void* p, int64_t i, int s, int n, float (&v)[NL]) {
+  const Elem<TYPE>* r = (const Elem<TYPE>*)p + i + s;
+  if constexpr (FULL) {
+    constexpr int RUN = 16 / sizeof(Elem<TYPE>) < NL ? 16 / sizeof(Elem<TYPE>) : NL;
+#pragma unroll
+    for (int k = 0; k < NL; k += RUN) get<RUN>(r + k, v + k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      v[k] = 0.f;
+      if (s + k < n) get<1>(r + k, v + k);
+    }
+  }
+}
+template <int NL, bool FULL>
+__device__ __forceinline__ void store_n(float* p, int64_t i, int s, int n, const float (&v)[NL]) {
+  float* r = p + i + s;
+  if constexpr (FULL) {
+#pragma unroll
+    for (int k = 0; k < NL; k += NL < 4 ? NL : 4) put<(NL < 4 ? NL : 4)>(r + k, v + k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NL; ++k)
+      if (s + k < n) r[k] = v[k];
+  }
+}
+
+// A chunk in which a trajectory starts: what enters it does not reach its end.
+constexpr float CUT = -INFINITY;
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+}  // namespace mgn

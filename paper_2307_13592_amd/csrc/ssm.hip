@@ -1,0 +1,222 @@
+// Selective state space scan along time (gfx950): every column of every row has n
+// states, with a step size, an input and an output vector of each step's own:
+//   delta = softplus(dt + bias) (or dt + bias),
+//   h_t[k] = exp(delta A[k]) h_{t-1}[k] + delta x B_t[k],
+//   y_t = (sum_k C_t[k] h_t[k] + D x) z sigmoid(z).
+//
+// The states stay in registers (ssm.h) from the first step to the last, and each
+// input is read once.  With few columns the time axis is cut into chunks: a first
+// launch takes each chunk from zero states to its end, a second joins these (all
+// that a chunk does to what enters it is the factor exp(A sum of delta), of which the
+// sum is one number a column), a third runs every chunk from the state that enters
+// it.  A chunk's work is then done twice but for y.
+//
+// Bound by the vector units: an exponential takes the time of 4 other
+// instructions, and there are 4 of these for a state and step, against 6 - 16 bytes
+// an element; with one step by the states' 8 n bytes.
+#include "ssm.h"
+
+namespace mgn {
+namespace {
+
+constexpr int NT = 256;
+enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES };
+
+template <int TYPE, int NL, bool FULL, int PASS>
+__global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
+  constexpr int STEPS = NL <= 4 ? 4 : NL == 8 ? 2 : 1;  // steps whose loads are in flight together
+  const int per_row = (a.cols + 3) / 4, q = threadIdx.x & 3;
+  const int64_t gi = a.group0 + ((int64_t)blockIdx.x * NT + threadIdx.x) / 4, row = gi / per_row;
+  const int g = (int)(gi - row * per_row) * 4, col = g + q, s = q * NL;
+  const bool in = row < a.rows, ok = in && col < a.cols;
+  const int c = blockIdx.y;
+  const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
+  const int64_t C = a.rows * a.cols, i = row * a.cols + col, bn = row * a.n, at = (row * a.cols + g) * a.n;
+
+  float h[4][NL], A[4][NL];
+  const float* const from = PASS == FROM_STATES ? a.state + c * C * a.n : PASS == WHOLE_AXIS ? a.h0 : nullptr;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) h[j][k] = A[j][k] = 0.f;
+    if (in && g + j < a.cols) {
+      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(g + j) * a.n, s, a.n, A[j]);
+      if (from) load_n<MGN_FP32, NL, FULL>(from, at + j * a.n, s, a.n, h[j]);
+    }
+#pragma unroll
+    for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
+  }
+  const float bias = a.bias && ok ? a.bias[col] : 0.f, D = a.D && ok ? a.D[col] : 0.f;
+  float sum = 0.f;
+
+  for (int64_t t = ts; t < te; t += STEPS) {
+    float x[STEPS], dt[STEPS], z[STEPS], B[STEPS][NL], Cn[STEPS][NL];
+    bool fresh[STEPS];
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+      x[e] = dt[e] = z[e] = 0.f;
+      fresh[e] = false;
+#pragma unroll
+      for (int k = 0; k < NL; ++k) B[e][k] = Cn[e][k] = 0.f;
+      if (t + e >= te) continue;
+      if (a.starts) fresh[e] = a.starts[t + e];
+      if (ok) {
+        x[e] = load1<TYPE>(a.x, (t + e) * C + i);
+        dt[e] = load1<TYPE>(a.dt, (t + e) * C + i);
+        if (PASS != LOCAL_ENDS && a.z) z[e] = load1<TYPE>(a.z, (t + e) * C + i);
+      }
+      if (in) {
+        load_n<TYPE, NL, FULL>(a.B, (t + e) * a.rows * a.n + bn, s, a.n, B[e]);
+        if constexpr (PASS != LOCAL_ENDS) load_n<TYPE, NL, FULL>(a.C, (t + e) * a.rows * a.n + bn, s, a.n, Cn[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+      if (t + e >= te) break;
+      if (PASS != LOCAL_ENDS && a.marks && (t + e) % MGN_MARK_STEPS == 0)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (in && g + j < a.cols)
+            store_n<NL, FULL>(a.marks + (t + e) / MGN_MARK_STEPS * C * a.n, at + j * a.n, s, a.n, h[j]);
+      if (fresh[e]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int k = 0; k < NL; ++k) h[j][k] = 0.f;
+        sum = CUT;
+      }
+      float delta = dt[e] + bias;
+      if (a.softplus) delta = softplus(delta);
+      delta = ok ? delta : 0.f;
+      sum += delta;
+      float d[4], u[4], y[4];
+      quads(delta, d);
+      quads(mul_or_0(delta, x[e]), u);
+      // B may hold anything where a column's step has size 0
+      const auto step = [&](auto held) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          y[j] = 0.f;
+#pragma unroll
+          for (int k = 0; k < NL; ++k) {
+            const float b = held() ? mul_or_0(u[j], B[e][k]) : u[j] * B[e][k];
+            h[j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), h[j][k], b);
+            if constexpr (PASS != LOCAL_ENDS) y[j] = fmaf(Cn[e][k], h[j][k], y[j]);
+          }
+        }
+      };
+      if (any(ok && delta == 0.f)) step(std::true_type());
+      else step(std::false_type());
+      if constexpr (PASS != LOCAL_ENDS) {
+        float v = quad_sums(y);
+        if (a.D) v = fmaf(D, x[e], v);
+        if (a.z) v *= z[e] * sigmoid(z[e]);
+        if (ok) store1<TYPE>(a.y, (t + e) * C + i, v);
+      }
+    }
+  }
+  float* const to = PASS == LOCAL_ENDS ? a.state + c * C * a.n : te == a.steps ? a.h_last : nullptr;
+  if (to)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (in && g + j < a.cols) store_n<NL, FULL>(to, at + j * a.n, s, a.n, h[j]);
+  if (PASS == LOCAL_ENDS && ok) a.sums[c * C + i] = sum;
+}
+
+// Chunk by chunk: what enters each, in the place of its own end.  A lane a state.
+constexpr int AHEAD = 8;
+__global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* first, bool reverse) {
+  const int64_t C = a.rows * a.cols, S = C * a.n, step = reverse ? -1 : 1;
+  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < S; i += (int64_t)gridDim.x * NT) {
+    const int64_t ch = i / a.n;
+    const float A = a.A[ch % a.cols * a.n + (i - ch * a.n)] * LOG2E;
+    float v = first ? first[i] : 0.f;
+    int64_t c = reverse ? a.chunks - 1 : 0;
+    for (int64_t k = 0; k < a.chunks; k += AHEAD) {
+      float own[AHEAD], sum[AHEAD];
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (k + e < a.chunks - 1) own[e] = a.state[(c + step * e) * S + i], sum[e] = a.sums[(c + step * e) * C + ch];
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (k + e < a.chunks) {
+          a.state[(c + step * e) * S + i] = v;
+          if (k + e < a.chunks - 1) v = sum[e] == CUT ? own[e] : fmaf(__builtin_amdgcn_exp2f(A * sum[e]), v, own[e]);
+        }
+      c += step * AHEAD;
+    }
+  }
+}
+
+constexpr int64_t LAUNCH = 1 << 28;  // groups of one launch (a grid holds less than 2^32 threads)
+constexpr int64_t WAVES = 2048;  // waves that a launch wants before it leaves the time axis whole
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+template <int TYPE, int PASS>
+hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
+  const int64_t groups = a.rows * ((a.cols + 3) / 4);
+  const auto go = [&](auto nl) {
+    constexpr int NL = nl();
+    hipError_t e = hipSuccess;
+    for (a.group0 = 0; a.group0 < groups && e == hipSuccess; a.group0 += LAUNCH) {
+      const int64_t n = groups - a.group0 < LAUNCH ? groups - a.group0 : LAUNCH;
+      const dim3 grid((unsigned)((n * 4 + NT - 1) / NT), (unsigned)chunks);
+      if (a.n == 4 * NL) hipLaunchKernelGGL((ssm_kernel<TYPE, NL, true, PASS>), grid, dim3(NT), 0, st, a);
+      else hipLaunchKernelGGL((ssm_kernel<TYPE, NL, false, PASS>), grid, dim3(NT), 0, st, a);
+      e = hipGetLastError();
+    }
+    return e;
+  };
+  if (a.n <= 4) return go(Int<1>());
+  if (a.n <= 8) return go(Int<2>());
+  if (a.n <= 16) return go(Int<4>());
+  if (a.n <= 32) return go(Int<8>());
+  return go(Int<16>());
+}
+
+template <int TYPE>
+hipError_t launch_typed(SsmArgs& a, hipStream_t st) {
+  if (a.chunks == 1) return launch_pass<TYPE, WHOLE_AXIS>(a, 1, st);
+  hipError_t e = launch_pass<TYPE, LOCAL_ENDS>(a, a.chunks - 1, st);
+  if (e == hipSuccess) e = launch_ssm_join(a, a.h0, false, st);
+  return e == hipSuccess ? launch_pass<TYPE, FROM_STATES>(a, a.chunks, st) : e;
+}
+
+}  // namespace
+
+int64_t ssm_chunk(int64_t steps, int64_t rows, int cols, int64_t want) {
+  const int64_t waves = (rows * ((cols + 3) / 4) + 15) / 16, least = 4 * MGN_MARK_STEPS;
+  int64_t n = want / (waves > 0 ? waves : 1);
+  if (n > steps / least) n = steps / least;
+  if (n < 2) return steps;
+  const int64_t chunk = (steps + n - 1) / n;
+  return (chunk + MGN_MARK_STEPS - 1) / MGN_MARK_STEPS * MGN_MARK_STEPS;
+}
+
+hipError_t launch_ssm_join(const SsmArgs& a, const float* first, bool reverse, hipStream_t st) {
+  const int64_t n = a.rows * a.cols * a.n, b = (n + NT - 1) / NT;
+  hipLaunchKernelGGL(ssm_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(NT), 0, st, a, first, reverse);
+  return hipGetLastError();
+}
+
+size_t ssm_work_bytes(int64_t steps, int64_t rows, int cols, int n) {
+  if (steps <= 0 || rows <= 0) return 0;
+  const int64_t chunk = ssm_chunk(steps, rows, cols, WAVES), chunks = (steps + chunk - 1) / chunk;
+  if (chunks < 2) return 0;
+  return up(4 * chunks * rows * cols * n) + up(4 * chunks * rows * cols);
+}
+
+hipError_t launch_ssm(SsmArgs a, int type, void* work, hipStream_t st) {
+  const int64_t C = a.rows * a.cols;
+  if (C <= 0) return hipSuccess;
+  if (a.steps <= 0)
+    return a.h_last && a.h_last != a.h0 ? launch_state_copy(a.h0, a.h_last, C * a.n, st) : hipSuccess;
+  a.chunk = ssm_chunk(a.steps, a.rows, a.cols, WAVES);
+  a.chunks = (a.steps + a.chunk - 1) / a.chunk;
+  a.state = (float*)work;
+  a.sums = (float*)((char*)work + up(4 * a.chunks * C * a.n));
+  return type == MGN_BF16 ? launch_typed<MGN_BF16>(a, st) : launch_typed<MGN_FP32>(a, st);
+}
+
+}  // namespace mgn
