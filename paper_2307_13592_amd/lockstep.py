@@ -18,7 +18,7 @@ import torch
 
 from . import (mgn_halo_masks, mgn_lockstep_backward, mgn_lockstep_backward8, mgn_lockstep_forward,
                mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step, _on)
-from .runner import LatentCache, Session
+from .runner import LatentCache, Session, clip_grads
 
 
 def nocomm_edges(send, recv, part):
@@ -111,11 +111,14 @@ class Lockstep:
             mgn_lockstep_backward(*args, False, stream)
         return self.d_params
 
-    def sgd(self, lr: float, stream=None):
+    def sgd(self, lr: float, stream=None, max_norm=None):
         """Every part's model takes the same update with the summed gradient,
-        so the parts' parameters stay identical."""
+        so the parts' parameters stay identical.  max_norm: that gradient is first
+        scaled, in place, to at most this norm; returns the norm that it had."""
+        norm = None if max_norm is None else clip_grads([self.d_params], max_norm, stream)
         for s in self.sessions:
             mgn_sgd_step(s.model, self.d_params, lr, stream)
+        return norm
 
     def close(self):
         for s in self.sessions:

@@ -10,7 +10,9 @@ from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_d
                mgn_graph_validate, mgn_mse_grad, mgn_param_count, mgn_set_params, mgn_set_recompute,
                mgn_norm_accumulate, mgn_norm_apply, MGN_NORM_WORK_PER_COL, mgn_rollout_update, mgn_set_h1_stash,
                mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
-               mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on)
+               mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on, mgn_causal_conv,
+               mgn_causal_conv_grad, mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad,
+               mgn_selective_marks, mgn_selective_scan, mgn_selective_scan_grad)
 
 
 class Session:
@@ -97,15 +99,21 @@ class Session:
         mgn_backward(self.model, d_out, self.d_params, accumulate, self.d_halo, stream)
         return self.d_params, self.d_halo
 
-    def sgd(self, lr: float, grad=None, stream=None):
-        """Parameter update with the last backward's gradient (or `grad`)."""
-        mgn_sgd_step(self.model, self.d_params if grad is None else grad, lr, stream)
+    def sgd(self, lr: float, grad=None, stream=None, max_norm=None):
+        """Parameter update with the last backward's gradient (or `grad`); max_norm:
+        that is first scaled, in place, to at most this norm.  Returns the norm that
+        it had (float32 [1] on the device; None without max_norm)."""
+        grad = self.d_params if grad is None else grad
+        norm = None if max_norm is None else clip_grads([grad], max_norm, stream)
+        mgn_sgd_step(self.model, grad, lr, stream)
+        return norm
 
     def rollout(self, steps: int, col0: int = 3, stream=None, memory=None, history=None):
         """`steps` next-step predictions, each fed back into the flow columns
         of the node features (q <- q + p); returns the outputs of every step.
         memory: a GatedMemory of this session's outputs with a gate; the
-        increments fed back are then its states, h <- f h + (1 - f) p.
+        increments fed back are then its states, h <- f h + (1 - f) p; or a
+        SelectiveMemory of them with dt, B and C: its outputs.
         history: a LatentCache of at least steps * n_owned slots; the outputs
         are then kept there in 8 bits (step t in slots t n_owned ..), and the
         cache is returned.  (A row of a few columns has a scale of 4 bytes of its
@@ -244,6 +252,56 @@ class RmsNorm:
         return dx
 
 
+class LayerNorm:
+    """Layer norm of node rows with a weight and a bias per column, and the addition
+    of a residual before it."""
+
+    def __init__(self, cols: int, device: str = "cuda", eps: float = 1e-5):
+        self.cols, self.eps = cols, eps
+        self.weight = torch.ones(cols, dtype=torch.float32, device=device)
+        self.bias = torch.zeros_like(self.weight)
+        self.d_weight, self.d_bias = torch.zeros_like(self.weight), torch.zeros_like(self.weight)
+
+    def apply(self, x, res=None, dtype=None, stream=None):
+        """(y, t): y the norm of t = x + res (of x without a residual) in
+        `dtype` (x's by default)."""
+        with _on(stream, x.device):
+            y = torch.empty_like(x, dtype=x.dtype if dtype is None else dtype)
+            total = x if res is None else torch.empty_like(x)
+        mgn_layer_norm(x, self.weight, self.bias, y, res, None if res is None else total, None, self.eps, stream)
+        return y, total
+
+    def store(self, x, cache: LatentCache, first: int = 0, res=None, stream=None):
+        """The norm of x + res in 8 bits, into the cache's slots from `first`
+        on; returns the sum."""
+        q, scale = cache._span(first, x.shape[0])
+        with _on(stream, x.device):
+            total = x if res is None else torch.empty_like(x)
+        mgn_layer_norm(x, self.weight, self.bias, q, res, None if res is None else total, scale, self.eps, stream)
+        return total
+
+    def grad(self, total, dy, d_total=None, accumulate: bool = False, stream=None):
+        """dL/dt from dy and the gradient that reaches t otherwise; d_weight and
+        d_bias take (accumulate: add) theirs."""
+        with _on(stream, total.device):
+            dx = torch.empty_like(total)
+        mgn_layer_norm_grad(total, self.weight, dy, dx, self.d_weight, self.d_bias, d_total, accumulate, None, self.eps,
+                            stream)
+        return dx
+
+
+def clip_grads(grads, max_norm: float, stream=None):
+    """Scales gradients (tensors, or an mgn_grad_list of them) to at most max_norm
+    together, in place (into the list's outs); returns the norm that they had, a
+    float32 [1] on their device."""
+    grads = grads if isinstance(grads, mgn_grad_list) else mgn_grad_list(grads)
+    device = grads.tensors[0][0].device if grads.tensors[0] else "cuda"
+    with _on(stream, device):
+        norm = torch.empty(1, dtype=torch.float32, device=device)
+    mgn_grad_clip(grads, max_norm, norm, stream=stream)
+    return norm
+
+
 class GatedMemory:
     """A gated linear recurrence over time on rows of `cols` columns:
     h <- f h + (1 - f) x with f = sigmoid(g).  step() carries `state` along a
@@ -286,3 +344,69 @@ class GatedMemory:
         h0 = getattr(h, "h0", self.h0) if h0 is None else h0
         mgn_gated_scan_grad(g, x, h, dg, dx, dh, dh_last, dh0, h0, starts, x_scale, None, stream)
         return dg, dx, dh0
+
+
+class SelectiveMemory:
+    """A selective state space memory over time on rows of `cols` columns: a short
+    causal convolution with SiLU of the inputs, then a scan with `states` states a
+    column, whose step sizes, input and output vectors (dt [rows][cols], B, C
+    [rows][states] of a step) the caller brings, from projections of its own or fixed
+    ones: `dt`, `B`, `C` are what step() uses when it is given none.  step() carries
+    the states along a rollout (Session.rollout(memory=...)); scan() and grad() run
+    whole trajectories.  The parameters are float32: conv_weight [cols][width],
+    conv_bias, A [cols][states] (negative), D, dt_bias (the step size is the softplus of
+    dt + dt_bias); their gradients lie in `grads`, by the same names."""
+
+    def __init__(self, rows: int, cols: int, states: int = 16, width: int = 4, dtype=torch.float32, device: str = "cuda",
+                 dt=None, B=None, C=None):
+        new = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=device)
+        self.conv_weight, self.conv_bias = new(cols, width), new(cols)
+        self.conv_weight[:, -1] = 1  # the step's own input
+        self.A = -torch.arange(1, states + 1, dtype=torch.float32, device=device).repeat(cols, 1)
+        self.D, self.dt_bias = new(cols) + 1, new(cols)
+        self.grads = {k: torch.zeros_like(getattr(self, k)) for k in ("conv_weight", "conv_bias", "A", "D", "dt_bias")}
+        self.state = new(rows, cols, states)
+        self.past = torch.zeros((width - 1, rows, cols), dtype=dtype, device=device)
+        self.dt, self.B, self.C = dt, B, C
+        self._out = torch.empty((2, 1, rows, cols), dtype=dtype, device=device)
+
+    def step(self, x, dt=None, B=None, C=None, z=None, stream=None):
+        """One time step (x, dt, z [rows][cols], B, C [rows][states]); returns its
+        output, which the next step() overwrites."""
+        dt, B, C = (a if b is None else b for a, b in ((self.dt, dt), (self.B, B), (self.C, C)))
+        if dt is None or B is None or C is None:
+            raise ValueError("dt, B, C: not given")
+        u, y = self._out[0], self._out[1]
+        mgn_causal_conv(x[None], self.conv_weight, u, self.conv_bias, self.past, self.past, None, True, stream)
+        mgn_selective_scan(u, dt[None], self.A, B[None], C[None], y, self.D, self.dt_bias, None if z is None else z[None],
+                           self.state, self.state, None, None, True, None, stream)
+        return y[0]
+
+    def scan(self, x, dt, B, C, z=None, starts=None, stream=None):
+        """(y, kept): every output of a trajectory [steps][rows][cols] that continues
+        from what the last one left, and what grad() takes of it."""
+        with _on(stream, x.device):
+            u, y, past = torch.empty_like(x), torch.empty_like(x), self.past.clone()
+        marks = mgn_selective_marks(x, self.A, stream)
+        mgn_causal_conv(x, self.conv_weight, u, self.conv_bias, self.past, self.past, starts, True, stream)
+        mgn_selective_scan(u, dt, self.A, B, C, y, self.D, self.dt_bias, z, self.state, self.state, marks, starts, True,
+                           None, stream)
+        return y, (past, u, marks)
+
+    def grad(self, x, dt, B, C, kept, dy, z=None, starts=None, dh_last=None, d_past=None, accumulate: bool = False,
+             stream=None):
+        """A dict of dx, ddt, dB, dC, dz (None without z) and of dh0 and d_past, the
+        gradients of what the scan() began with; dh_last and d_past: those of what it
+        left (a later window's).  self.grads take (accumulate: add) the parameters'."""
+        past, u, marks = kept
+        with _on(stream, x.device):
+            du, dx, ddt, dB, dC = (torch.empty_like(a) for a in (x, x, dt, B, C))
+            dz = None if z is None else torch.empty_like(z)
+            dh0 = torch.empty_like(self.state)
+            d_before = torch.empty(past.shape, dtype=torch.float32, device=x.device)
+        p, g = self, self.grads
+        mgn_selective_scan_grad(u, dt, p.A, B, C, marks, dy, du, ddt, g["A"], dB, dC, g["D"], g["dt_bias"], dz, p.D,
+                                p.dt_bias, z, dh_last, dh0, starts, True, accumulate, None, stream)
+        mgn_causal_conv_grad(x, p.conv_weight, du, dx, g["conv_weight"], g["conv_bias"], p.conv_bias, past, d_before,
+                             d_past, starts, True, accumulate, None, stream)
+        return dict(dx=dx, ddt=ddt, dB=dB, dC=dC, dz=dz, dh0=dh0, d_past=d_before)
