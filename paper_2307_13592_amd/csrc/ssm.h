@@ -34,7 +34,7 @@ __device__ __forceinline__ float softplus(float v) {
   p = fmaf(w, p, 0.40024651f);
   p = fmaf(w, p, 0.6666632f);
   p = fmaf(w, p, 2.f);
-  return v != v ? v : fmaf(s, p, fmaxf(v, 0.f));
+  return fmaf(s, p, fmaxf(v, 0.f));  // (NaN: s is)
 }
 
 // v of lane J of each four.
@@ -80,6 +80,84 @@ __device__ __forceinline__ void load_n(const void* p, int64_t i, int s, int n, f
     }
   }
 }
+
+// A lane's offset as the compiler finds it here: it is then added by the access
+// itself, to a scalar address, and not beforehand to every array's, which would take
+// two registers for each of them.
+__device__ __forceinline__ uint32_t here(uint32_t o) {
+  asm volatile("" : "+v"(o));
+  return o;
+}
+// The element at byte `o` from a wave's base: a scalar address and a 32-bit offset.
+template <int TYPE>
+__device__ __forceinline__ uint32_t raw1(const char* base, uint32_t o) {
+  o = here(o);
+  if constexpr (TYPE == MGN_BF16) return *(const uint16_t*)(base + o);
+  else return *(const uint32_t*)(base + o);
+}
+template <int TYPE>
+__device__ __forceinline__ float value1(uint32_t w) {
+  return __uint_as_float(TYPE == MGN_BF16 ? w << 16 : w);
+}
+template <int TYPE>
+__device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
+  if constexpr (TYPE == MGN_BF16) *(uint16_t*)(base + here(o)) = (uint16_t)pack_bf16(v, 0.f);
+  else *(float*)(base + here(o)) = v;
+}
+// NL numbers as they lie in memory, so that a load in flight is not waited for
+// before its step comes: numbers s .. of the n at byte o.
+template <int TYPE, int NL, bool FULL>
+struct Raw {
+  static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = FULL ? (NL * SIZE + 3) / 4 : NL;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const char* base, uint32_t o, int s, int n) {
+    if constexpr (FULL) {
+      __builtin_memcpy(w, base + here(o + (uint32_t)(s * SIZE)), NL * SIZE);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NL; ++k) w[k] = raw1<TYPE>(base, o + (uint32_t)((s + k < n ? s + k : n - 1) * SIZE));
+    }
+  }
+  __device__ __forceinline__ void get(int s, int n, float (&v)[NL]) const {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      if constexpr (TYPE != MGN_BF16) v[k] = __uint_as_float(w[k]);
+      else if constexpr (!FULL) v[k] = __uint_as_float(w[k] << 16);
+      else v[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+      if constexpr (!FULL) v[k] = s + k < n ? v[k] : 0.f;
+    }
+  }
+};
+
+// Where a lane's groups and columns lie: the wave's first ones (the same for all of
+// its lanes, so that addresses are a scalar and a lane's 32-bit offset), and the
+// lane's from there.
+struct Spot {
+  int64_t row0, i0, bn0, at0;  // first row; first column of [rows][cols], [rows][n], [rows][cols][n]
+  uint32_t o, ob, oa;          // the lane's column, row of n numbers, states of its group's first column
+  int64_t row;
+  int g, col;  // the group's first column, the lane's
+  bool in, ok; // the group, the lane's column is there
+  __device__ __forceinline__ Spot(const SsmArgs& a, int64_t group, int q) {
+    const int per_row = (a.cols + 3) / 4, ld = (threadIdx.x & 63) >> 2;
+    row0 = group >> 32 ? group / per_row : (int64_t)((uint32_t)group / (uint32_t)per_row);
+    const int g0 = (int)(group - row0 * per_row);
+    const uint32_t down = (uint32_t)(g0 + ld) / (uint32_t)per_row;
+    row = row0 + down;
+    g = (g0 + ld - (int)down * per_row) * 4;
+    col = g + q;
+    in = row < a.rows;
+    ok = in && col < a.cols;
+    i0 = row0 * a.cols + g0 * 4;
+    bn0 = row0 * a.n;
+    at0 = i0 * a.n;
+    // lanes without a column read the first one's
+    o = ok ? down * a.cols + col - g0 * 4 : 0;
+    ob = in ? down * a.n : 0;
+    oa = in ? (down * a.cols + g - g0 * 4) * a.n : 0;
+  }
+};
+
 template <int NL, bool FULL>
 __device__ __forceinline__ void store_n(float* p, int64_t i, int s, int n, const float (&v)[NL]) {
   float* r = p + i + s;

@@ -22,16 +22,26 @@ namespace {
 constexpr int NT = 256;
 enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES };
 
+// What some steps bring, as it lies in memory.
+template <int TYPE, int NL, bool FULL, int STEPS>
+struct Inputs {
+  uint32_t x[STEPS], dt[STEPS], z[STEPS], fresh[STEPS];
+  Raw<TYPE, NL, FULL> B[STEPS], C[STEPS];
+};
+
 template <int TYPE, int NL, bool FULL, int PASS>
 __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   constexpr int STEPS = NL <= 4 ? 4 : NL == 8 ? 2 : 1;  // steps whose loads are in flight together
-  const int per_row = (a.cols + 3) / 4, q = threadIdx.x & 3;
-  const int64_t gi = a.group0 + ((int64_t)blockIdx.x * NT + threadIdx.x) / 4, row = gi / per_row;
-  const int g = (int)(gi - row * per_row) * 4, col = g + q, s = q * NL;
-  const bool in = row < a.rows, ok = in && col < a.cols;
+  using E = Elem<TYPE>;
+  using In = Inputs<TYPE, NL, FULL, STEPS>;
+  constexpr int SIZE = sizeof(E);
+  const int q = threadIdx.x & 3, s = q * NL, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t group = a.group0 + ((int64_t)blockIdx.x * (NT / 64) + wave) * 16;
+  const Spot p(a, group, q);
+  if (p.row0 >= a.rows) return;
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
-  const int64_t C = a.rows * a.cols, i = row * a.cols + col, bn = row * a.n, at = (row * a.cols + g) * a.n;
+  const int64_t C = a.rows * a.cols, cb = C * SIZE, rb = a.rows * a.n * SIZE;  // a step's bytes
 
   float h[4][NL], A[4][NL];
   const float* const from = PASS == FROM_STATES ? a.state + c * C * a.n : PASS == WHOLE_AXIS ? a.h0 : nullptr;
@@ -39,88 +49,141 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) h[j][k] = A[j][k] = 0.f;
-    if (in && g + j < a.cols) {
-      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(g + j) * a.n, s, a.n, A[j]);
-      if (from) load_n<MGN_FP32, NL, FULL>(from, at + j * a.n, s, a.n, h[j]);
+    if (p.in && p.g + j < a.cols) {
+      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(p.g + j) * a.n, s, a.n, A[j]);
+      if (from) load_n<MGN_FP32, NL, FULL>(from + p.at0, p.oa + j * a.n, s, a.n, h[j]);
     }
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   }
-  const float bias = a.bias && ok ? a.bias[col] : 0.f, D = a.D && ok ? a.D[col] : 0.f;
+  const float bias = a.bias && p.ok ? a.bias[p.col] : 0.f, D = a.D && p.ok ? a.D[p.col] : 0.f;
   float sum = 0.f;
 
-  for (int64_t t = ts; t < te; t += STEPS) {
-    float x[STEPS], dt[STEPS], z[STEPS], B[STEPS][NL], Cn[STEPS][NL];
-    bool fresh[STEPS];
+  // the next steps to load, and to store
+  const int64_t x0 = (ts * C + p.i0) * SIZE, n0 = (ts * a.rows * a.n + p.bn0) * SIZE;
+  const char *px = (const char*)a.x + x0, *pd = (const char*)a.dt + x0, *pz = (const char*)a.z + x0;
+  const char *pB = (const char*)a.B + n0, *pC = (const char*)a.C + n0;
+  char* py = (char*)a.y + x0;
+  const uint8_t* ps = a.starts + ts;
+  const uint32_t o = p.o * SIZE, ob = p.ob * SIZE;
+  const auto load = [&](In& v, int64_t left) {
+    const auto one = [&](int e, int64_t at) {
+      v.x[e] = raw1<TYPE>(px + at * cb, o);
+      v.dt[e] = raw1<TYPE>(pd + at * cb, o);
+      if (PASS != LOCAL_ENDS && a.z) v.z[e] = raw1<TYPE>(pz + at * cb, o);
+      v.B[e].load(pB + at * rb, ob, s, a.n);
+      if constexpr (PASS != LOCAL_ENDS) v.C[e].load(pC + at * rb, ob, s, a.n);
+      if (a.starts) v.fresh[e] = ps[at];
+    };
+    if (left <= 0) return;
+    if (left >= STEPS) {
 #pragma unroll
-    for (int e = 0; e < STEPS; ++e) {
-      x[e] = dt[e] = z[e] = 0.f;
-      fresh[e] = false;
+      for (int e = 0; e < STEPS; ++e) one(e, e);
+    } else {  // the last steps, some of them twice
 #pragma unroll
-      for (int k = 0; k < NL; ++k) B[e][k] = Cn[e][k] = 0.f;
-      if (t + e >= te) continue;
-      if (a.starts) fresh[e] = a.starts[t + e];
-      if (ok) {
-        x[e] = load1<TYPE>(a.x, (t + e) * C + i);
-        dt[e] = load1<TYPE>(a.dt, (t + e) * C + i);
-        if (PASS != LOCAL_ENDS && a.z) z[e] = load1<TYPE>(a.z, (t + e) * C + i);
-      }
-      if (in) {
-        load_n<TYPE, NL, FULL>(a.B, (t + e) * a.rows * a.n + bn, s, a.n, B[e]);
-        if constexpr (PASS != LOCAL_ENDS) load_n<TYPE, NL, FULL>(a.C, (t + e) * a.rows * a.n + bn, s, a.n, Cn[e]);
-      }
+      for (int e = 0; e < STEPS; ++e) one(e, e < left ? e : left - 1);
     }
+    px += STEPS * cb, pd += STEPS * cb, pz += STEPS * cb, pB += STEPS * rb, pC += STEPS * rb, ps += STEPS;
+  };
+  const auto run = [&](const In& v, int64_t t) {
+    const int n = te - t < STEPS ? (int)(te - t) : STEPS;
+    if (PASS != LOCAL_ENDS && a.marks && t % MGN_MARK_STEPS == 0)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (p.in && p.g + j < a.cols)
+          store_n<NL, FULL>(a.marks + (t / MGN_MARK_STEPS * C * a.n + p.at0), p.oa + j * a.n, s, a.n, h[j]);
+    // what is done once a column
+    float x[STEPS], delta[STEPS], y[STEPS], f[STEPS];
+    bool held = false;
+    uint32_t fresh = 0;
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
-      if (t + e >= te) break;
-      if (PASS != LOCAL_ENDS && a.marks && (t + e) % MGN_MARK_STEPS == 0)
+      x[e] = value1<TYPE>(v.x[e]);
+      delta[e] = value1<TYPE>(v.dt[e]) + bias;
+      y[e] = 0.f, f[e] = 1.f;
+    }
+    if (a.softplus)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (in && g + j < a.cols)
-            store_n<NL, FULL>(a.marks + (t + e) / MGN_MARK_STEPS * C * a.n, at + j * a.n, s, a.n, h[j]);
-      if (fresh[e]) {
+      for (int e = 0; e < STEPS; ++e) delta[e] = softplus(delta[e]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+    for (int e = 0; e < STEPS; ++e) {
+      held = held || (p.ok && delta[e] == 0.f);
+      delta[e] = p.ok ? delta[e] : 0.f;
+    }
+    if constexpr (PASS != LOCAL_ENDS) {
+      if (a.D)
 #pragma unroll
-          for (int k = 0; k < NL; ++k) h[j][k] = 0.f;
-        sum = CUT;
-      }
-      float delta = dt[e] + bias;
-      if (a.softplus) delta = softplus(delta);
-      delta = ok ? delta : 0.f;
-      sum += delta;
-      float d[4], u[4], y[4];
-      quads(delta, d);
-      quads(mul_or_0(delta, x[e]), u);
-      // B may hold anything where a column's step has size 0
-      const auto step = [&](auto held) {
+        for (int e = 0; e < STEPS; ++e) y[e] = D * x[e];
+      if (a.z)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          y[j] = 0.f;
-#pragma unroll
-          for (int k = 0; k < NL; ++k) {
-            const float b = held() ? mul_or_0(u[j], B[e][k]) : u[j] * B[e][k];
-            h[j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), h[j][k], b);
-            if constexpr (PASS != LOCAL_ENDS) y[j] = fmaf(Cn[e][k], h[j][k], y[j]);
-          }
+        for (int e = 0; e < STEPS; ++e) {
+          const float z = value1<TYPE>(v.z[e]);
+          f[e] = z * sigmoid(z);
         }
-      };
-      if (any(ok && delta == 0.f)) step(std::true_type());
-      else step(std::false_type());
-      if constexpr (PASS != LOCAL_ENDS) {
-        float v = quad_sums(y);
-        if (a.D) v = fmaf(D, x[e], v);
-        if (a.z) v *= z[e] * sigmoid(z[e]);
-        if (ok) store1<TYPE>(a.y, (t + e) * C + i, v);
+    }
+    if (a.starts)
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) fresh |= v.fresh[e];
+    const auto step = [&](int e, auto some_held) {
+      float d[4], w[4], r[4], B[NL], Cn[NL];
+      quads(delta[e], d);
+      quads(some_held() ? mul_or_0(delta[e], x[e]) : delta[e] * x[e], w);
+      v.B[e].get(s, a.n, B);
+      if constexpr (PASS != LOCAL_ENDS) v.C[e].get(s, a.n, Cn);
+      else sum += delta[e];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        r[j] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NL; ++k) {
+          const float b = some_held() ? mul_or_0(w[j], B[k]) : w[j] * B[k];
+          h[j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), h[j][k], b);
+          if constexpr (PASS != LOCAL_ENDS) r[j] = fmaf(Cn[k], h[j][k], r[j]);
+        }
+      }
+      if constexpr (PASS != LOCAL_ENDS) y[e] = (quad_sums(r) + y[e]) * f[e];
+    };
+    if (n == STEPS && !fresh && !any(held)) {
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) step(e, std::false_type());
+    } else {
+      // B may hold anything where a column's step has size 0
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) {
+        if (e >= n) break;
+        if (a.starts && v.fresh[e]) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < NL; ++k) h[j][k] = 0.f;
+          sum = CUT;
+        }
+        step(e, std::true_type());
       }
     }
+    if constexpr (PASS != LOCAL_ENDS) {
+      if (p.ok)
+#pragma unroll
+        for (int e = 0; e < STEPS; ++e)
+          if (e < n) store1<TYPE>(py + (e * cb + o), 0, y[e]);
+      py += STEPS * cb;
+    }
+  };
+  In v[2];
+  load(v[0], te - ts);
+  for (int64_t t = ts; t < te; t += 2 * STEPS) {
+    load(v[1], te - (t + STEPS));  // while the steps before run
+    run(v[0], t);
+    if (t + STEPS >= te) break;
+    load(v[0], te - (t + 2 * STEPS));
+    run(v[1], t + STEPS);
   }
   float* const to = PASS == LOCAL_ENDS ? a.state + c * C * a.n : te == a.steps ? a.h_last : nullptr;
   if (to)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (in && g + j < a.cols) store_n<NL, FULL>(to, at + j * a.n, s, a.n, h[j]);
-  if (PASS == LOCAL_ENDS && ok) a.sums[c * C + i] = sum;
+      if (p.in && p.g + j < a.cols) store_n<NL, FULL>(to + p.at0, p.oa + j * a.n, s, a.n, h[j]);
+  if (PASS == LOCAL_ENDS && p.ok) a.sums[c * C + p.i0 + p.o] = sum;
 }
 
 // Chunk by chunk: what enters each, in the place of its own end.  A lane a state.

@@ -48,8 +48,7 @@ struct GroupSums {
   int first;
   bool keeps;
   template <int N, int D>
-  __device__ __forceinline__ void level(float (&v)[M]) {
-    const bool hi = threadIdx.x & D;
+  __device__ __forceinline__ void level(float (&v)[M]) const {
     if constexpr (N > 1) {
 #pragma unroll
       for (int k = 0; k < N / 2; ++k) {
@@ -60,21 +59,29 @@ struct GroupSums {
           const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[k]), __float_as_uint(v[k + N / 2]), false, false);
           v[k] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
         } else {
+          const bool hi = threadIdx.x & D;
           const float mine = hi ? v[k + N / 2] : v[k], other = hi ? v[k] : v[k + N / 2];
           v[k] = mine + across<D>(other);
         }
       }
-      first += hi ? N / 2 : 0;
     } else {
       v[0] += across<D>(v[0]);
-      keeps = keeps && !hi;
     }
     if constexpr (D > 4) level<(N > 1 ? N / 2 : 1), D / 2>(v);
   }
-  __device__ __forceinline__ void operator()(float (&v)[M]) {
+  __device__ __forceinline__ void operator()(float (&v)[M]) const {
+    if constexpr (LG > 0) level<M, 2 << LG>(v);
+  }
+  __device__ __forceinline__ void find() {
     first = 0;
     keeps = true;
-    if constexpr (LG > 0) level<M, 2 << LG>(v);
+    int left = M;
+#pragma unroll
+    for (int d = 2 << LG; d >= 4; d /= 2) {
+      const bool hi = threadIdx.x & d;
+      if (left > 1) left /= 2, first += hi ? left : 0;
+      else keeps = keeps && !hi;
+    }
   }
 };
 
@@ -150,18 +157,25 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
   if (ok) a.sums[c * C + i] = sum;
 }
 
+// Steps of a unit: their states and factors stay in registers between the way forth
+// and the way back.
+constexpr int U = 2, UNITS = K / U;
+static_assert(U == 2 && UNITS >= 2);
+
 template <int TYPE, int NL, int NW, int LG, bool FULL, bool GATE>
-__global__ __launch_bounds__(64 * NW) void ssm_grad_kernel(SsmArgs a) {
-  constexpr int GP = 1 << LG, RPW = 16 / GP;
+__global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
+  constexpr int GP = 1 << LG, RPW = 16 / GP, SIZE = sizeof(Elem<TYPE>);
+  using Sums = GroupSums<2 * NL, LG>;
   __shared__ double accs[4 * NL][64 * NW];
-  __shared__ float red[NW > 1 ? 2 : 1][NW > 1 ? NW : 1][NW > 1 ? K : 1][3][64];
+  __shared__ float subs[UNITS - 2][4 * NL][64 * NW];  // the states before units 1 .. UNITS - 2
+  __shared__ float red[NW > 1 ? 2 : 1][NW > 1 ? NW : 1][NW > 1 ? U : 1][3][64];
   const int lane = threadIdx.x & 63, w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane & 3;
   const int tile = blockIdx.x % a.tiles, sub = (lane >> 2) >> LG;
   const int64_t slot = blockIdx.x / a.tiles;
   const int g = (tile * GP + ((lane >> 2) & (GP - 1))) * 4, col = g + q, s0 = (w * 4 + q) * NL;
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
-  const int64_t C = a.rows * a.cols;
+  const int64_t C = a.rows * a.cols, cb = C * SIZE, rb = a.rows * a.n * SIZE;  // a step's bytes
 
   float A[4][NL];
 #pragma unroll
@@ -175,166 +189,255 @@ __global__ __launch_bounds__(64 * NW) void ssm_grad_kernel(SsmArgs a) {
   const float bias = a.bias && col < a.cols ? a.bias[col] : 0.f, D = a.D && col < a.cols ? a.D[col] : 0.f;
   double dD = 0, d_bias = 0;
   int par = 0;
+  const auto step_size = [&](uint32_t raw, bool ok) {
+    float delta = value1<TYPE>(raw) + bias;
+    if (a.softplus) delta = softplus(delta);
+    return ok ? delta : 0.f;
+  };
 
   for (int64_t r0 = slot * RPW; r0 < a.rows; r0 += a.slots * RPW) {
-    const int64_t row = r0 + sub, i = row * a.cols + col, bn = row * a.n, at = (row * a.cols + g) * a.n;
-    const bool in = row < a.rows && g < a.cols, ok = in && col < a.cols;
-    float G[4][NL];
-    const float* const from = a.chunks > 1 ? a.state + c * C * a.n : a.dh_last;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-      for (int k = 0; k < NL; ++k) G[j][k] = 0.f;
-      if (from && in && g + j < a.cols) load_n<MGN_FP32, NL, FULL>(from, at + j * a.n, s0, a.n, G[j]);
-    }
-    for (int64_t t0 = (te - 1) / K * K; t0 >= ts; t0 -= K) {
-      const int n = te - t0 < K ? (int)(te - t0) : K;
-      float x[K], v[K], delta[K], dy[K], z[K], h[K + 1][4][NL];
-      bool fresh[K];
-#pragma unroll
-      for (int e = 0; e < K; ++e) {
-        x[e] = v[e] = delta[e] = dy[e] = z[e] = 0.f;
-        fresh[e] = false;
-        if (e >= n) continue;
-        if (a.starts) fresh[e] = a.starts[t0 + e];
-        if (ok) {
-          x[e] = load1<TYPE>(a.x, (t0 + e) * C + i);
-          v[e] = load1<TYPE>(a.dt, (t0 + e) * C + i) + bias;
-          dy[e] = load1<TYPE>(a.dy, (t0 + e) * C + i);
-          if (GATE) z[e] = load1<TYPE>(a.z, (t0 + e) * C + i);
-        }
-      }
+    const bool row_in = r0 + sub < a.rows, in = row_in && g < a.cols, ok = in && col < a.cols;
+    // the lane's column, states and n numbers from the wave's first row's on
+    // (lanes without one read that row's first)
+    const uint32_t o = ok ? (uint32_t)(sub * a.cols + col) * SIZE : 0, ob = row_in ? (uint32_t)(sub * a.n) * SIZE : 0;
+    const uint32_t oh = in ? (uint32_t)((sub * a.cols + g) * a.n) : 0;
+    float G[4][NL], h[U + 1][4][NL];
+    const auto load_states = [&](const float* from, float (&v)[4][NL]) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int k = 0; k < NL; ++k) h[0][j][k] = 0.f;
-        if (in && g + j < a.cols) load_n<MGN_FP32, NL, FULL>(a.marks + t0 / K * C * a.n, at + j * a.n, s0, a.n, h[0][j]);
+        for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
+        if (from && in && g + j < a.cols)
+          load_n<MGN_FP32, NL, FULL>(from + r0 * a.cols * a.n, here(oh + j * a.n + s0), 0, a.n - s0, v[j]);
       }
-      // the block's states
+    };
+    load_states(a.chunks > 1 ? a.state + c * C * a.n : a.dh_last, G);
+
+    for (int64_t t0 = (te - 1) / K * K; t0 >= ts; t0 -= K) {
+      const float* const mark = a.marks + t0 / K * C * a.n;
+      const int n = te - t0 < K ? (int)(te - t0) : K, last = (n - 1) / U;  // steps of the block, its last unit
+      const int64_t x0 = (t0 * C + r0 * a.cols) * SIZE, n0 = (t0 * a.rows + r0) * a.n * SIZE;
+      // the states before each unit
+      load_states(mark, h[0]);
+      for (int v = 0; v < last; ++v) {
+        uint32_t rx[U], rd[U], fresh[U];
+        Raw<TYPE, NL, FULL> rB[U];
+        const char *px = (const char*)a.x + x0 + v * U * cb, *pd = (const char*)a.dt + x0 + v * U * cb;
+        const char* pB = (const char*)a.B + n0 + v * U * rb;
 #pragma unroll
-      for (int e = 0; e < K; ++e) {
-        if (e >= n) break;
-        float B[NL];
-#pragma unroll
-        for (int k = 0; k < NL; ++k) B[k] = 0.f;
-        if (in) load_n<TYPE, NL, FULL>(a.B, (t0 + e) * a.rows * a.n + bn, s0, a.n, B);
-        delta[e] = ok ? a.softplus ? softplus(v[e]) : v[e] : 0.f;
-        float d[4], u[4];
-        quads(delta[e], d);
-        quads(mul_or_0(delta[e], x[e]), u);
-        // B may hold anything where a column's step has size 0
-        const auto step = [&](auto first, auto held) {
+        for (int e = 0; e < U; ++e) {
+          rx[e] = raw1<TYPE>(px + e * cb, o);
+          rd[e] = raw1<TYPE>(pd + e * cb, o);
+          rB[e].load(pB + e * rb, ob, s0, a.n);
+          fresh[e] = a.starts ? a.starts[t0 + v * U + e] : 0;
+        }
+        if (v)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int k = 0; k < NL; ++k) {
-              const float b = held() ? mul_or_0(u[j], B[k]) : u[j] * B[k];
-              h[e + 1][j][k] = first() ? b : fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), h[e][j][k], b);
-            }
+            for (int k = 0; k < NL; ++k) subs[v - 1][j * NL + k][threadIdx.x] = h[0][j][k];
+        float delta[U];
+        bool held = false;
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+          delta[e] = step_size(rd[e], ok);
+          held = held || (ok && delta[e] == 0.f);
+        }
+        const auto step = [&](int e, auto slow) {
+          float d[4], u[4], B[NL];
+          rB[e].get(s0, a.n, B);
+          quads(delta[e], d);
+          quads(slow() ? mul_or_0(delta[e], value1<TYPE>(rx[e])) : delta[e] * value1<TYPE>(rx[e]), u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < NL; ++k)  // B may hold anything where a column's step has size 0
+              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && fresh[e] ? 0.f : h[0][j][k],
+                                slow() ? mul_or_0(u[j], B[k]) : u[j] * B[k]);
         };
-        if (fresh[e]) step(std::true_type(), std::true_type());
-        else if (any(ok && delta[e] == 0.f)) step(std::false_type(), std::true_type());
-        else step(std::false_type(), std::false_type());
+        if (!(fresh[0] | fresh[1]) && !any(held)) {
+#pragma unroll
+          for (int e = 0; e < U; ++e) step(e, std::false_type());
+        } else {
+#pragma unroll
+          for (int e = 0; e < U; ++e) step(e, std::true_type());
+        }
       }
-      // and back
       float dA[4][NL], sD = 0.f, sb = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int k = 0; k < NL; ++k) dA[j][k] = 0.f;
-      // the gradients of one column and step, from the sums over all its states
-      const auto finish = [&](int e, float sB, float sA, float y) {
-        const float sg = GATE ? sigmoid(z[e]) : 0.f, o = GATE ? dy[e] * (z[e] * sg) : dy[e];
-        float dx = mul_or_0(delta[e], sB), dd = fmaf(sA, LN2, sB * x[e]);
-        if (a.D) dx = fmaf(D, o, dx), sD = fmaf(o, x[e], sD);
-        if (a.softplus) dd = mul_or_0(sigmoid(v[e]), dd);
-        sb += dd;
-        if (!ok) return;
-        store1<TYPE>(a.dx, (t0 + e) * C + i, dx);
-        store1<TYPE>(a.ddt, (t0 + e) * C + i, dd);
-        if (GATE) {
-          if (a.D) y = fmaf(D, x[e], y);
-          store1<TYPE>(a.dz, (t0 + e) * C + i, dy[e] * y * (sg * fmaf(z[e], 1.f - sg, 1.f)));
+      for (int v = last; v >= 0; --v) {
+        const int m = n - v * U < U ? n - v * U : U;  // the unit's steps
+        const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb, tu = t0 + v * U;
+        uint32_t rx[U], rd[U], ro[U], rz[U], fresh[U];
+        Raw<TYPE, NL, FULL> rB[U], rC[U];
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+          const int64_t i = xu + (e < m ? e : 0) * cb, b = nu + (e < m ? e : 0) * rb;
+          rx[e] = raw1<TYPE>((const char*)a.x + i, o);
+          rd[e] = raw1<TYPE>((const char*)a.dt + i, o);
+          ro[e] = raw1<TYPE>((const char*)a.dy + i, o);
+          if (GATE) rz[e] = raw1<TYPE>((const char*)a.z + i, o);
+          rB[e].load((const char*)a.B + b, ob, s0, a.n);
+          rC[e].load((const char*)a.C + b, ob, s0, a.n);
+          fresh[e] = a.starts ? a.starts[tu + (e < m ? e : 0)] : 0;
         }
-      };
+        if (v != last) {
+          if (v == 0) {
+            load_states(mark, h[0]);
+          } else {
 #pragma unroll
-      for (int e = K - 1; e >= 0; --e) {
-        if (e >= n) continue;
-        float B[NL], Cn[NL];
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int k = 0; k < NL; ++k) B[k] = Cn[k] = 0.f;
-        if (in) {
-          load_n<TYPE, NL, FULL>(a.B, (t0 + e) * a.rows * a.n + bn, s0, a.n, B);
-          load_n<TYPE, NL, FULL>(a.C, (t0 + e) * a.rows * a.n + bn, s0, a.n, Cn);
-        }
-        float d[4], u[4], o[4], sB[4], sA[4], y[4], p[2 * NL];
-        quads(delta[e], d);
-        quads(mul_or_0(delta[e], x[e]), u);
-        quads(GATE ? dy[e] * (z[e] * sigmoid(z[e])) : dy[e], o);
-#pragma unroll
-        for (int k = 0; k < 2 * NL; ++k) p[k] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sB[j] = sA[j] = y[j] = 0.f;
-#pragma unroll
-          for (int k = 0; k < NL; ++k) {
-            const float Gt = fmaf(Cn[k], o[j], G[j][k]);
-            sB[j] = fmaf(Gt, B[k], sB[j]);
-            p[k] = fmaf(Gt, u[j], p[k]);
-            p[NL + k] = fmaf(o[j], h[e + 1][j][k], p[NL + k]);
-            if (GATE) y[j] = fmaf(Cn[k], h[e + 1][j][k], y[j]);
-            G[j][k] = Gt;
+              for (int k = 0; k < NL; ++k) h[0][j][k] = subs[v - 1][j * NL + k][threadIdx.x];
           }
         }
-        if (fresh[e]) {  // nothing passes a start
+        float delta[U], ov[U], f[U][4][NL], tB[U], tA[U], ty[U], p[U][2 * NL];
+        bool held = false;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int k = 0; k < NL; ++k) G[j][k] = 0.f;
-        } else {
+        for (int e = 0; e < U; ++e) {
+          delta[e] = step_size(rd[e], ok);
+          held = held || (ok && delta[e] == 0.f);
+          ov[e] = value1<TYPE>(ro[e]);
+          if (GATE) {
+            const float z = value1<TYPE>(rz[e]);
+            ov[e] *= z * sigmoid(z);
+          }
+          // a step that is not there changes nothing
+          if (!ok || e >= m) delta[e] = ov[e] = 0.f;
+          if (e >= m) fresh[e] = 0;
+        }
+        const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(rx[e])); };
+        const auto forth = [&](int e, auto first, auto some_held) {
+          float d[4], u[4], B[NL];
+          rB[e].get(s0, a.n, B);
+          quads(delta[e], d);
+          quads(input(e), u);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int k = 0; k < NL; ++k) {
-              G[j][k] *= __builtin_amdgcn_exp2f(d[j] * A[j][k]);
+              // B may hold anything where a column's step has size 0
+              const float b = some_held() ? mul_or_0(u[j], B[k]) : u[j] * B[k];
+              f[e][j][k] = first() ? 0.f : __builtin_amdgcn_exp2f(d[j] * A[j][k]);
+              h[e + 1][j][k] = first() ? b : fmaf(f[e][j][k], h[e][j][k], b);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto forth_any = [&](int e) {
+          if (fresh[e]) forth(e, std::true_type(), std::true_type());
+          else forth(e, std::false_type(), std::true_type());
+        };
+        const auto back = [&](int e) {
+          float B[NL], Cn[NL], d[4], u[4], ot[4], sB[4], sA[4], y[4];
+          rB[e].get(s0, a.n, B);
+          rC[e].get(s0, a.n, Cn);
+          quads(delta[e], d);
+          quads(input(e), u);
+          quads(ov[e], ot);
+#pragma unroll
+          for (int k = 0; k < 2 * NL; ++k) p[e][k] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            sB[j] = sA[j] = y[j] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NL; ++k) {
+              const float Gt = fmaf(Cn[k], ot[j], G[j][k]);
+              sB[j] = fmaf(Gt, B[k], sB[j]);
+              p[e][k] = fmaf(Gt, u[j], p[e][k]);
+              p[e][NL + k] = fmaf(ot[j], h[e + 1][j][k], p[e][NL + k]);
+              if (GATE) y[j] = fmaf(Cn[k], h[e + 1][j][k], y[j]);
+              G[j][k] = Gt * f[e][j][k];
               const float wk = G[j][k] * h[e][j][k];
               sA[j] = fmaf(wk, A[j][k], sA[j]);
               dA[j][k] = fmaf(wk, d[j], dA[j][k]);
             }
-        }
-        GroupSums<2 * NL, LG> sums;
-        sums(p);
-        if (row < a.rows && sums.keeps) {
-          const int64_t at_t = (t0 + e) * a.rows + row;
-#pragma unroll
-          for (int k = 0; k < sums.LEFT; ++k) {
-            const int f = sums.first + k, st = s0 + (f < NL ? f : f - NL);
-            if (!FULL && st >= a.n) continue;
-            if (a.tiles > 1) a.bc[(tile * a.steps * a.rows + at_t) * 2 * a.n + (f < NL ? 0 : a.n) + st] = p[k];
-            else store1<TYPE>(f < NL ? a.dB : a.dC, at_t * a.n + st, p[k]);
           }
-        }
-        const float tB = quad_sums(sB), tA = quad_sums(sA), ty = GATE ? quad_sums(y) : 0.f;
-        if constexpr (NW == 1) {
-          finish(e, tB, tA, ty);
+          tB[e] = quad_sums(sB), tA[e] = quad_sums(sA);
+          if (GATE) ty[e] = quad_sums(y);
+          Sums()(p[e]);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto zero = [](float (&v)[4][NL]) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
+        };
+        if (!any(held) && !(fresh[0] | fresh[1])) {
+          forth(0, std::false_type(), std::false_type());
+          forth(1, std::false_type(), std::false_type());
         } else {
-          red[par][w][e][0][lane] = tB, red[par][w][e][1][lane] = tA;
-          if (GATE) red[par][w][e][2][lane] = ty;
+          forth_any(0);
+          forth_any(1);
         }
-      }
-      if constexpr (NW > 1) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < K; ++e) {
-          if (e >= n || e % NW != w) continue;
-          float t[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-          for (int f = 0; f < NW; ++f)
-#pragma unroll
-            for (int k = 0; k < (GATE ? 3 : 2); ++k) t[k] += red[par][f][e][k][lane];
-          finish(e, t[0], t[1], t[2]);
+        // a first step (f = 0) sees no state, whatever the one before it left, and
+        // passes no gradient on
+        if (fresh[1]) zero(h[1]);
+        back(1);
+        if (fresh[1]) {
+          zero(G);
+          forth_any(0);
         }
-        par ^= 1;
+        if (fresh[0]) zero(h[0]);
+        back(0);
+        if (fresh[0]) zero(G);
+        // dB, dC: a number of a step and row in one lane of the wave
+        Sums where;
+        where.find();
+        if (row_in && where.keeps)
+#pragma unroll
+          for (int k = 0; k < Sums::LEFT; ++k) {
+            const int x = where.first + k, st = s0 + (x < NL ? x : x - NL);
+            if (!FULL && st >= a.n) continue;
+#pragma unroll
+            for (int e = 0; e < U; ++e) {
+              if (e >= m) continue;
+              if (a.tiles > 1)
+                write1<MGN_FP32>((char*)a.bc + ((tile * a.steps + tu + e) * a.rows + r0) * 2 * a.n * 4,
+                                 (uint32_t)(sub * 2 * a.n + (x < NL ? 0 : a.n) + st) * 4, p[e][k]);
+              else if (x < NL)
+                write1<TYPE>((char*)a.dB + (nu + e * rb), ob + (uint32_t)(st * SIZE), p[e][k]);
+              else
+                write1<TYPE>((char*)a.dC + (nu + e * rb), ob + (uint32_t)(st * SIZE), p[e][k]);
+            }
+          }
+        if constexpr (NW > 1) {
+#pragma unroll
+          for (int e = 0; e < U; ++e) {
+            red[par][w][e][0][lane] = tB[e], red[par][w][e][1][lane] = tA[e];
+            if (GATE) red[par][w][e][2][lane] = ty[e];
+          }
+          __syncthreads();
+        }
+        // the gradients of one column and step, from the sums over all its states
+        if (ok)
+#pragma unroll
+          for (int e = 0; e < U; ++e) {
+            if (e >= m || (NW > 1 && e % NW != w)) continue;
+            if constexpr (NW > 1) {
+              tB[e] = tA[e] = ty[e] = 0.f;
+#pragma unroll
+              for (int x = 0; x < NW; ++x) {
+                tB[e] += red[par][x][e][0][lane], tA[e] += red[par][x][e][1][lane];
+                if (GATE) ty[e] += red[par][x][e][2][lane];
+              }
+            }
+            const float x = value1<TYPE>(rx[e]);
+            float dx = mul_or_0(delta[e], tB[e]), dd = fmaf(tA[e], LN2, tB[e] * x);
+            if (a.D) dx = fmaf(D, ov[e], dx), sD = fmaf(ov[e], x, sD);
+            if (a.softplus) dd = mul_or_0(sigmoid(value1<TYPE>(rd[e]) + bias), dd);
+            sb += dd;
+            write1<TYPE>((char*)a.dx + (xu + e * cb), o, dx);
+            write1<TYPE>((char*)a.ddt + (xu + e * cb), o, dd);
+            if (GATE) {
+              const float z = value1<TYPE>(rz[e]), s = sigmoid(z), y = a.D ? fmaf(D, x, ty[e]) : ty[e];
+              write1<TYPE>((char*)a.dz + (xu + e * cb), o, value1<TYPE>(ro[e]) * y * (s * fmaf(z, 1.f - s, 1.f)));
+            }
+          }
+        if constexpr (NW > 1) par ^= 1;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -346,7 +449,7 @@ __global__ __launch_bounds__(64 * NW) void ssm_grad_kernel(SsmArgs a) {
     if (ts == 0 && a.dh0)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (in && g + j < a.cols) store_n<NL, FULL>(a.dh0, at + j * a.n, s0, a.n, G[j]);
+        if (in && g + j < a.cols) store_n<NL, FULL>(a.dh0 + r0 * a.cols * a.n, oh + j * a.n, s0, a.n, G[j]);
   }
   if (!a.part) return;
   const int64_t width = (int64_t)a.cols * (a.n + 2);
@@ -363,7 +466,7 @@ __global__ __launch_bounds__(64 * NW) void ssm_grad_kernel(SsmArgs a) {
     t[64 * NW + threadIdx.x] = d_bias;
     __syncthreads();
     dD = d_bias = 0;
-    for (int f = 0; f < NW; ++f) dD += t[f * 64 + lane], d_bias += t[(NW + f) * 64 + lane];
+    for (int m = 0; m < NW; ++m) dD += t[m * 64 + lane], d_bias += t[(NW + m) * 64 + lane];
   }
   if (w == 0 && col < a.cols) {
     dst[(int64_t)a.cols * a.n + col] = (float)dD;
