@@ -20,7 +20,7 @@ namespace mgn {
 namespace {
 
 constexpr int NT = 256;
-enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES };
+enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES, ONE_STEP };
 
 // What some steps bring, as it lies in memory.
 template <int TYPE, int NL, bool FULL, int STEPS>
@@ -31,7 +31,7 @@ struct Inputs {
 
 template <int TYPE, int NL, bool FULL, int PASS>
 __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
-  constexpr int STEPS = NL <= 4 ? 4 : NL == 8 ? 2 : 1;  // steps whose loads are in flight together
+  constexpr int STEPS = PASS == ONE_STEP || NL == 16 ? 1 : NL == 8 ? 2 : 4;  // steps whose loads are in flight together
   using E = Elem<TYPE>;
   using In = Inputs<TYPE, NL, FULL, STEPS>;
   constexpr int SIZE = sizeof(E);
@@ -42,22 +42,6 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
   const int64_t C = a.rows * a.cols, cb = C * SIZE, rb = a.rows * a.n * SIZE;  // a step's bytes
-
-  float h[4][NL], A[4][NL];
-  const float* const from = PASS == FROM_STATES ? a.state + c * C * a.n : PASS == WHOLE_AXIS ? a.h0 : nullptr;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-#pragma unroll
-    for (int k = 0; k < NL; ++k) h[j][k] = A[j][k] = 0.f;
-    if (p.in && p.g + j < a.cols) {
-      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(p.g + j) * a.n, s, a.n, A[j]);
-      if (from) load_n<MGN_FP32, NL, FULL>(from + p.at0, p.oa + j * a.n, s, a.n, h[j]);
-    }
-#pragma unroll
-    for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
-  }
-  const float bias = a.bias && p.ok ? a.bias[p.col] : 0.f, D = a.D && p.ok ? a.D[p.col] : 0.f;
-  float sum = 0.f;
 
   // the next steps to load, and to store
   const int64_t x0 = (ts * C + p.i0) * SIZE, n0 = (ts * a.rows * a.n + p.bn0) * SIZE;
@@ -85,6 +69,27 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
     }
     px += STEPS * cb, pd += STEPS * cb, pz += STEPS * cb, pB += STEPS * rb, pC += STEPS * rb, ps += STEPS;
   };
+  In v[2];
+  load(v[0], te - ts);
+
+  float h[4][NL], A[4][NL];
+  const float* const from = PASS == FROM_STATES ? a.state + c * C * a.n : PASS == LOCAL_ENDS ? nullptr : a.h0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) h[j][k] = A[j][k] = 0.f;
+    if (p.in && p.g + j < a.cols) {
+      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(p.g + j) * a.n, s, a.n, A[j]);
+      if (from) load_n<MGN_FP32, NL, FULL>(from + p.at0, p.oa + j * a.n, s, a.n, h[j]);
+    }
+  }
+  const float bias = a.bias && p.ok ? a.bias[p.col] : 0.f, D = a.D && p.ok ? a.D[p.col] : 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
+  float sum = 0.f;
+
   const auto run = [&](const In& v, int64_t t) {
     const int n = te - t < STEPS ? (int)(te - t) : STEPS;
     if (PASS != LOCAL_ENDS && a.marks && t % MGN_MARK_STEPS == 0)
@@ -169,9 +174,8 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
       py += STEPS * cb;
     }
   };
-  In v[2];
-  load(v[0], te - ts);
-  for (int64_t t = ts; t < te; t += 2 * STEPS) {
+  if constexpr (PASS == ONE_STEP) run(v[0], ts);
+  else for (int64_t t = ts; t < te; t += 2 * STEPS) {
     load(v[1], te - (t + STEPS));  // while the steps before run
     run(v[0], t);
     if (t + STEPS >= te) break;
@@ -186,27 +190,54 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   if (PASS == LOCAL_ENDS && p.ok) a.sums[c * C + p.i0 + p.o] = sum;
 }
 
-// Chunk by chunk: what enters each, in the place of its own end.  A lane a state.
-constexpr int AHEAD = 8;
+// What enters each chunk, in the place of its own end.  A workgroup takes JOIN_S
+// neighbouring states, JOIN_G of its threads to one, each of them AHEAD consecutive
+// chunks at a time: it joins its chunks, the groups join theirs in LDS, and each runs
+// its chunks again from what enters them.  Two latencies for up to 256 chunks.
+constexpr int JOIN_S = 16, JOIN_G = NT / JOIN_S, AHEAD = 16;
 __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* first, bool reverse) {
+  __shared__ float lds[2][JOIN_G][JOIN_S];
   const int64_t C = a.rows * a.cols, S = C * a.n, step = reverse ? -1 : 1;
-  for (int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x; i < S; i += (int64_t)gridDim.x * NT) {
-    const int64_t ch = i / a.n;
+  const int si = threadIdx.x % JOIN_S, gr = threadIdx.x / JOIN_S;
+  for (int64_t i0 = (int64_t)blockIdx.x * JOIN_S; i0 < S; i0 += (int64_t)gridDim.x * JOIN_S) {
+    const int64_t i = i0 + si < S ? i0 + si : S - 1, ch = i / a.n;
+    const bool ok = i0 + si < S;
     const float A = a.A[ch % a.cols * a.n + (i - ch * a.n)] * LOG2E;
     float v = first ? first[i] : 0.f;
-    int64_t c = reverse ? a.chunks - 1 : 0;
-    for (int64_t k = 0; k < a.chunks; k += AHEAD) {
-      float own[AHEAD], sum[AHEAD];
+    for (int64_t k0 = 0; k0 < a.chunks; k0 += JOIN_G * AHEAD) {
+      const int64_t k = k0 + gr * AHEAD, c = reverse ? a.chunks - 1 - k : k;  // chunk k of the order
+      float own[AHEAD], f[AHEAD];
 #pragma unroll
-      for (int e = 0; e < AHEAD; ++e)
-        if (k + e < a.chunks - 1) own[e] = a.state[(c + step * e) * S + i], sum[e] = a.sums[(c + step * e) * C + ch];
+      for (int e = 0; e < AHEAD; ++e) {
+        own[e] = 0.f, f[e] = 0.f;
+        if (k + e < a.chunks - 1) own[e] = a.state[(c + step * e) * S + i], f[e] = a.sums[(c + step * e) * C + ch];
+      }
+      float p = 1.f, q = 0.f;
+      uint32_t cuts = 0;  // chunks in which a trajectory starts
 #pragma unroll
-      for (int e = 0; e < AHEAD; ++e)
-        if (k + e < a.chunks) {
-          a.state[(c + step * e) * S + i] = v;
-          if (k + e < a.chunks - 1) v = sum[e] == CUT ? own[e] : fmaf(__builtin_amdgcn_exp2f(A * sum[e]), v, own[e]);
-        }
-      c += step * AHEAD;
+      for (int e = 0; e < AHEAD; ++e) {
+        const bool here = k + e < a.chunks - 1 && f[e] == CUT;
+        f[e] = k + e < a.chunks - 1 ? __builtin_amdgcn_exp2f(A * f[e]) : 1.f;
+        cuts |= (uint32_t)here << e;
+        q = here ? own[e] : fmaf(f[e], q, own[e]);
+        p *= f[e];
+      }
+      lds[0][gr][si] = cuts ? CUT : p, lds[1][gr][si] = q;
+      __syncthreads();
+      float mine = v;
+#pragma unroll
+      for (int e = 0; e < JOIN_G; ++e) {
+        if (e == gr) mine = v;
+        const float pe = lds[0][e][si], qe = lds[1][e][si];
+        v = pe == CUT ? qe : fmaf(pe, v, qe);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) {
+        if (k + e >= a.chunks) break;
+        if (ok) a.state[(c + step * e) * S + i] = mine;
+        mine = cuts >> e & 1 ? own[e] : fmaf(f[e], mine, own[e]);
+      }
     }
   }
 }
@@ -240,6 +271,7 @@ hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
 
 template <int TYPE>
 hipError_t launch_typed(SsmArgs& a, hipStream_t st) {
+  if (a.steps == 1) return launch_pass<TYPE, ONE_STEP>(a, 1, st);
   if (a.chunks == 1) return launch_pass<TYPE, WHOLE_AXIS>(a, 1, st);
   hipError_t e = launch_pass<TYPE, LOCAL_ENDS>(a, a.chunks - 1, st);
   if (e == hipSuccess) e = launch_ssm_join(a, a.h0, false, st);
@@ -249,7 +281,7 @@ hipError_t launch_typed(SsmArgs& a, hipStream_t st) {
 }  // namespace
 
 int64_t ssm_chunk(int64_t steps, int64_t rows, int cols, int64_t want) {
-  const int64_t waves = (rows * ((cols + 3) / 4) + 15) / 16, least = 4 * MGN_MARK_STEPS;
+  const int64_t waves = (rows * ((cols + 3) / 4) + 15) / 16, least = 2 * MGN_MARK_STEPS;
   int64_t n = want / (waves > 0 ? waves : 1);
   if (n > steps / least) n = steps / least;
   if (n < 2) return steps;
@@ -258,7 +290,7 @@ int64_t ssm_chunk(int64_t steps, int64_t rows, int cols, int64_t want) {
 }
 
 hipError_t launch_ssm_join(const SsmArgs& a, const float* first, bool reverse, hipStream_t st) {
-  const int64_t n = a.rows * a.cols * a.n, b = (n + NT - 1) / NT;
+  const int64_t n = a.rows * a.cols * a.n, b = (n + JOIN_S - 1) / JOIN_S;
   hipLaunchKernelGGL(ssm_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(NT), 0, st, a, first, reverse);
   return hipGetLastError();
 }

@@ -194,6 +194,15 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
     if (a.softplus) delta = softplus(delta);
     return ok ? delta : 0.f;
   };
+  // What a unit's steps bring, as it lies in memory.
+  struct In {
+    uint32_t x[U], dt[U], o[U], z[U], fresh[U];
+    Raw<TYPE, NL, FULL> B[U], C[U];
+  };
+  struct Sweep {
+    uint32_t x[U], dt[U], fresh[U];
+    Raw<TYPE, NL, FULL> B[U];
+  };
 
   for (int64_t r0 = slot * RPW; r0 < a.rows; r0 += a.slots * RPW) {
     const bool row_in = r0 + sub < a.rows, in = row_in && g < a.cols, ok = in && col < a.cols;
@@ -217,20 +226,40 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
       const float* const mark = a.marks + t0 / K * C * a.n;
       const int n = te - t0 < K ? (int)(te - t0) : K, last = (n - 1) / U;  // steps of the block, its last unit
       const int64_t x0 = (t0 * C + r0 * a.cols) * SIZE, n0 = (t0 * a.rows + r0) * a.n * SIZE;
-      // the states before each unit
-      load_states(mark, h[0]);
-      for (int v = 0; v < last; ++v) {
-        uint32_t rx[U], rd[U], fresh[U];
-        Raw<TYPE, NL, FULL> rB[U];
-        const char *px = (const char*)a.x + x0 + v * U * cb, *pd = (const char*)a.dt + x0 + v * U * cb;
-        const char* pB = (const char*)a.B + n0 + v * U * rb;
+      const auto load_unit = [&](int v, In& r) {
+        const int m = n - v * U;
+        const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
-          rx[e] = raw1<TYPE>(px + e * cb, o);
-          rd[e] = raw1<TYPE>(pd + e * cb, o);
-          rB[e].load(pB + e * rb, ob, s0, a.n);
-          fresh[e] = a.starts ? a.starts[t0 + v * U + e] : 0;
+          const int at = e < m ? e : 0;
+          const int64_t i = xu + at * cb, b = nu + at * rb;
+          r.x[e] = raw1<TYPE>((const char*)a.x + i, o);
+          r.dt[e] = raw1<TYPE>((const char*)a.dt + i, o);
+          r.o[e] = raw1<TYPE>((const char*)a.dy + i, o);
+          if (GATE) r.z[e] = raw1<TYPE>((const char*)a.z + i, o);
+          r.B[e].load((const char*)a.B + b, ob, s0, a.n);
+          r.C[e].load((const char*)a.C + b, ob, s0, a.n);
+          r.fresh[e] = a.starts ? a.starts[t0 + v * U + at] : 0;
         }
+      };
+      const auto load_sweep = [&](int v, Sweep& r) {
+        const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb;
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+          r.x[e] = raw1<TYPE>((const char*)a.x + (xu + e * cb), o);
+          r.dt[e] = raw1<TYPE>((const char*)a.dt + (xu + e * cb), o);
+          r.B[e].load((const char*)a.B + (nu + e * rb), ob, s0, a.n);
+          r.fresh[e] = a.starts ? a.starts[t0 + v * U + e] : 0;
+        }
+      };
+      // the states before each unit, its loads in flight while the one before it runs
+      load_states(mark, h[0]);
+      In r;
+      Sweep now, next;
+      if (last) load_sweep(0, now);
+      load_unit(last, r);
+      for (int v = 0; v < last; ++v) {
+        if (v + 1 < last) load_sweep(v + 1, next);
         if (v)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -240,28 +269,29 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         bool held = false;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
-          delta[e] = step_size(rd[e], ok);
+          delta[e] = step_size(now.dt[e], ok);
           held = held || (ok && delta[e] == 0.f);
         }
         const auto step = [&](int e, auto slow) {
           float d[4], u[4], B[NL];
-          rB[e].get(s0, a.n, B);
+          now.B[e].get(s0, a.n, B);
           quads(delta[e], d);
-          quads(slow() ? mul_or_0(delta[e], value1<TYPE>(rx[e])) : delta[e] * value1<TYPE>(rx[e]), u);
+          quads(slow() ? mul_or_0(delta[e], value1<TYPE>(now.x[e])) : delta[e] * value1<TYPE>(now.x[e]), u);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int k = 0; k < NL; ++k)  // B may hold anything where a column's step has size 0
-              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && fresh[e] ? 0.f : h[0][j][k],
+              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && now.fresh[e] ? 0.f : h[0][j][k],
                                 slow() ? mul_or_0(u[j], B[k]) : u[j] * B[k]);
         };
-        if (!(fresh[0] | fresh[1]) && !any(held)) {
+        if (!(now.fresh[0] | now.fresh[1]) && !any(held)) {
 #pragma unroll
           for (int e = 0; e < U; ++e) step(e, std::false_type());
         } else {
 #pragma unroll
           for (int e = 0; e < U; ++e) step(e, std::true_type());
         }
+        now = next;
       }
       float dA[4][NL], sD = 0.f, sb = 0.f;
 #pragma unroll
@@ -271,19 +301,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
       for (int v = last; v >= 0; --v) {
         const int m = n - v * U < U ? n - v * U : U;  // the unit's steps
         const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb, tu = t0 + v * U;
-        uint32_t rx[U], rd[U], ro[U], rz[U], fresh[U];
-        Raw<TYPE, NL, FULL> rB[U], rC[U];
-#pragma unroll
-        for (int e = 0; e < U; ++e) {
-          const int64_t i = xu + (e < m ? e : 0) * cb, b = nu + (e < m ? e : 0) * rb;
-          rx[e] = raw1<TYPE>((const char*)a.x + i, o);
-          rd[e] = raw1<TYPE>((const char*)a.dt + i, o);
-          ro[e] = raw1<TYPE>((const char*)a.dy + i, o);
-          if (GATE) rz[e] = raw1<TYPE>((const char*)a.z + i, o);
-          rB[e].load((const char*)a.B + b, ob, s0, a.n);
-          rC[e].load((const char*)a.C + b, ob, s0, a.n);
-          fresh[e] = a.starts ? a.starts[tu + (e < m ? e : 0)] : 0;
-        }
+        if (v != last) load_unit(v, r);
+        uint32_t(&fresh)[U] = r.fresh;
         if (v != last) {
           if (v == 0) {
             load_states(mark, h[0]);
@@ -294,25 +313,26 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
               for (int k = 0; k < NL; ++k) h[0][j][k] = subs[v - 1][j * NL + k][threadIdx.x];
           }
         }
-        float delta[U], ov[U], f[U][4][NL], tB[U], tA[U], ty[U], p[U][2 * NL];
+        float delta[U], ov[U], sz[U], f[U][4][NL], tB[U], tA[U], ty[U], p[U][2 * NL];
         bool held = false;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
-          delta[e] = step_size(rd[e], ok);
+          delta[e] = step_size(r.dt[e], ok);
           held = held || (ok && delta[e] == 0.f);
-          ov[e] = value1<TYPE>(ro[e]);
+          ov[e] = value1<TYPE>(r.o[e]);
           if (GATE) {
-            const float z = value1<TYPE>(rz[e]);
-            ov[e] *= z * sigmoid(z);
+            const float z = value1<TYPE>(r.z[e]);
+            sz[e] = sigmoid(z);
+            ov[e] *= z * sz[e];
           }
           // a step that is not there changes nothing
           if (!ok || e >= m) delta[e] = ov[e] = 0.f;
           if (e >= m) fresh[e] = 0;
         }
-        const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(rx[e])); };
+        const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(r.x[e])); };
         const auto forth = [&](int e, auto first, auto some_held) {
           float d[4], u[4], B[NL];
-          rB[e].get(s0, a.n, B);
+          r.B[e].get(s0, a.n, B);
           quads(delta[e], d);
           quads(input(e), u);
 #pragma unroll
@@ -332,8 +352,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         };
         const auto back = [&](int e) {
           float B[NL], Cn[NL], d[4], u[4], ot[4], sB[4], sA[4], y[4];
-          rB[e].get(s0, a.n, B);
-          rC[e].get(s0, a.n, Cn);
+          r.B[e].get(s0, a.n, B);
+          r.C[e].get(s0, a.n, Cn);
           quads(delta[e], d);
           quads(input(e), u);
           quads(ov[e], ot);
@@ -425,16 +445,16 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
                 if (GATE) ty[e] += red[par][x][e][2][lane];
               }
             }
-            const float x = value1<TYPE>(rx[e]);
+            const float x = value1<TYPE>(r.x[e]);
             float dx = mul_or_0(delta[e], tB[e]), dd = fmaf(tA[e], LN2, tB[e] * x);
             if (a.D) dx = fmaf(D, ov[e], dx), sD = fmaf(ov[e], x, sD);
-            if (a.softplus) dd = mul_or_0(sigmoid(value1<TYPE>(rd[e]) + bias), dd);
+            if (a.softplus) dd = mul_or_0(sigmoid(value1<TYPE>(r.dt[e]) + bias), dd);
             sb += dd;
             write1<TYPE>((char*)a.dx + (xu + e * cb), o, dx);
             write1<TYPE>((char*)a.ddt + (xu + e * cb), o, dd);
             if (GATE) {
-              const float z = value1<TYPE>(rz[e]), s = sigmoid(z), y = a.D ? fmaf(D, x, ty[e]) : ty[e];
-              write1<TYPE>((char*)a.dz + (xu + e * cb), o, value1<TYPE>(ro[e]) * y * (s * fmaf(z, 1.f - s, 1.f)));
+              const float z = value1<TYPE>(r.z[e]), s = sz[e], y = a.D ? fmaf(D, x, ty[e]) : ty[e];
+              write1<TYPE>((char*)a.dz + (xu + e * cb), o, value1<TYPE>(r.o[e]) * y * (s * fmaf(z, 1.f - s, 1.f)));
             }
           }
         if constexpr (NW > 1) par ^= 1;
@@ -494,7 +514,7 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a backward is dealt, and its scratch.
 struct Deal {
-  int lg, tiles, waves;  // groups of a tile (their logarithm), tiles of a row, waves of a workgroup
+  int lg, tiles;  // groups of a tile (their logarithm), tiles of a row
   int64_t chunk, chunks, slots, parts;
   size_t state, sums, bc, part, all;
 };
@@ -503,7 +523,6 @@ Deal deal(int64_t steps, int64_t rows, int cols, int n) {
   const int per_row = (cols + 3) / 4;
   d.lg = per_row == 1 ? 0 : per_row <= 4 ? 2 : 4;
   d.tiles = (per_row + (1 << d.lg) - 1) >> d.lg;
-  d.waves = n <= 16 ? 1 : n <= 32 ? 2 : 4;
   const int rpw = 16 >> d.lg;
   d.chunk = ssm_chunk(steps, rows, cols, CHUNK_WAVES);
   d.chunks = (steps + d.chunk - 1) / d.chunk;

@@ -174,18 +174,19 @@ def test_a_trajectory_that_is_not_finite_ends_at_a_start(T, rows, cols, n):
 def test_windows_and_single_steps_are_the_whole(dtype):
     """Window by window, and step by step with the states updated in place; the
     windows' backward hands dh0 on, in place too."""
-    T, rows, cols, n = 48, 40, 64, 16
+    T, rows, cols, n = 31, 40, 64, 16
     c = _case(T, rows, cols, n, dtype, seed=7)
+    assert mgn.mgn_selective_scan_work(T, rows, cols, n) == 0  # (chunks would add in another order)
     y, last, marks = _forward(c)
     g = _backward(c, marks)
-    for cuts in (list(range(T + 1)), [0, 8, 16, 17, 48]):
+    for cuts in (list(range(T + 1)), [0, 8, 16, 17, 31]):
         h, ys = c["h0"].clone(), []
         for a, b in zip(cuts, cuts[1:]):
             ys.append(torch.empty_like(c["x"][a:b]))
             p = {k: (c[k][a:b] if k in ("x", "dt", "B", "C", "z") else c[k]) for k in c}
             mgn.mgn_selective_scan(p["x"], p["dt"], p["A"], p["B"], p["C"], ys[-1], h0=h, h_last=h, **_args(p))
         assert torch.equal(torch.cat(ys), y) and torch.equal(h, last)
-    cuts, d, dA = [0, 8, 32, 48], c["dh_last"].clone(), None
+    cuts, d, dA = [0, 8, 24, 31], c["dh_last"].clone(), None
     hs = [c["h0"]]
     parts = []
     for a, b in zip(cuts, cuts[1:]):
