@@ -24,15 +24,15 @@ constexpr int64_t NORM_WGS_MANY = 256;     // with several
 constexpr int64_t FOLD = 4096;             // partials above which a launch of their own adds them
 constexpr int64_t CLIP_WGS = 4096;
 
-// The tensor that holds a tile.
+// The tensor that holds a tile: how many of the tensors begin at or before it, each
+// lane counting for its own ones.
 __device__ __forceinline__ int tensor_of(const GradTable& t, uint32_t tile) {
-  int lo = 0, hi = t.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (t.first[mid] <= tile) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < GRAD_TABLE; k += 64)
+    n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k + lane < t.count && t.first[k + lane] <= tile));
+  return n - 1;
 }
 
 __device__ __forceinline__ double wave_sum(double v) {

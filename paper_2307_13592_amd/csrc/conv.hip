@@ -14,25 +14,26 @@
 // again from the inputs that it holds.
 #include <type_traits>
 
-#include "kernels.h"
-#include "rows8.h"
+#include "raw.h"
 
 namespace mgn {
 namespace {
 
 constexpr int NT = 256, MAX_W = MGN_CONV_MAX_WIDTH;
 
-// V neighbouring elements; V = 1, or a run of 4 or 8 on its own boundary.
+// V neighbouring elements; V = 1, or a run of 4 on its own boundary.
 template <int TYPE, int V>
 __device__ __forceinline__ void load(const void* p, int64_t i, float (&v)[V]) {
   get<V>((const Elem<TYPE>*)p + i, v);
 }
 template <int TYPE, int V>
 __device__ __forceinline__ void store(void* p, int64_t i, const float (&v)[V]) {
-  put<V>((Elem<TYPE>*)p + i, v);
+  if constexpr (TYPE == MGN_BF16 && V == 4)
+    __builtin_nontemporal_store((uint64_t)pack_bf16(v[0], v[1]) | (uint64_t)pack_bf16(v[2], v[3]) << 32,
+                                (uint64_t*)((uint16_t*)p + i));
+  else
+    put<V>((Elem<TYPE>*)p + i, v);
 }
-
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
 // A thread's place: its columns from c on, and its rows r, r + rows_wg * gridDim.x, ...
 template <int V>
@@ -58,14 +59,20 @@ __device__ __forceinline__ int age_at(const uint8_t* starts, int64_t t) {
   return n;
 }
 
+// The weights of V neighbouring columns lie one behind the other.
 template <int W, int V>
 __device__ __forceinline__ void load_taps(const ConvArgs& a, int c, bool ok, float (&w)[W][V], float (&b)[V]) {
+  float all[V * W];
+  const float* const p = a.w + (ok ? (int64_t)c * W : 0);
+  constexpr int RUN = V * W % 4 == 0 ? 4 : 1;
 #pragma unroll
-  for (int k = 0; k < V; ++k) b[k] = a.b && ok ? a.b[c + k] : 0.f;
+  for (int k = 0; k < V * W; k += RUN) get<RUN>(p + k, all + k);
 #pragma unroll
-  for (int j = 0; j < W; ++j)
+  for (int k = 0; k < V; ++k) {
+    b[k] = a.b ? a.b[ok ? c + k : k] : 0.f;
 #pragma unroll
-    for (int k = 0; k < V; ++k) w[j][k] = ok ? a.w[(int64_t)(c + k) * W + j] : 0.f;
+    for (int j = 0; j < W; ++j) w[j][k] = all[k * W + j];
+  }
 }
 
 // Inputs t0 - (W - 1) .. t0 - 1 of a row, oldest first.
@@ -101,7 +108,28 @@ __device__ __forceinline__ void taps(const float (*xs)[V], const float (&w)[W][V
   }
 }
 
-template <int TYPE, int W, int V, int STEPS>
+// What some steps bring, as it lies in memory; N arrays.  PAST: read past the caches.
+template <int TYPE, int V, int STEPS, int N, bool PAST>
+struct Inputs {
+  Raw<TYPE, V, true> v[N][STEPS];
+  uint32_t fresh[STEPS];
+  // steps t .. of those before `end` (the last of them again for those that are not)
+  __device__ __forceinline__ void load(const ConvArgs& a, const void* x, const void* y, int64_t t, int64_t end, int64_t C,
+                                       int64_t i) {
+    if (t >= end) return;
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e) {
+      const int64_t s = t + e < end ? t + e : end - 1;
+      const char* const p = (const char*)x + (s * C + i) * (int64_t)sizeof(Elem<TYPE>);
+      if constexpr (PAST) v[0][e].stream(p);
+      else v[0][e].load(p, 0, 0, V);
+      if constexpr (N > 1) v[1][e].load((const char*)y + (s * C + i) * (int64_t)sizeof(Elem<TYPE>), 0, 0, V);
+      fresh[e] = a.starts ? a.starts[s] : 0;
+    }
+  }
+};
+
+template <int TYPE, int W, int V, int STEPS, bool PAST>
 __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
   const Place<V> p(a);
   const int64_t C = a.rows * a.cols;
@@ -113,21 +141,19 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V];
+    Inputs<TYPE, V, STEPS, 1, PAST> now, next;
+    now.load(a, a.x, nullptr, t0, t1, C, i);
     load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
     int age = age_at<W>(a.starts, t0 - 1);
     for (int64_t t = t0; t < t1; t += STEPS) {
-      bool fresh[STEPS];
+      next.load(a, a.x, nullptr, t + STEPS, t1, C, i);  // while these steps run
+      const int n = t1 - t < STEPS ? (int)(t1 - t) : STEPS;
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) now.v[0][e].get(0, V, xs[W - 1 + e]);
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
-        fresh[e] = a.starts && t + e < t1 && a.starts[t + e];
-#pragma unroll
-        for (int k = 0; k < V; ++k) xs[W - 1 + e][k] = 0.f;
-        if (ok && t + e < t1) load<TYPE, V>(a.x, (t + e) * C + i, xs[W - 1 + e]);
-      }
-#pragma unroll
-      for (int e = 0; e < STEPS; ++e) {
-        if (t + e >= t1) break;
-        age = fresh[e] ? 0 : age < W ? age + 1 : W;
+        if (e >= n) break;
+        age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
         float v[V];
         taps<W, V>(xs + e, w, b, age, v);
         if (a.silu) {
@@ -136,21 +162,15 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
         }
         if (ok) store<TYPE, V>(a.y, (t + e) * C + i, v);
       }
-      const int n = t1 - t < STEPS ? (int)(t1 - t) : STEPS;  // the last W - 1 inputs to the front
-      if (n == STEPS) {
+      // the last W - 1 inputs to the front
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j)
+      for (int e = 1; e <= STEPS; ++e)
+        if (e == n)
 #pragma unroll
-          for (int k = 0; k < V; ++k) xs[j][k] = xs[STEPS + j][k];
-      } else {
+          for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-        for (int e = 1; e < STEPS; ++e)
-          if (e == n)
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-              for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k];
-      }
+            for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k];
+      now = next;
     }
     if (a.past_out && ok && s + 1 == a.segs) {
       // what the next window's steps see: nothing from before the last start
@@ -166,20 +186,31 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
 }
 
 // The backward; a.y is dx.  A thread's sums of dw and db go over all its items, in
-// fp32 over STEPS steps and in fp64 over these.
+// fp32 over SUM_STEPS steps and in fp64 over these.
+constexpr int SUM_STEPS = 8;
 template <int TYPE, int W, int V, int STEPS>
 __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
+  static_assert(SUM_STEPS % STEPS == 0);
   const Place<V> p(a);
   const int64_t C = a.rows * a.cols;
-  float w[W][V], b[V];
+  float w[W][V], b[V], sw[W][V], sb[V];
   load_taps<W, V>(a, p.c, p.ok, w, b);
   double dw[W][V], db[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    db[k] = 0;
+    db[k] = 0, sb[k] = 0.f;
 #pragma unroll
-    for (int j = 0; j < W; ++j) dw[j][k] = 0;
+    for (int j = 0; j < W; ++j) dw[j][k] = 0, sw[j][k] = 0.f;
   }
+  const auto add = [&] {
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      db[k] += sb[k], sb[k] = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) dw[j][k] += sw[j][k], sw[j][k] = 0.f;
+    }
+  };
+  int turn = 0;
   for (int64_t item = blockIdx.x; item < a.groups * a.segs; item += gridDim.x) {
     const int64_t s = item / a.groups, r = (item - s * a.groups) * p.per + p.r;
     const int64_t t0 = s * a.seg, t1 = s + 1 == a.segs ? a.steps : t0 + a.seg;
@@ -187,6 +218,8 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V], g[W - 1 + STEPS][V];  // g[j]: gradient of the input of xs[j]
+    Inputs<TYPE, V, STEPS, 2, false> now, next;
+    now.load(a, a.x, a.dy, t0, te, C, i);
     load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
@@ -200,30 +233,23 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
       else if (t < 0 && a.d_past) store<MGN_FP32, V>(a.d_past, (t + W - 1) * C + i, v);
     };
     for (int64_t t = t0; t < te; t += STEPS) {
+      next.load(a, a.x, a.dy, t + STEPS, te, C, i);  // while these steps run
+      const int n = te - t < STEPS ? (int)(te - t) : STEPS;
       float d[STEPS][V];
-      bool fresh[STEPS];
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
-        fresh[e] = a.starts && t + e < te && a.starts[t + e];
+        now.v[0][e].get(0, V, xs[W - 1 + e]);
+        now.v[1][e].get(0, V, d[e]);
 #pragma unroll
-        for (int k = 0; k < V; ++k) xs[W - 1 + e][k] = d[e][k] = g[W - 1 + e][k] = 0.f;
-        if (ok && t + e < te) {
-          load<TYPE, V>(a.x, (t + e) * C + i, xs[W - 1 + e]);
-          load<TYPE, V>(a.dy, (t + e) * C + i, d[e]);
+        for (int k = 0; k < V; ++k) {
+          g[W - 1 + e][k] = 0.f;
+          if (!ok) xs[W - 1 + e][k] = d[e][k] = 0.f;
         }
       }
-      float sw[W][V], sb[V];
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        sb[k] = 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) sw[j][k] = 0.f;
-      }
-      const int n = te - t < STEPS ? (int)(te - t) : STEPS;
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
-        age = fresh[e] ? 0 : age < W ? age + 1 : W;
+        age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
         if (a.silu) {
           float v[V];
           taps<W, V>(xs + e, w, b, age, v);
@@ -247,12 +273,7 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
           for (int k = 0; k < V; ++k) sb[k] += d[e][k];
         out(t + e - (W - 1), g[e]);
       }
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        db[k] += sb[k];
-#pragma unroll
-        for (int j = 0; j < W; ++j) dw[j][k] += sw[j][k];
-      }
+      if (++turn % (SUM_STEPS / STEPS) == 0) add();
 #pragma unroll
       for (int e = 1; e <= STEPS; ++e)
         if (e == n)
@@ -260,6 +281,7 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
           for (int j = 0; j < W - 1; ++j)
 #pragma unroll
             for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k], g[j][k] = g[e + j][k];
+      now = next;
     }
     if (s + 1 == a.segs) {
       // the inputs that steps after the last one see
@@ -276,6 +298,7 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
     }
   }
   if (!a.part) return;
+  add();
   // the workgroup's rows, one behind the other, in fp64
   __shared__ double lds[NT];
   const int64_t width = (int64_t)a.cols * (W + 1);
@@ -326,6 +349,10 @@ __global__ __launch_bounds__(NT) void past_tail_kernel(ConvArgs a, int W) {
 
 constexpr int64_t FWD_WGS = 4096;   // workgroups that a forward launch wants
 constexpr int64_t MOST_WGS = 1 << 20;
+// A forward that moves more than the last-level cache holds reads past it: 20 steps of
+// 100,003 x 64 bf16 115 us through it, 108 past it; its backward 352 and 354 (600 steps
+// of 1,885 x 128 fp32).
+constexpr int64_t CACHE = (int64_t)256 << 20;
 constexpr int64_t LEAST_SEG = 32;   // steps of a segment
 
 int64_t type_size(int type) { return type == MGN_FP32 ? 4 : 2; }
@@ -339,7 +366,7 @@ void deal(ConvArgs& a, int V, int64_t want) {
   const int per = NT / a.lanes;
   a.groups = (a.rows + per - 1) / per;
   const int64_t have = a.groups * a.tiles, most = a.steps / LEAST_SEG;
-  a.segs = (want + have - 1) / have;
+  a.segs = want / have;
   a.segs = a.segs < most ? a.segs : most;
   if (a.segs < 1) a.segs = 1;
   a.seg = (a.steps + a.segs - 1) / a.segs;
@@ -347,8 +374,6 @@ void deal(ConvArgs& a, int V, int64_t want) {
   if (a.segs > 1 && a.steps - (a.segs - 1) * a.seg < MAX_W) --a.segs;  // the last one takes its few steps too
 }
 
-template <int W>
-using Int = std::integral_constant<int, W>;
 template <class F>
 hipError_t by_width(int width, F f) {
   switch (width) {
@@ -374,22 +399,23 @@ hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
   const int64_t past_bytes = (width - 1) * C * type_size(type);
   if (a.steps <= 0)
     return a.past_out && a.past_out != a.past ? copy_bytes(a.past, a.past_out, past_bytes, st) : hipSuccess;
-  const int run = type == MGN_BF16 ? 8 : 4;
-  const bool vec = a.cols % run == 0 && at(a.x, 16) && at(a.y, 16) && at(a.past, 16) && at(a.past_out, 16);
+  const int run = 4, edge = run * type_size(type);
+  const bool vec = a.cols % run == 0 && at(a.x, edge) && at(a.y, edge) && at(a.past, edge) && at(a.past_out, edge);
   deal(a, vec ? run : 1, FWD_WGS);
+  const bool past = 2 * a.steps * C * type_size(type) > CACHE;
   const bool tail = a.past_out && a.past_out == a.past && a.segs > 1;
   ConvArgs m = a;
   if (tail) m.past_out = nullptr;
   const int64_t items = a.groups * a.segs;
   const dim3 grid((unsigned)(items < MOST_WGS ? items : MOST_WGS), (unsigned)a.tiles);
   const hipError_t e = by_width(width, [&](auto w) {
-    if (type == MGN_BF16) {
-      if (vec) hipLaunchKernelGGL((conv_kernel<MGN_BF16, w(), 8, 4>), grid, dim3(NT), 0, st, m);
-      else hipLaunchKernelGGL((conv_kernel<MGN_BF16, w(), 1, 8>), grid, dim3(NT), 0, st, m);
-    } else {
-      if (vec) hipLaunchKernelGGL((conv_kernel<MGN_FP32, w(), 4, 4>), grid, dim3(NT), 0, st, m);
-      else hipLaunchKernelGGL((conv_kernel<MGN_FP32, w(), 1, 8>), grid, dim3(NT), 0, st, m);
-    }
+    const auto go = [&](auto ty) {
+      if (vec && past) hipLaunchKernelGGL((conv_kernel<ty(), w(), 4, 4, true>), grid, dim3(NT), 0, st, m);
+      else if (vec) hipLaunchKernelGGL((conv_kernel<ty(), w(), 4, 4, false>), grid, dim3(NT), 0, st, m);
+      else hipLaunchKernelGGL((conv_kernel<ty(), w(), 1, 8, false>), grid, dim3(NT), 0, st, m);
+    };
+    if (type == MGN_BF16) go(Int<MGN_BF16>());
+    else go(Int<MGN_FP32>());
     return hipGetLastError();
   });
   if (e != hipSuccess || !tail || width < 2) return e;

@@ -1,0 +1,75 @@
+// Loads held as they lie in memory while other steps run, and the accesses of a lane
+// at a 32-bit offset from its wave's address (gfx950).
+#pragma once
+#include <type_traits>
+
+#include "kernels.h"
+#include "rows8.h"
+
+namespace mgn {
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+
+// A lane's offset as the compiler finds it here: it is then added by the access
+// itself, to a scalar address, and not beforehand to every array's, which would take
+// two registers for each of them.
+__device__ __forceinline__ uint32_t here(uint32_t o) {
+  asm volatile("" : "+v"(o));
+  return o;
+}
+// The element at byte `o` from a wave's base: a scalar address and a 32-bit offset.
+template <int TYPE>
+__device__ __forceinline__ uint32_t raw1(const char* base, uint32_t o) {
+  o = here(o);
+  if constexpr (TYPE == MGN_BF16) return *(const uint16_t*)(base + o);
+  else return *(const uint32_t*)(base + o);
+}
+template <int TYPE>
+__device__ __forceinline__ float value1(uint32_t w) {
+  return __uint_as_float(TYPE == MGN_BF16 ? w << 16 : w);
+}
+template <int TYPE>
+__device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
+  if constexpr (TYPE == MGN_BF16) *(uint16_t*)(base + here(o)) = (uint16_t)pack_bf16(v, 0.f);
+  else *(float*)(base + here(o)) = v;
+}
+// NL numbers as they lie in memory, so that a load in flight is not waited for
+// before its step comes: numbers s .. of the n at byte o.
+template <int TYPE, int NL, bool FULL>
+struct Raw {
+  static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = FULL ? (NL * SIZE + 3) / 4 : NL;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const char* base, uint32_t o, int s, int n) {
+    if constexpr (FULL) {
+      __builtin_memcpy(w, base + here(o + (uint32_t)(s * SIZE)), NL * SIZE);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NL; ++k) w[k] = raw1<TYPE>(base, o + (uint32_t)((s + k < n ? s + k : n - 1) * SIZE));
+    }
+  }
+  // All numbers at p, past the caches.
+  __device__ __forceinline__ void stream(const char* p) {
+    if constexpr (WORDS == 2) {
+      const uint64_t u = __builtin_nontemporal_load((const uint64_t*)p);
+      w[0] = (uint32_t)u, w[1] = (uint32_t)(u >> 32);
+    } else {
+      static_assert(WORDS == 4);
+      const uintx4 u = __builtin_nontemporal_load((const uintx4*)p);
+      w[0] = u[0], w[1] = u[1], w[2] = u[2], w[3] = u[3];
+    }
+  }
+  __device__ __forceinline__ void get(int s, int n, float (&v)[NL]) const {
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      if constexpr (TYPE != MGN_BF16) v[k] = __uint_as_float(w[k]);
+      else if constexpr (!FULL) v[k] = __uint_as_float(w[k] << 16);
+      else v[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+      if constexpr (!FULL) v[k] = s + k < n ? v[k] : 0.f;
+    }
+  }
+};
+
+}  // namespace mgn

@@ -11,7 +11,7 @@
 #include <type_traits>
 
 #include "kernels.h"
-#include "rows8.h"
+#include "raw.h"
 
 namespace mgn {
 
@@ -21,8 +21,6 @@ constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 __device__ __forceinline__ float mul_or_0(float a, float b) { return a == 0.f ? 0.f : a * b; }
 // Whether any lane of the wave says so.
 __device__ __forceinline__ bool any(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
-
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
 // log(1 + e^v), to a few half-steps of itself at any v: with e = e^-|v| the
 // logarithm of 1 + e is 2 atanh(s), s = e / (2 + e), an odd series in s <= 1 / 3
@@ -81,54 +79,6 @@ __device__ __forceinline__ void load_n(const void* p, int64_t i, int s, int n, f
   }
 }
 
-// A lane's offset as the compiler finds it here: it is then added by the access
-// itself, to a scalar address, and not beforehand to every array's, which would take
-// two registers for each of them.
-__device__ __forceinline__ uint32_t here(uint32_t o) {
-  asm volatile("" : "+v"(o));
-  return o;
-}
-// The element at byte `o` from a wave's base: a scalar address and a 32-bit offset.
-template <int TYPE>
-__device__ __forceinline__ uint32_t raw1(const char* base, uint32_t o) {
-  o = here(o);
-  if constexpr (TYPE == MGN_BF16) return *(const uint16_t*)(base + o);
-  else return *(const uint32_t*)(base + o);
-}
-template <int TYPE>
-__device__ __forceinline__ float value1(uint32_t w) {
-  return __uint_as_float(TYPE == MGN_BF16 ? w << 16 : w);
-}
-template <int TYPE>
-__device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
-  if constexpr (TYPE == MGN_BF16) *(uint16_t*)(base + here(o)) = (uint16_t)pack_bf16(v, 0.f);
-  else *(float*)(base + here(o)) = v;
-}
-// NL numbers as they lie in memory, so that a load in flight is not waited for
-// before its step comes: numbers s .. of the n at byte o.
-template <int TYPE, int NL, bool FULL>
-struct Raw {
-  static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = FULL ? (NL * SIZE + 3) / 4 : NL;
-  uint32_t w[WORDS];
-  __device__ __forceinline__ void load(const char* base, uint32_t o, int s, int n) {
-    if constexpr (FULL) {
-      __builtin_memcpy(w, base + here(o + (uint32_t)(s * SIZE)), NL * SIZE);
-    } else {
-#pragma unroll
-      for (int k = 0; k < NL; ++k) w[k] = raw1<TYPE>(base, o + (uint32_t)((s + k < n ? s + k : n - 1) * SIZE));
-    }
-  }
-  __device__ __forceinline__ void get(int s, int n, float (&v)[NL]) const {
-#pragma unroll
-    for (int k = 0; k < NL; ++k) {
-      if constexpr (TYPE != MGN_BF16) v[k] = __uint_as_float(w[k]);
-      else if constexpr (!FULL) v[k] = __uint_as_float(w[k] << 16);
-      else v[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-      if constexpr (!FULL) v[k] = s + k < n ? v[k] : 0.f;
-    }
-  }
-};
-
 // Where a lane's groups and columns lie: the wave's first ones (the same for all of
 // its lanes, so that addresses are a scalar and a lane's 32-bit offset), and the
 // lane's from there.
@@ -173,8 +123,5 @@ __device__ __forceinline__ void store_n(float* p, int64_t i, int s, int n, const
 
 // A chunk in which a trajectory starts: what enters it does not reach its end.
 constexpr float CUT = -INFINITY;
-
-template <int N>
-using Int = std::integral_constant<int, N>;
 
 }  // namespace mgn
