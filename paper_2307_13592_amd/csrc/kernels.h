@@ -240,16 +240,20 @@ struct SsmArgs {
   int tiles;  // backward: column tiles of a row
 };
 // A list of tensors (clip.hip), at most GRAD_TABLE of them a launch: tiles of
-// GRAD_TILE elements, tensor k's being first[k] .. first[k + 1] - 1.
-constexpr int GRAD_TABLE = 128;
+// GRAD_TILE elements, tensor k's being first[k] .. first[k + 1] - 1, the last of them
+// holding rem[k] + 1.  It goes with the kernel's arguments, which hold 4 KB, so
+// addresses take 48 bits.
+constexpr int GRAD_TABLE = 208;
 constexpr int64_t GRAD_TILE = 8192;
 struct GradTable {
-  const void* g[GRAD_TABLE];
-  void* out[GRAD_TABLE];
-  int64_t n[GRAD_TABLE];
-  uint32_t first[GRAD_TABLE + 1];
-  uint32_t bf16[GRAD_TABLE / 32];  // a bit for each tensor
+  uint32_t g_lo[GRAD_TABLE], out_lo[GRAD_TABLE], first[GRAD_TABLE + 1];
+  uint16_t g_hi[GRAD_TABLE], out_hi[GRAD_TABLE], rem[GRAD_TABLE];
+  uint32_t bf16[(GRAD_TABLE + 31) / 32];  // a bit for each tensor
   int count;
+  __host__ __device__ char* g(int k) const { return (char*)((uint64_t)g_hi[k] << 32 | g_lo[k]); }
+  __host__ __device__ char* out(int k) const { return (char*)((uint64_t)out_hi[k] << 32 | out_lo[k]); }
+  __host__ __device__ bool is_bf16(int k) const { return bf16[k / 32] >> (k % 32) & 1; }
+  __host__ __device__ int64_t n(int k) const { return (int64_t)(first[k + 1] - first[k] - 1) * GRAD_TILE + rem[k] + 1; }
 };
 // Gated recurrence (scan.hip): [steps][rows][cols] arrays, states [rows][cols].
 struct ScanArgs {

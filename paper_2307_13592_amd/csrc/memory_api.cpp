@@ -333,9 +333,9 @@ mgn_status grads_checked(const char* fn, const mgn_grads* list, const float* nor
   if (clash({to(norm, 4), to(work, (int64_t)need)})) return bad(fn, "overlapping arrays");
   for (const GradTable& t : list->tables)
     for (int k = 0; k < t.count; ++k) {
-      const int64_t b = t.n[k] * (t.bf16[k / 32] >> (k % 32) & 1 ? 2 : 4);
+      const int64_t b = t.n(k) * (t.is_bf16(k) ? 2 : 4);
       for (const Span& s : {to(norm, 4), to(work, (int64_t)need)})
-        if (touch(s, rd(t.g[k], b)) || touch(s, rd(t.out[k], b))) return bad(fn, "overlapping arrays");
+        if (touch(s, rd(t.g(k), b)) || touch(s, rd(t.out(k), b))) return bad(fn, "overlapping arrays");
     }
   return MGN_OK;
 }
@@ -353,6 +353,7 @@ mgn_status mgn_grads_create(const mgn_grad* tensors, int64_t count, mgn_grads** 
     if (!float_type(t.type)) return bad(fn, "unknown storage type");
     if (!size_ok(t.n, 1) || t.n / GRAD_TILE >= 1 << 24) return bad(fn, "bad sizes");
     if (t.n > 0 && !t.grad) return bad(fn, "NULL argument");
+    if (((uint64_t)t.grad | (uint64_t)t.out) >> 48) return bad(fn, "not a device address");
     if (!aligned(t.grad, type_size(t.type)) || !aligned(t.out, type_size(t.type))) return bad(fn, "misaligned pointer");
   }
   mgn_grads* list = nullptr;
@@ -365,9 +366,10 @@ mgn_status mgn_grads_create(const mgn_grad* tensors, int64_t count, mgn_grads** 
       if (list->tables.empty() || list->tables.back().count == GRAD_TABLE) list->tables.emplace_back(GradTable{});
       GradTable& to = list->tables.back();
       const int i = to.count++;
-      to.g[i] = t.grad;
-      to.out[i] = t.out ? t.out : const_cast<void*>(t.grad);
-      to.n[i] = t.n;
+      const uint64_t g = (uint64_t)t.grad, out = t.out ? (uint64_t)t.out : g;
+      to.g_lo[i] = (uint32_t)g, to.g_hi[i] = (uint16_t)(g >> 32);
+      to.out_lo[i] = (uint32_t)out, to.out_hi[i] = (uint16_t)(out >> 32);
+      to.rem[i] = (uint16_t)((t.n - 1) % GRAD_TILE);
       to.first[i + 1] = to.first[i] + (uint32_t)((t.n + GRAD_TILE - 1) / GRAD_TILE);
       if (t.type == MGN_BF16) to.bf16[i / 32] |= 1u << (i % 32);
     }
