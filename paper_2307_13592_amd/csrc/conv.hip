@@ -4,7 +4,7 @@
 //   d_t = dy_t act'(v_t),  dx_t = sum_k w[W - 1 - k] d_{t+k},
 //   dw[W - 1 - k] = sum d_t x_{t-k},  db = sum d_t.
 //
-// A lane holds V neighbouring columns of a row and goes through time with the last
+// A lane holds V columns of a row and goes through time with the last
 // W - 1 inputs in registers, STEPS steps' loads in flight together, so that each
 // input is read once.  A workgroup takes as many rows as it has lanes for and, with
 // many rows, all steps of them; with fewer the time axis is cut into segments,
@@ -21,30 +21,51 @@ namespace {
 
 constexpr int NT = 256, MAX_W = MGN_CONV_MAX_WIDTH;
 
-// V neighbouring elements; V = 1, or a run of 4 on its own boundary.
-template <int TYPE, int V>
-__device__ __forceinline__ void load(const void* p, int64_t i, float (&v)[V]) {
-  get<V>((const Elem<TYPE>*)p + i, v);
-}
-template <int TYPE, int V>
-__device__ __forceinline__ void store(void* p, int64_t i, const float (&v)[V]) {
-  if constexpr (TYPE == MGN_BF16 && V == 4)
-    __builtin_nontemporal_store((uint64_t)pack_bf16(v[0], v[1]) | (uint64_t)pack_bf16(v[2], v[3]) << 32,
-                                (uint64_t*)((uint16_t*)p + i));
-  else
-    put<V>((Elem<TYPE>*)p + i, v);
-}
+constexpr int V = 4;  // columns of a lane
 
-// A thread's place: its columns from c on, and its rows r, r + rows_wg * gridDim.x, ...
-template <int V>
+// A thread's place: its columns, and its row among the `per` rows of a workgroup.  NEAR:
+// the columns are neighbours, read at once; otherwise (rows of any width and alignment)
+// they lie `lanes` apart, so that the wave's accesses are of neighbours still.
+template <int TYPE, bool NEAR>
 struct Place {
-  int c, r, per;  // per: rows of a workgroup
+  int c, r, per, lanes, left;  // first column; left: columns of it on
   bool ok;
   __device__ __forceinline__ explicit Place(const ConvArgs& a) {
-    per = NT / a.lanes;
-    r = threadIdx.x / a.lanes;
-    c = ((int)blockIdx.y * a.lanes + threadIdx.x % a.lanes) * V;
+    lanes = a.lanes;
+    per = NT / lanes;
+    r = threadIdx.x / lanes;
+    const int l = threadIdx.x % lanes;
+    c = (int)blockIdx.y * lanes * V + l * (NEAR ? V : 1);
     ok = r < per && c < a.cols;
+    left = ok ? a.cols - c : 0;
+    if (!ok) c = 0;
+  }
+  // whether column k of the thread's is there
+  __device__ __forceinline__ bool has(int k) const { return NEAR ? ok : k * lanes < left; }
+  __device__ __forceinline__ int column(int k) const { return NEAR ? c + k : c + k * lanes; }
+  __device__ __forceinline__ int64_t at(int k) const { return NEAR ? k : has(k) ? (int64_t)k * lanes : 0; }
+  template <int T>
+  __device__ __forceinline__ void load(const void* p, int64_t i, float (&v)[V]) const {
+    const Elem<T>* const r = (const Elem<T>*)p + i;
+    if constexpr (NEAR) {
+      get<V>(r, v);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) get<1>(r + at(k), v + k);
+    }
+  }
+  template <int T>
+  __device__ __forceinline__ void store(void* p, int64_t i, const float (&v)[V]) const {
+    Elem<T>* const r = (Elem<T>*)p + i;
+    if constexpr (!NEAR) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (has(k)) put<1>(r + at(k), v + k);
+    } else if constexpr (T == MGN_BF16) {
+      __builtin_nontemporal_store((uint64_t)pack_bf16(v[0], v[1]) | (uint64_t)pack_bf16(v[2], v[3]) << 32, (uint64_t*)r);
+    } else {
+      put<V>(r, v);
+    }
   }
 };
 
@@ -59,38 +80,39 @@ __device__ __forceinline__ int age_at(const uint8_t* starts, int64_t t) {
   return n;
 }
 
-// The weights of V neighbouring columns lie one behind the other.
-template <int W, int V>
-__device__ __forceinline__ void load_taps(const ConvArgs& a, int c, bool ok, float (&w)[W][V], float (&b)[V]) {
-  float all[V * W];
-  const float* const p = a.w + (ok ? (int64_t)c * W : 0);
-  constexpr int RUN = V * W % 4 == 0 ? 4 : 1;
-#pragma unroll
-  for (int k = 0; k < V * W; k += RUN) get<RUN>(p + k, all + k);
+template <int W, class P>
+__device__ __forceinline__ void load_taps(const ConvArgs& a, const P& p, float (&w)[W][V], float (&b)[V]) {
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    b[k] = a.b ? a.b[ok ? c + k : k] : 0.f;
+    const int c = p.has(k) ? p.column(k) : 0;
+    b[k] = a.b ? a.b[c] : 0.f;
+    float all[W];
+    get<(W % 4 == 0 ? W : 1)>(a.w + (int64_t)c * W, all);
+    if constexpr (W % 4 != 0)
 #pragma unroll
-    for (int j = 0; j < W; ++j) w[j][k] = all[k * W + j];
+      for (int j = 1; j < W; ++j) all[j] = a.w[(int64_t)c * W + j];
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j][k] = all[j];
   }
 }
 
 // Inputs t0 - (W - 1) .. t0 - 1 of a row, oldest first.
-template <int TYPE, int W, int V>
-__device__ __forceinline__ void load_before(const ConvArgs& a, int64_t t0, int64_t C, int64_t i, bool ok, float (*xs)[V]) {
+template <int TYPE, int W, class P>
+__device__ __forceinline__ void load_before(const ConvArgs& a, const P& p, int64_t t0, int64_t C, int64_t i, bool ok,
+                                            float (*xs)[V]) {
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) {
     const int64_t t = t0 - (W - 1) + j;
 #pragma unroll
     for (int k = 0; k < V; ++k) xs[j][k] = 0.f;
-    if (ok && t >= 0) load<TYPE, V>(a.x, t * C + i, xs[j]);
-    else if (ok && a.past) load<TYPE, V>(a.past, (t + W - 1) * C + i, xs[j]);
+    if (ok && t >= 0) p.template load<TYPE>(a.x, t * C + i, xs[j]);
+    else if (ok && a.past) p.template load<TYPE>(a.past, (t + W - 1) * C + i, xs[j]);
   }
 }
 
 // The weighted inputs of the step whose own input is xs[W - 1]; of those before it
 // the last `age` count, the others are left out whatever they are.
-template <int W, int V>
+template <int W>
 __device__ __forceinline__ void taps(const float (*xs)[V], const float (&w)[W][V], const float (&b)[V], int age, float (&v)[V]) {
 #pragma unroll
   for (int k = 0; k < V; ++k) v[k] = b[k];
@@ -109,44 +131,56 @@ __device__ __forceinline__ void taps(const float (*xs)[V], const float (&w)[W][V
 }
 
 // What some steps bring, as it lies in memory; N arrays.  PAST: read past the caches.
-template <int TYPE, int V, int STEPS, int N, bool PAST>
+template <int TYPE, int STEPS, int N, bool NEAR, bool PAST>
 struct Inputs {
-  Raw<TYPE, V, true> v[N][STEPS];
+  Raw<TYPE, V, NEAR> v[N][STEPS];
   uint32_t fresh[STEPS];
   // steps t .. of those before `end` (the last of them again for those that are not)
-  __device__ __forceinline__ void load(const ConvArgs& a, const void* x, const void* y, int64_t t, int64_t end, int64_t C,
-                                       int64_t i) {
+  __device__ __forceinline__ void load(const ConvArgs& a, const Place<TYPE, NEAR>& p, const void* x, const void* y, int64_t t,
+                                       int64_t end, int64_t C, int64_t i) {
     if (t >= end) return;
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
       const int64_t s = t + e < end ? t + e : end - 1;
-      const char* const p = (const char*)x + (s * C + i) * (int64_t)sizeof(Elem<TYPE>);
-      if constexpr (PAST) v[0][e].stream(p);
-      else v[0][e].load(p, 0, 0, V);
-      if constexpr (N > 1) v[1][e].load((const char*)y + (s * C + i) * (int64_t)sizeof(Elem<TYPE>), 0, 0, V);
+      one(p, x, s * C + i, v[0][e]);
+      if constexpr (N > 1) one(p, y, s * C + i, v[1][e]);
       fresh[e] = a.starts ? a.starts[s] : 0;
+    }
+  }
+  __device__ __forceinline__ void one(const Place<TYPE, NEAR>& p, const void* x, int64_t i, Raw<TYPE, V, NEAR>& r) {
+    const Elem<TYPE>* const q = (const Elem<TYPE>*)x + i;
+    if constexpr (!NEAR) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if constexpr (TYPE == MGN_BF16) r.w[k] = q[p.at(k)];
+        else r.w[k] = __float_as_uint(q[p.at(k)]);
+      }
+    } else if constexpr (PAST) {
+      r.stream((const char*)q);
+    } else {
+      r.load((const char*)q, 0, 0, V);
     }
   }
 };
 
-template <int TYPE, int W, int V, int STEPS, bool PAST>
+template <int TYPE, int W, int STEPS, bool NEAR, bool PAST>
 __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
-  const Place<V> p(a);
+  const Place<TYPE, NEAR> p(a);
   const int64_t C = a.rows * a.cols;
   float w[W][V], b[V];
-  load_taps<W, V>(a, p.c, p.ok, w, b);
+  load_taps<W>(a, p, w, b);
   for (int64_t item = blockIdx.x; item < a.groups * a.segs; item += gridDim.x) {
     const int64_t s = item / a.groups, r = (item - s * a.groups) * p.per + p.r;
     const int64_t t0 = s * a.seg, t1 = s + 1 == a.segs ? a.steps : t0 + a.seg;
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V];
-    Inputs<TYPE, V, STEPS, 1, PAST> now, next;
-    now.load(a, a.x, nullptr, t0, t1, C, i);
-    load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
+    Inputs<TYPE, STEPS, 1, NEAR, PAST> now, next;
+    now.load(a, p, a.x, nullptr, t0, t1, C, i);
+    load_before<TYPE, W>(a, p, t0, C, i, ok, xs);
     int age = age_at<W>(a.starts, t0 - 1);
     for (int64_t t = t0; t < t1; t += STEPS) {
-      next.load(a, a.x, nullptr, t + STEPS, t1, C, i);  // while these steps run
+      next.load(a, p, a.x, nullptr, t + STEPS, t1, C, i);  // while these steps run
       const int n = t1 - t < STEPS ? (int)(t1 - t) : STEPS;
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) now.v[0][e].get(0, V, xs[W - 1 + e]);
@@ -155,12 +189,12 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
         if (e >= n) break;
         age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
         float v[V];
-        taps<W, V>(xs + e, w, b, age, v);
+        taps<W>(xs + e, w, b, age, v);
         if (a.silu) {
 #pragma unroll
           for (int k = 0; k < V; ++k) v[k] *= sigmoid(v[k]);
         }
-        if (ok) store<TYPE, V>(a.y, (t + e) * C + i, v);
+        if (ok) p.template store<TYPE>(a.y, (t + e) * C + i, v);
       }
       // the last W - 1 inputs to the front
 #pragma unroll
@@ -179,7 +213,7 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
         float v[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = W - 2 - j <= age ? xs[j][k] : 0.f;
-        store<TYPE, V>(a.past_out, j * C + i, v);
+        p.template store<TYPE>(a.past_out, j * C + i, v);
       }
     }
   }
@@ -188,13 +222,13 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
 // The backward; a.y is dx.  A thread's sums of dw and db go over all its items, in
 // fp32 over SUM_STEPS steps and in fp64 over these.
 constexpr int SUM_STEPS = 8;
-template <int TYPE, int W, int V, int STEPS>
+template <int TYPE, int W, int STEPS, bool NEAR>
 __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
   static_assert(SUM_STEPS % STEPS == 0);
-  const Place<V> p(a);
+  const Place<TYPE, NEAR> p(a);
   const int64_t C = a.rows * a.cols;
   float w[W][V], b[V], sw[W][V], sb[V];
-  load_taps<W, V>(a, p.c, p.ok, w, b);
+  load_taps<W>(a, p, w, b);
   double dw[W][V], db[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) {
@@ -218,9 +252,9 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V], g[W - 1 + STEPS][V];  // g[j]: gradient of the input of xs[j]
-    Inputs<TYPE, V, STEPS, 2, false> now, next;
-    now.load(a, a.x, a.dy, t0, te, C, i);
-    load_before<TYPE, W, V>(a, t0, C, i, ok, xs);
+    Inputs<TYPE, STEPS, 2, NEAR, false> now, next;
+    now.load(a, p, a.x, a.dy, t0, te, C, i);
+    load_before<TYPE, W>(a, p, t0, C, i, ok, xs);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -229,11 +263,11 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
     // the gradient of input t, complete
     const auto out = [&](int64_t t, const float (&v)[V]) {
       if (!ok || t >= t1) return;
-      if (t >= t0) store<TYPE, V>(a.y, t * C + i, v);
-      else if (t < 0 && a.d_past) store<MGN_FP32, V>(a.d_past, (t + W - 1) * C + i, v);
+      if (t >= t0) p.template store<TYPE>(a.y, t * C + i, v);
+      else if (t < 0 && a.d_past) p.template store<MGN_FP32>(a.d_past, (t + W - 1) * C + i, v);
     };
     for (int64_t t = t0; t < te; t += STEPS) {
-      next.load(a, a.x, a.dy, t + STEPS, te, C, i);  // while these steps run
+      next.load(a, p, a.x, a.dy, t + STEPS, te, C, i);  // while these steps run
       const int n = te - t < STEPS ? (int)(te - t) : STEPS;
       float d[STEPS][V];
 #pragma unroll
@@ -252,7 +286,7 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
         age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
         if (a.silu) {
           float v[V];
-          taps<W, V>(xs + e, w, b, age, v);
+          taps<W>(xs + e, w, b, age, v);
 #pragma unroll
           for (int k = 0; k < V; ++k) {
             const float f = sigmoid(v[k]);
@@ -289,7 +323,7 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
       for (int j = 0; j < W - 1; ++j) {
         if (a.d_past_out && ok && W - 2 - j <= age) {
           float v[V];
-          load<MGN_FP32, V>(a.d_past_out, j * C + i, v);
+          p.template load<MGN_FP32>(a.d_past_out, j * C + i, v);
 #pragma unroll
           for (int k = 0; k < V; ++k) g[j][k] += v[k];
         }
@@ -300,24 +334,30 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
   if (!a.part) return;
   add();
   // the workgroup's rows, one behind the other, in fp64
-  __shared__ double lds[NT];
+  __shared__ double lds[V][NT];
   const int64_t width = (int64_t)a.cols * (W + 1);
   float* const dst = a.part + blockIdx.x * width;
-  const auto total = [&](double v, int64_t at) {
-    lds[threadIdx.x] = p.ok ? v : 0;
-    __syncthreads();
-    if (p.ok && p.r == 0) {
-      for (int e = 1; e < p.per; ++e) v += lds[e * a.lanes + threadIdx.x];
-      dst[at] = (float)v;
+  const auto total = [&](const double (&v)[V], int j) {  // j == W: db
+#pragma unroll
+    for (int k = 0; k < V; ++k) lds[k][threadIdx.x] = v[k];
+    for (int n = p.per; n > 1;) {  // the upper half of the rows to the lower
+      __syncthreads();
+      const int half = (n + 1) / 2;
+      if (p.r + half < n)
+#pragma unroll
+        for (int k = 0; k < V; ++k) lds[k][threadIdx.x] += lds[k][threadIdx.x + half * p.lanes];
+      n = half;
     }
+    if (p.ok && p.r == 0)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (p.has(k))
+          dst[j == W ? (int64_t)a.cols * W + p.column(k) : (int64_t)p.column(k) * W + j] = (float)lds[k][threadIdx.x];
     __syncthreads();
   };
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-#pragma unroll
-    for (int j = 0; j < W; ++j) total(dw[j][k], (int64_t)(p.c + k) * W + j);
-    total(db[k], (int64_t)a.cols * W + p.c + k);
-  }
+  for (int j = 0; j < W; ++j) total(dw[j], j);
+  total(db, W);
 }
 
 // past_out where no steps come: past, or zeros.
@@ -353,13 +393,13 @@ constexpr int64_t MOST_WGS = 1 << 20;
 // 100,003 x 64 bf16 115 us through it, 108 past it; its backward 352 and 354 (600 steps
 // of 1,885 x 128 fp32).
 constexpr int64_t CACHE = (int64_t)256 << 20;
-constexpr int64_t LEAST_SEG = 32;   // steps of a segment
+constexpr int64_t LEAST_SEG = 8;    // steps of a segment (a short one reads its neighbours' steps again, but only where the card has room)
 
 int64_t type_size(int type) { return type == MGN_FP32 ? 4 : 2; }
 bool at(const void* p, int64_t bytes) { return (uintptr_t)p % bytes == 0; }
 
-// How the rows and steps are dealt for V columns a lane and about `want` workgroups.
-void deal(ConvArgs& a, int V, int64_t want) {
+// How the rows and steps are dealt to about `want` workgroups.
+void deal(ConvArgs& a, int64_t want) {
   const int per_row = (a.cols + V - 1) / V;
   a.tiles = (per_row + NT - 1) / NT;
   a.lanes = (per_row + a.tiles - 1) / a.tiles;
@@ -399,9 +439,9 @@ hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
   const int64_t past_bytes = (width - 1) * C * type_size(type);
   if (a.steps <= 0)
     return a.past_out && a.past_out != a.past ? copy_bytes(a.past, a.past_out, past_bytes, st) : hipSuccess;
-  const int run = 4, edge = run * type_size(type);
-  const bool vec = a.cols % run == 0 && at(a.x, edge) && at(a.y, edge) && at(a.past, edge) && at(a.past_out, edge);
-  deal(a, vec ? run : 1, FWD_WGS);
+  const int64_t edge = V * type_size(type);
+  const bool near = a.cols % V == 0 && at(a.x, edge) && at(a.y, edge) && at(a.past, edge) && at(a.past_out, edge);
+  deal(a, FWD_WGS);
   const bool past = 2 * a.steps * C * type_size(type) > CACHE;
   const bool tail = a.past_out && a.past_out == a.past && a.segs > 1;
   ConvArgs m = a;
@@ -410,9 +450,10 @@ hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
   const dim3 grid((unsigned)(items < MOST_WGS ? items : MOST_WGS), (unsigned)a.tiles);
   const hipError_t e = by_width(width, [&](auto w) {
     const auto go = [&](auto ty) {
-      if (vec && past) hipLaunchKernelGGL((conv_kernel<ty(), w(), 4, 4, true>), grid, dim3(NT), 0, st, m);
-      else if (vec) hipLaunchKernelGGL((conv_kernel<ty(), w(), 4, 4, false>), grid, dim3(NT), 0, st, m);
-      else hipLaunchKernelGGL((conv_kernel<ty(), w(), 1, 8, false>), grid, dim3(NT), 0, st, m);
+      constexpr int STEPS = 4;
+      if (near && past) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, true>), grid, dim3(NT), 0, st, m);
+      else if (near) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, false>), grid, dim3(NT), 0, st, m);
+      else hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, false, false>), grid, dim3(NT), 0, st, m);
     };
     if (type == MGN_BF16) go(Int<MGN_BF16>());
     else go(Int<MGN_FP32>());
@@ -432,23 +473,21 @@ hipError_t launch_conv_grad(ConvArgs a, int type, int width, float* dw, float* d
   if (C > 0 && a.steps <= 0 && a.d_past)
     if (const hipError_t e = copy_bytes(a.d_past_out, a.d_past, (width - 1) * C * 4, st); e != hipSuccess) return e;
   if (C > 0 && a.steps > 0) {
-    const int run = 4;
-    const bool vec = a.cols % run == 0 && at(a.x, run * type_size(type)) && at(a.y, run * type_size(type)) &&
-                     at(a.dy, run * type_size(type)) && at(a.past, run * type_size(type)) && at(a.d_past, 16) &&
-                     at(a.d_past_out, 16);
-    deal(a, vec ? run : 1, MGN_CONV_PARTS);
+    const int64_t edge = V * type_size(type);
+    const bool near = a.cols % V == 0 && at(a.x, edge) && at(a.y, edge) && at(a.dy, edge) && at(a.past, edge) &&
+                      at(a.d_past, 16) && at(a.d_past_out, 16);
+    deal(a, MGN_CONV_PARTS);
     const int64_t items = a.groups * a.segs;
     parts = items < MGN_CONV_PARTS ? items : MGN_CONV_PARTS;
     const dim3 grid((unsigned)parts, (unsigned)a.tiles);
     const hipError_t e = by_width(width, [&](auto w) {
-      constexpr int STEPS = w() > 4 ? 2 : 4;
-      if (type == MGN_BF16) {
-        if (vec) hipLaunchKernelGGL((conv_grad_kernel<MGN_BF16, w(), 4, STEPS>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((conv_grad_kernel<MGN_BF16, w(), 1, 8>), grid, dim3(NT), 0, st, a);
-      } else {
-        if (vec) hipLaunchKernelGGL((conv_grad_kernel<MGN_FP32, w(), 4, STEPS>), grid, dim3(NT), 0, st, a);
-        else hipLaunchKernelGGL((conv_grad_kernel<MGN_FP32, w(), 1, 8>), grid, dim3(NT), 0, st, a);
-      }
+      const auto go = [&](auto ty) {
+        constexpr int STEPS = w() > 4 ? 2 : 4;
+        if (near) hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), STEPS, true>), grid, dim3(NT), 0, st, a);
+        else hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), 2, false>), grid, dim3(NT), 0, st, a);
+      };
+      if (type == MGN_BF16) go(Int<MGN_BF16>());
+      else go(Int<MGN_FP32>());
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;

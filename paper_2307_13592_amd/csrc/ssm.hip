@@ -190,21 +190,24 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   if (PASS == LOCAL_ENDS && p.ok) a.sums[c * C + p.i0 + p.o] = sum;
 }
 
-// What enters each chunk, in the place of its own end.  A workgroup takes JOIN_S
-// neighbouring states, JOIN_G of its threads to one, each of them AHEAD consecutive
-// chunks at a time: it joins its chunks, the groups join theirs in LDS, and each runs
-// its chunks again from what enters them.  Two latencies for up to 256 chunks.
-constexpr int JOIN_S = 16, JOIN_G = NT / JOIN_S, AHEAD = 16;
+// What enters each chunk, in the place of its own end.  G threads to a state, each of
+// them AHEAD consecutive chunks at a time: it joins its chunks, the G join theirs in
+// LDS, and each runs its chunks again from what enters them.  G = 1 for few chunks
+// (18 of 96,256 states 29 us with 16, of which 14 idle); two latencies for 256 chunks
+// with G = 16.
+constexpr int AHEAD = 16;
+template <int G>
 __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* first, bool reverse) {
-  __shared__ float lds[2][JOIN_G][JOIN_S];
+  constexpr int STATES = NT / G;
+  __shared__ float lds[2][G][G > 1 ? STATES : 1];
   const int64_t C = a.rows * a.cols, S = C * a.n, step = reverse ? -1 : 1;
-  const int si = threadIdx.x % JOIN_S, gr = threadIdx.x / JOIN_S;
-  for (int64_t i0 = (int64_t)blockIdx.x * JOIN_S; i0 < S; i0 += (int64_t)gridDim.x * JOIN_S) {
+  const int si = threadIdx.x % STATES, gr = threadIdx.x / STATES;
+  for (int64_t i0 = (int64_t)blockIdx.x * STATES; i0 < S; i0 += (int64_t)gridDim.x * STATES) {
     const int64_t i = i0 + si < S ? i0 + si : S - 1, ch = i / a.n;
     const bool ok = i0 + si < S;
     const float A = a.A[ch % a.cols * a.n + (i - ch * a.n)] * LOG2E;
     float v = first ? first[i] : 0.f;
-    for (int64_t k0 = 0; k0 < a.chunks; k0 += JOIN_G * AHEAD) {
+    for (int64_t k0 = 0; k0 < a.chunks; k0 += G * AHEAD) {
       const int64_t k = k0 + gr * AHEAD, c = reverse ? a.chunks - 1 - k : k;  // chunk k of the order
       float own[AHEAD], f[AHEAD];
 #pragma unroll
@@ -218,26 +221,32 @@ __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* fi
       for (int e = 0; e < AHEAD; ++e) {
         const bool here = k + e < a.chunks - 1 && f[e] == CUT;
         f[e] = k + e < a.chunks - 1 ? __builtin_amdgcn_exp2f(A * f[e]) : 1.f;
+        if (here) f[e] = 0.f;
         cuts |= (uint32_t)here << e;
-        q = here ? own[e] : fmaf(f[e], q, own[e]);
-        p *= f[e];
+        if constexpr (G > 1) {
+          q = here ? own[e] : fmaf(f[e], q, own[e]);
+          p *= f[e];
+        }
       }
-      lds[0][gr][si] = cuts ? CUT : p, lds[1][gr][si] = q;
-      __syncthreads();
       float mine = v;
+      if constexpr (G > 1) {
+        lds[0][gr][si] = cuts ? CUT : p, lds[1][gr][si] = q;
+        __syncthreads();
 #pragma unroll
-      for (int e = 0; e < JOIN_G; ++e) {
-        if (e == gr) mine = v;
-        const float pe = lds[0][e][si], qe = lds[1][e][si];
-        v = pe == CUT ? qe : fmaf(pe, v, qe);
+        for (int e = 0; e < G; ++e) {
+          if (e == gr) mine = v;
+          const float pe = lds[0][e][si], qe = lds[1][e][si];
+          v = pe == CUT ? qe : fmaf(pe, v, qe);
+        }
+        __syncthreads();
       }
-      __syncthreads();
 #pragma unroll
       for (int e = 0; e < AHEAD; ++e) {
         if (k + e >= a.chunks) break;
         if (ok) a.state[(c + step * e) * S + i] = mine;
         mine = cuts >> e & 1 ? own[e] : fmaf(f[e], mine, own[e]);
       }
+      if constexpr (G == 1) v = mine;
     }
   }
 }
@@ -290,8 +299,10 @@ int64_t ssm_chunk(int64_t steps, int64_t rows, int cols, int64_t want) {
 }
 
 hipError_t launch_ssm_join(const SsmArgs& a, const float* first, bool reverse, hipStream_t st) {
-  const int64_t n = a.rows * a.cols * a.n, b = (n + JOIN_S - 1) / JOIN_S;
-  hipLaunchKernelGGL(ssm_join_kernel, dim3((unsigned)(b < 65536 ? b : 65536)), dim3(NT), 0, st, a, first, reverse);
+  const int64_t n = a.rows * a.cols * a.n, per = a.chunks <= 2 * AHEAD ? NT : NT / 16, b = (n + per - 1) / per;
+  const dim3 grid((unsigned)(b < 65536 ? b : 65536));
+  if (per == NT) hipLaunchKernelGGL((ssm_join_kernel<1>), grid, dim3(NT), 0, st, a, first, reverse);
+  else hipLaunchKernelGGL((ssm_join_kernel<16>), grid, dim3(NT), 0, st, a, first, reverse);
   return hipGetLastError();
 }
 

@@ -473,12 +473,20 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   }
   if (!a.part) return;
   const int64_t width = (int64_t)a.cols * (a.n + 2);
-  float* const dst = a.part + ((slot * a.chunks + c) * RPW + sub) * width;
+  float* const dst = a.part + (slot * a.chunks + c) * width;
+  // the wave's rows
+  const auto rows = [&](double v) {
+#pragma unroll
+    for (int d = 4 * GP; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+  };
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int k = 0; k < NL; ++k)
-      if (g + j < a.cols && s0 + k < a.n) dst[(int64_t)(g + j) * a.n + s0 + k] = (float)accs[j * NL + k][threadIdx.x];
+    for (int k = 0; k < NL; ++k) {
+      const double v = rows(accs[j * NL + k][threadIdx.x]);
+      if (sub == 0 && g + j < a.cols && s0 + k < a.n) dst[(int64_t)(g + j) * a.n + s0 + k] = (float)v;
+    }
   if constexpr (NW > 1) {  // the waves' steps
     double* const t = &accs[0][0];
     __syncthreads();
@@ -488,7 +496,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
     dD = d_bias = 0;
     for (int m = 0; m < NW; ++m) dD += t[m * 64 + lane], d_bias += t[(NW + m) * 64 + lane];
   }
-  if (w == 0 && col < a.cols) {
+  dD = rows(dD), d_bias = rows(d_bias);
+  if (w == 0 && sub == 0 && col < a.cols) {
     dst[(int64_t)a.cols * a.n + col] = (float)dD;
     dst[(int64_t)a.cols * (a.n + 1) + col] = (float)d_bias;
   }
@@ -521,14 +530,14 @@ struct Deal {
 Deal deal(int64_t steps, int64_t rows, int cols, int n) {
   Deal d{};
   const int per_row = (cols + 3) / 4;
-  d.lg = per_row == 1 ? 0 : per_row <= 4 ? 2 : 4;
+  d.lg = per_row <= 4 ? 2 : 4;
   d.tiles = (per_row + (1 << d.lg) - 1) >> d.lg;
   const int rpw = 16 >> d.lg;
   d.chunk = ssm_chunk(steps, rows, cols, CHUNK_WAVES);
   d.chunks = (steps + d.chunk - 1) / d.chunk;
   const int64_t most = (rows + rpw - 1) / rpw, want = (WAVES + d.tiles * d.chunks - 1) / (d.tiles * d.chunks);
   d.slots = most < want ? most : want;
-  d.parts = d.slots * d.chunks * rpw;
+  d.parts = d.slots * d.chunks;
   const int64_t C = rows * cols;
   d.state = d.chunks > 1 ? up(4 * d.chunks * C * n) : 0;
   d.sums = d.chunks > 1 ? up(4 * d.chunks * C) : 0;
@@ -551,7 +560,7 @@ hipError_t by_states(int n, F f) {
 }
 template <class F>
 hipError_t by_groups(int lg, F f) {
-  return lg == 0 ? f(Int<0>()) : lg == 2 ? f(Int<2>()) : f(Int<4>());
+  return lg == 2 ? f(Int<2>()) : f(Int<4>());
 }
 
 template <int TYPE, bool GATE>
