@@ -229,19 +229,20 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
   const int64_t C = a.rows * a.cols;
   float w[W][V], b[V], sw[W][V], sb[V];
   load_taps<W>(a, p, w, b);
-  double dw[W][V], db[V];
+  // [tap, or W for db][column][thread]: each thread adds to its own places only
+  __shared__ double sums[W + 1][V][NT];
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    db[k] = 0, sb[k] = 0.f;
+    sums[W][k][threadIdx.x] = 0, sb[k] = 0.f;
 #pragma unroll
-    for (int j = 0; j < W; ++j) dw[j][k] = 0, sw[j][k] = 0.f;
+    for (int j = 0; j < W; ++j) sums[j][k][threadIdx.x] = 0, sw[j][k] = 0.f;
   }
   const auto add = [&] {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      db[k] += sb[k], sb[k] = 0.f;
+      sums[W][k][threadIdx.x] += sb[k], sb[k] = 0.f;
 #pragma unroll
-      for (int j = 0; j < W; ++j) dw[j][k] += sw[j][k], sw[j][k] = 0.f;
+      for (int j = 0; j < W; ++j) sums[j][k][threadIdx.x] += sw[j][k], sw[j][k] = 0.f;
     }
   };
   int turn = 0;
@@ -333,31 +334,26 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
   }
   if (!a.part) return;
   add();
-  // the workgroup's rows, one behind the other, in fp64
-  __shared__ double lds[V][NT];
-  const int64_t width = (int64_t)a.cols * (W + 1);
-  float* const dst = a.part + blockIdx.x * width;
-  const auto total = [&](const double (&v)[V], int j) {  // j == W: db
-#pragma unroll
-    for (int k = 0; k < V; ++k) lds[k][threadIdx.x] = v[k];
-    for (int n = p.per; n > 1;) {  // the upper half of the rows to the lower
-      __syncthreads();
-      const int half = (n + 1) / 2;
-      if (p.r + half < n)
-#pragma unroll
-        for (int k = 0; k < V; ++k) lds[k][threadIdx.x] += lds[k][threadIdx.x + half * p.lanes];
-      n = half;
-    }
-    if (p.ok && p.r == 0)
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (p.has(k))
-          dst[j == W ? (int64_t)a.cols * W + p.column(k) : (int64_t)p.column(k) * W + j] = (float)lds[k][threadIdx.x];
+  // the workgroup's rows, the upper half to the lower
+  for (int n = p.per; n > 1;) {
     __syncthreads();
-  };
+    const int half = (n + 1) / 2;
+    if (p.r + half < n)
 #pragma unroll
-  for (int j = 0; j < W; ++j) total(dw[j], j);
-  total(db, W);
+      for (int j = 0; j <= W; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) sums[j][k][threadIdx.x] += sums[j][k][threadIdx.x + half * p.lanes];
+    n = half;
+  }
+  if (!p.ok || p.r != 0) return;
+  float* const dst = a.part + blockIdx.x * ((int64_t)a.cols * (W + 1));
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    if (!p.has(k)) continue;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dst[(int64_t)p.column(k) * W + j] = (float)sums[j][k][threadIdx.x];
+    dst[(int64_t)a.cols * W + p.column(k)] = (float)sums[W][k][threadIdx.x];
+  }
 }
 
 // past_out where no steps come: past, or zeros.
