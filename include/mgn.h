@@ -382,7 +382,8 @@ mgn_status mgn_causal_conv_grad(const void* x, int32_t type, const float* weight
  * by a row's columns) of one storage type (MGN_FP32 or MGN_BF16); A fp32 [cols][n],
  * D (NULL: zeros) and dt_bias (NULL: zeros) fp32 [cols]; all of them finite.  starts
  * as mgn_gated_scan.  States are fp32 [rows][cols][n] and stay so.  A step of size 0
- * (softplus of -infinity, say) leaves the states as they were whatever x and B hold. */
+ * (softplus of -infinity, say) leaves the states as they were whatever x and B hold;
+ * a state that is NaN or infinite stays one of them until a start. */
 #define MGN_STATES_MAX 64
 #define MGN_MARK_STEPS 8
 typedef struct {

@@ -777,6 +777,8 @@ class mgn_grad_list:
             raise ValueError("outs: expected one for each of grads")
         self._list = None
         self.tensors, self.dev = (grads, outs), grads[0].get_device() if grads else -1
+        if grads and self.dev < 0:
+            raise ValueError("grads[0]: expected a device tensor")
         rec = (mgn_grad * max(len(grads), 1))()
         for k, (g, o) in enumerate(zip(grads, outs)):
             ty = _type(g, f"grads[{k}]")
@@ -784,14 +786,14 @@ class mgn_grad_list:
                               _arr(o, f"outs[{k}]", g.dtype, g.shape, self.dev), g.numel(), ty)
         p = C.c_void_p()
         _check(lib().mgn_grads_create(rec, len(grads), C.byref(p)))
-        self._list = p
+        self._list, self._destroy = p, lib().mgn_grads_destroy
         n = C.c_size_t()
         _check(lib().mgn_grads_work(p, C.byref(n)))
         self.work_bytes = int(n.value)
 
     def __del__(self):
         if getattr(self, "_list", None):
-            lib().mgn_grads_destroy(self._list)
+            self._destroy(self._list)
             self._list = None
 
 

@@ -45,6 +45,8 @@ struct Lookup {
   }
 };
 
+static_assert(sizeof(GradTable) + 64 <= 4096);
+
 // The workgroup's tiles.
 struct Tiles {
   uint32_t begin, end;

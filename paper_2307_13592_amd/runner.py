@@ -104,6 +104,8 @@ class Session:
         that is first scaled, in place, to at most this norm.  Returns the norm that
         it had (float32 [1] on the device; None without max_norm)."""
         grad = self.d_params if grad is None else grad
+        if grad.numel() != self.n_params:
+            raise ValueError("gradient vector has the wrong length")
         norm = None if max_norm is None else clip_grads([grad], max_norm, stream)
         mgn_sgd_step(self.model, grad, lr, stream)
         return norm

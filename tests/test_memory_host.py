@@ -210,6 +210,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
     with pytest.raises(ValueError):
         mgn.mgn_grad_norm([torch.zeros(3)], torch.zeros(1))
     with pytest.raises(ValueError):
+        mgn.mgn_grad_list([torch.zeros(3)])
+    with pytest.raises(ValueError):
         mgn.mgn_grad_list([torch.zeros(3)], [None, None])
     with pytest.raises(ValueError):
         mgn.mgn_grad_list([torch.zeros(3, dtype=torch.float16)])
