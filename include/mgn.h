@@ -383,7 +383,9 @@ mgn_status mgn_causal_conv_grad(const void* x, int32_t type, const float* weight
  * D (NULL: zeros) and dt_bias (NULL: zeros) fp32 [cols]; all of them finite.  starts
  * as mgn_gated_scan.  States are fp32 [rows][cols][n] and stay so.  A step of size 0
  * (softplus of -infinity, say) leaves the states as they were whatever x and B hold;
- * a state that is NaN or infinite stays one of them until a start. */
+ * a state that is NaN or infinite stays one of them until a start.  States may grow
+ * (delta A > 0), but a nonzero one only so far that exp(A sum of delta) over the steps
+ * of a call stays within the fp32 range. */
 #define MGN_STATES_MAX 64
 #define MGN_MARK_STEPS 8
 typedef struct {
@@ -409,7 +411,9 @@ mgn_status mgn_selective_scan(const mgn_ssm* s, const float* h0, void* y, float*
  * (fp32 [rows][cols][n] = dL/dh_last, NULL: zeros): dx, ddt, dB, dC and (with z) dz
  * in x's type; dA, dD and d_bias fp32, each NULL if not wanted, overwritten or added
  * to when accumulate != 0; dh0 (NULL: not wanted; it may be dh_last) = dL/dh0.
- * A step of size 0 gives x and B no gradient, nor dt where its softplus is level. */
+ * A step of size 0 gives x and B no gradient, nor dt where its softplus is level; with
+ * dy = 0 there too, no gradient takes anything from what x and B hold (C and z are
+ * finite). */
 typedef struct {
   void *dx, *ddt, *dB, *dC, *dz;
   float *dA, *dD, *d_bias;

@@ -434,7 +434,9 @@ def _scratch(nbytes: int, dev: int, stream):
     belongs to a HIP graph that records the call)."""
     import torch
     device = torch.device("cuda", dev) if dev >= 0 else None
-    with _on(None if device is None else stream, device):
+    if stream is None or device is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _on(stream, device):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
@@ -768,13 +770,18 @@ def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=N
 class mgn_grad_list:
     """Device tensors (float32 or bfloat16, contiguous, on one GPU) whose global norm
     mgn_grad_norm and mgn_grad_clip take; outs: where the clipped ones go (None: in
-    place).  The list holds the tensors; it is made once for a program's gradients."""
+    place).  It is made once for a program's gradients, stands for the memory that they
+    have then, and keeps that memory."""
 
     def __init__(self, grads, outs=None):
         grads = list(grads)
         outs = [None] * len(grads) if outs is None else list(outs)
+        # (aliases: a tensor whose .data is set to another leaves its memory here)
+        grads, outs = ([None if t is None else t.detach() for t in ts] for ts in (grads, outs))
         if len(outs) != len(grads):
             raise ValueError("outs: expected one for each of grads")
+        if any(g is None for g in grads):
+            raise ValueError("grads: expected tensors, got None")
         self._list = None
         self.tensors, self.dev = (grads, outs), grads[0].get_device() if grads else -1
         if grads and self.dev < 0:

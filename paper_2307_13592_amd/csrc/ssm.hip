@@ -196,6 +196,9 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 // (18 of 96,256 states 29 us with 16, of which 14 idle); two latencies for 256 chunks
 // with G = 16.
 constexpr int AHEAD = 16;
+// What leaves chunks that v enters.  Zero states stay zero whatever a chunk's factor is
+// (over many growing steps it passes the fp32 range).
+__device__ __forceinline__ float carried(float f, float v, float own) { return v == 0.f ? own : fmaf(f, v, own); }
 template <int G>
 __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* first, bool reverse) {
   constexpr int STATES = NT / G;
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* fi
         if (here) f[e] = 0.f;
         cuts |= (uint32_t)here << e;
         if constexpr (G > 1) {
-          q = here ? own[e] : fmaf(f[e], q, own[e]);
+          q = here ? own[e] : carried(f[e], q, own[e]);
           p *= f[e];
         }
       }
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* fi
         for (int e = 0; e < G; ++e) {
           if (e == gr) mine = v;
           const float pe = lds[0][e][si], qe = lds[1][e][si];
-          v = pe == CUT ? qe : fmaf(pe, v, qe);
+          v = pe == CUT ? qe : carried(pe, v, qe);
         }
         __syncthreads();
       }
@@ -244,7 +247,7 @@ __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* fi
       for (int e = 0; e < AHEAD; ++e) {
         if (k + e >= a.chunks) break;
         if (ok) a.state[(c + step * e) * S + i] = mine;
-        mine = cuts >> e & 1 ? own[e] : fmaf(f[e], mine, own[e]);
+        mine = cuts >> e & 1 ? own[e] : carried(f[e], mine, own[e]);
       }
       if constexpr (G == 1) v = mine;
     }

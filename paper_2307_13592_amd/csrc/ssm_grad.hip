@@ -447,14 +447,15 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
             }
             const float x = value1<TYPE>(r.x[e]);
             float dx = mul_or_0(delta[e], tB[e]), dd = fmaf(tA[e], LN2, tB[e] * x);
-            if (a.D) dx = fmaf(D, ov[e], dx), sD = fmaf(ov[e], x, sD);
+            // (x may hold anything at a step of size 0 that no gradient reaches)
+            if (a.D) dx = fmaf(D, ov[e], dx), sD += mul_or_0(ov[e], x);
             if (a.softplus) dd = mul_or_0(sigmoid(value1<TYPE>(r.dt[e]) + bias), dd);
             sb += dd;
             write1<TYPE>((char*)a.dx + (xu + e * cb), o, dx);
             write1<TYPE>((char*)a.ddt + (xu + e * cb), o, dd);
             if (GATE) {
               const float z = value1<TYPE>(r.z[e]), s = sz[e], y = a.D ? fmaf(D, x, ty[e]) : ty[e];
-              write1<TYPE>((char*)a.dz + (xu + e * cb), o, value1<TYPE>(r.o[e]) * y * (s * fmaf(z, 1.f - s, 1.f)));
+              write1<TYPE>((char*)a.dz + (xu + e * cb), o, mul_or_0(value1<TYPE>(r.o[e]), y) * (s * fmaf(z, 1.f - s, 1.f)));
             }
           }
         if constexpr (NW > 1) par ^= 1;

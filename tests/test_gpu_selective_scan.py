@@ -143,6 +143,48 @@ def test_steps_of_size_0(T, rows, cols, n, dtype):
     assert torch.equal(after, last)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,rows,cols,n", [(9, 30, 64, 16), (700, 1, 64, 16), (70, 1, 32, 40)])
+def test_steps_that_no_gradient_reaches(T, rows, cols, n, dtype):
+    """Steps of size 0 with dy = 0: the gradients are those with zeros in x and B there."""
+    c = _case(T, rows, cols, n, dtype, seed=12)
+    held = torch.as_tensor(np.random.default_rng(13).random((T, rows)) < 0.3).cuda()
+    c["dt"][held], c["dy"][held], c["x"][held], c["B"][held] = -float("inf"), 0, 0, 0
+    _, last0, marks0 = _forward(c)
+    want = _backward(c, marks0)
+    c["x"][held], c["B"][held] = float("nan"), float("inf")
+    _, last, marks = _forward(c)
+    got = _backward(c, marks)
+    assert torch.equal(last, last0) and torch.equal(marks, marks0)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+
+
+@pytest.mark.parametrize("T,rows,cols", [(600, 1, 64), (1000, 1, 8), (40, 1, 8), (600, 40, 3)])
+def test_zero_states_under_growing_factors(T, rows, cols):
+    """exp(A sum of delta) passes the fp32 range over many steps; states (and their
+    gradients) that are zero stay so."""
+    n, few = 5, 3
+    c = _case(T, rows, cols, n, torch.float32, gate=False, softplus=False, bias=False, state=False, seed=14)
+    c["A"] = 6 + 2 * torch.rand_like(c["A"])
+    c["dt"][:] = 1
+    c["x"][:-few], c["dy"][few:] = 0, 0
+    y, last, marks = _forward(c)
+    g = _backward(c, marks)
+    assert not y[:-few].any()
+    cut = lambda s: {k: v[s] if k in ("x", "dt", "B", "C", "dy") else v for k, v in _ref(c).items()}
+    end, begin = cut(slice(T - few, T)), cut(slice(0, few))
+    f = ref.ssm(end)
+    ref.near("y", y[-few:], f["y"], f["ey"])
+    ref.near("h_last", last, f["last"], f["elast"])
+    want = ref.ssm_grad(begin, ref.ssm(begin), begin["dy"], None)
+    for k in ("dx", "ddt", "dB", "dC"):
+        assert not g[k][few:].any(), k
+        ref.near(k, g[k][:few], *want[k])
+    assert not g["dA"].any()
+    ref.near("dh0", g["dh0"], *want["dh0"])
+
+
 @pytest.mark.parametrize("T,rows,cols,n", [(30, 3, 40, 16), (900, 1, 20, 16)])
 def test_a_trajectory_that_is_not_finite_ends_at_a_start(T, rows, cols, n):
     c = _case(T, rows, cols, n, torch.float32, seed=6)
