@@ -20,16 +20,18 @@ __device__ __forceinline__ uint32_t here(uint32_t o) {
   asm volatile("" : "+v"(o));
   return o;
 }
+// An element as it lies in memory, of its own width: widened to 32 bits it would be
+// waited for where it is loaded, since the compiler widens it there.
+template <int TYPE>
+using Word = std::conditional_t<TYPE == MGN_BF16, uint16_t, uint32_t>;
 // The element at byte `o` from a wave's base: a scalar address and a 32-bit offset.
 template <int TYPE>
-__device__ __forceinline__ uint32_t raw1(const char* base, uint32_t o) {
-  o = here(o);
-  if constexpr (TYPE == MGN_BF16) return *(const uint16_t*)(base + o);
-  else return *(const uint32_t*)(base + o);
+__device__ __forceinline__ Word<TYPE> raw1(const char* base, uint32_t o) {
+  return *(const Word<TYPE>*)(base + here(o));
 }
 template <int TYPE>
-__device__ __forceinline__ float value1(uint32_t w) {
-  return __uint_as_float(TYPE == MGN_BF16 ? w << 16 : w);
+__device__ __forceinline__ float value1(Word<TYPE> w) {
+  return __uint_as_float(TYPE == MGN_BF16 ? (uint32_t)w << 16 : (uint32_t)w);
 }
 template <int TYPE>
 __device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
@@ -41,7 +43,7 @@ __device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
 template <int TYPE, int NL, bool FULL>
 struct Raw {
   static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = FULL ? (NL * SIZE + 3) / 4 : NL;
-  uint32_t w[WORDS];
+  std::conditional_t<FULL, uint32_t, Word<TYPE>> w[WORDS];
   __device__ __forceinline__ void load(const char* base, uint32_t o, int s, int n) {
     if constexpr (FULL) {
       __builtin_memcpy(w, base + here(o + (uint32_t)(s * SIZE)), NL * SIZE);
@@ -64,8 +66,7 @@ struct Raw {
   __device__ __forceinline__ void get(int s, int n, float (&v)[NL]) const {
 #pragma unroll
     for (int k = 0; k < NL; ++k) {
-      if constexpr (TYPE != MGN_BF16) v[k] = __uint_as_float(w[k]);
-      else if constexpr (!FULL) v[k] = __uint_as_float(w[k] << 16);
+      if constexpr (!FULL || TYPE != MGN_BF16) v[k] = value1<TYPE>((Word<TYPE>)w[k]);
       else v[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
       if constexpr (!FULL) v[k] = s + k < n ? v[k] : 0.f;
     }

@@ -25,7 +25,7 @@ enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES, ONE_STEP };
 // What some steps bring, as it lies in memory.
 template <int TYPE, int NL, bool FULL, int STEPS>
 struct Inputs {
-  uint32_t x[STEPS], dt[STEPS], z[STEPS], fresh[STEPS];
+  Word<TYPE> x[STEPS], dt[STEPS], z[STEPS];
   Raw<TYPE, NL, FULL> B[STEPS], C[STEPS];
 };
 
@@ -43,31 +43,28 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
   const int64_t C = a.rows * a.cols, cb = C * SIZE, rb = a.rows * a.n * SIZE;  // a step's bytes
 
-  // the next steps to load, and to store
+  // the next steps to load, and to store.  No branch stands between the loads or around
+  // them: where its ways meet, the compiler waits as for the one with the fewest loads.
+  // So a z that is not there is read from x's place, and behind the last step comes the
+  // last one again.
   const int64_t x0 = (ts * C + p.i0) * SIZE, n0 = (ts * a.rows * a.n + p.bn0) * SIZE;
-  const char *px = (const char*)a.x + x0, *pd = (const char*)a.dt + x0, *pz = (const char*)a.z + x0;
+  const char *px = (const char*)a.x + x0, *pd = (const char*)a.dt + x0, *pz = (const char*)(a.z ? a.z : a.x) + x0;
   const char *pB = (const char*)a.B + n0, *pC = (const char*)a.C + n0;
   char* py = (char*)a.y + x0;
-  const uint8_t* ps = a.starts + ts;
   const uint32_t o = p.o * SIZE, ob = p.ob * SIZE;
   const auto load = [&](In& v, int64_t left) {
-    const auto one = [&](int e, int64_t at) {
-      v.x[e] = raw1<TYPE>(px + at * cb, o);
-      v.dt[e] = raw1<TYPE>(pd + at * cb, o);
-      if (PASS != LOCAL_ENDS && a.z) v.z[e] = raw1<TYPE>(pz + at * cb, o);
-      v.B[e].load(pB + at * rb, ob, s, a.n);
-      if constexpr (PASS != LOCAL_ENDS) v.C[e].load(pC + at * rb, ob, s, a.n);
-      if (a.starts) v.fresh[e] = ps[at];
-    };
-    if (left <= 0) return;
-    if (left >= STEPS) {
+    const int n = left < STEPS ? left < 1 ? 1 : (int)left : STEPS;
+    int64_t xo = 0, no = 0;
 #pragma unroll
-      for (int e = 0; e < STEPS; ++e) one(e, e);
-    } else {  // the last steps, some of them twice
-#pragma unroll
-      for (int e = 0; e < STEPS; ++e) one(e, e < left ? e : left - 1);
+    for (int e = 0; e < STEPS; ++e) {
+      v.x[e] = raw1<TYPE>(px + xo, o);
+      v.dt[e] = raw1<TYPE>(pd + xo, o);
+      if constexpr (PASS != LOCAL_ENDS) v.z[e] = raw1<TYPE>(pz + xo, o);
+      v.B[e].load(pB + no, ob, s, a.n);
+      if constexpr (PASS != LOCAL_ENDS) v.C[e].load(pC + no, ob, s, a.n);
+      if (e + 1 < n) xo += cb, no += rb;
     }
-    px += STEPS * cb, pd += STEPS * cb, pz += STEPS * cb, pB += STEPS * rb, pC += STEPS * rb, ps += STEPS;
+    if (left > STEPS) px += STEPS * cb, pd += STEPS * cb, pz += STEPS * cb, pB += STEPS * rb, pC += STEPS * rb;
   };
   In v[2];
   load(v[0], te - ts);
@@ -89,8 +86,26 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   float sum = 0.f;
+  // the starts of 64 steps, a bit each, from the lanes' loads of one; those of the next
+  // 64 are on their way
+  uint64_t begins = 0;
+  uint8_t ahead = 0;
+  const int lane = threadIdx.x & 63;
+  const auto look = [&](int64_t t) {
+    if (t + lane < te) ahead = a.starts[t + lane];
+    else ahead = 0;
+  };
+  if (a.starts) look(ts);
 
   const auto run = [&](const In& v, int64_t t) {
+    if (a.starts) {
+      if ((t - ts) % 64 == 0) {
+        begins = __builtin_amdgcn_ballot_w64(ahead != 0);
+        look(t + 64);
+      } else {
+        begins >>= STEPS;
+      }
+    }
     const int n = te - t < STEPS ? (int)(te - t) : STEPS;
     if (PASS != LOCAL_ENDS && a.marks && t % MGN_MARK_STEPS == 0)
 #pragma unroll
@@ -100,7 +115,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
     // what is done once a column
     float x[STEPS], delta[STEPS], y[STEPS], f[STEPS];
     bool held = false;
-    uint32_t fresh = 0;
+    const uint32_t fresh = (uint32_t)begins & ((1u << n) - 1);
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
       x[e] = value1<TYPE>(v.x[e]);
@@ -126,9 +141,6 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
           f[e] = z * sigmoid(z);
         }
     }
-    if (a.starts)
-#pragma unroll
-      for (int e = 0; e < STEPS; ++e) fresh |= v.fresh[e];
     const auto step = [&](int e, auto some_held) {
       float d[4], w[4], r[4], B[NL], Cn[NL];
       quads(delta[e], d);
@@ -156,7 +168,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
-        if (a.starts && v.fresh[e]) {
+        if (fresh >> e & 1) {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll

@@ -189,18 +189,20 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   const float bias = a.bias && col < a.cols ? a.bias[col] : 0.f, D = a.D && col < a.cols ? a.D[col] : 0.f;
   double dD = 0, d_bias = 0;
   int par = 0;
-  const auto step_size = [&](uint32_t raw, bool ok) {
+  const auto step_size = [&](Word<TYPE> raw, bool ok) {
     float delta = value1<TYPE>(raw) + bias;
     if (a.softplus) delta = softplus(delta);
     return ok ? delta : 0.f;
   };
   // What a unit's steps bring, as it lies in memory.
   struct In {
-    uint32_t x[U], dt[U], o[U], z[U], fresh[U];
+    Word<TYPE> x[U], dt[U], o[U], z[U];
+    uint32_t fresh[U];
     Raw<TYPE, NL, FULL> B[U], C[U];
   };
   struct Sweep {
-    uint32_t x[U], dt[U], fresh[U];
+    Word<TYPE> x[U], dt[U];
+    uint32_t fresh[U];
     Raw<TYPE, NL, FULL> B[U];
   };
 
