@@ -167,7 +167,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   constexpr int GP = 1 << LG, RPW = 16 / GP, SIZE = sizeof(Elem<TYPE>);
   using Sums = GroupSums<2 * NL, LG>;
   __shared__ double accs[4 * NL][64 * NW];
-  __shared__ float subs[UNITS - 2][4 * NL][64 * NW];  // the states before units 1 .. UNITS - 2
+  // the states before units 0 .. UNITS - 2 (with 4 waves unit 0's are read again: two
+  // workgroups of a CU have no room for them)
+  constexpr int KEPT = NW == 4 ? 1 : 0;
+  __shared__ float subs[UNITS - 1 - KEPT][4 * NL][64 * NW];
   __shared__ float red[NW > 1 ? 2 : 1][NW > 1 ? NW : 1][NW > 1 ? U : 1][3][64];
   const int lane = threadIdx.x & 63, w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane & 3;
   const int tile = blockIdx.x % a.tiles, sub = (lane >> 2) >> LG;
@@ -197,12 +200,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   // What a unit's steps bring, as it lies in memory.
   struct In {
     Word<TYPE> x[U], dt[U], o[U], z[U];
-    uint32_t fresh[U];
     Raw<TYPE, NL, FULL> B[U], C[U];
   };
   struct Sweep {
     Word<TYPE> x[U], dt[U];
-    uint32_t fresh[U];
     Raw<TYPE, NL, FULL> B[U];
   };
 
@@ -223,6 +224,12 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
       }
     };
     load_states(a.chunks > 1 ? a.state + c * C * a.n : a.dh_last, G);
+    // the starts of a block's steps, from the lanes' loads of one; those of the block
+    // before are on their way.  (Without starts a byte of x stands in: no branch, where
+    // its ways meet the compiler waits as for the one with the fewest loads.)
+    const uint8_t* const starts = a.starts ? a.starts : (const uint8_t*)a.x;
+    const auto look = [&](int64_t t) { return starts[t + (lane & (K - 1)) < te ? t + (lane & (K - 1)) : te - 1]; };
+    uint8_t ahead = look((te - 1) / K * K);
 
     for (int64_t t0 = (te - 1) / K * K; t0 >= ts; t0 -= K) {
       const float* const mark = a.marks + t0 / K * C * a.n;
@@ -241,32 +248,38 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           if (GATE) r.z[e] = raw1<TYPE>((const char*)a.z + i, o);
           r.B[e].load((const char*)a.B + b, ob, s0, a.n);
           r.C[e].load((const char*)a.C + b, ob, s0, a.n);
-          r.fresh[e] = a.starts ? a.starts[t0 + v * U + at] : 0;
         }
       };
       const auto load_sweep = [&](int v, Sweep& r) {
         const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
-          r.x[e] = raw1<TYPE>((const char*)a.x + (xu + e * cb), o);
-          r.dt[e] = raw1<TYPE>((const char*)a.dt + (xu + e * cb), o);
-          r.B[e].load((const char*)a.B + (nu + e * rb), ob, s0, a.n);
-          r.fresh[e] = a.starts ? a.starts[t0 + v * U + e] : 0;
+          const int at = v * U + e < n ? e : 0;
+          r.x[e] = raw1<TYPE>((const char*)a.x + (xu + at * cb), o);
+          r.dt[e] = raw1<TYPE>((const char*)a.dt + (xu + at * cb), o);
+          r.B[e].load((const char*)a.B + (nu + at * rb), ob, s0, a.n);
         }
       };
+      const uint32_t begins =
+          a.starts ? (uint32_t)__builtin_amdgcn_ballot_w64(ahead != 0 && t0 + (lane & (K - 1)) < te) & ((1 << K) - 1) : 0;
+      ahead = look(t0 >= ts + K ? t0 - K : ts);
       // the states before each unit, its loads in flight while the one before it runs
       load_states(mark, h[0]);
-      In r;
-      Sweep now, next;
-      if (last) load_sweep(0, now);
-      load_unit(last, r);
-      for (int v = 0; v < last; ++v) {
-        if (v + 1 < last) load_sweep(v + 1, next);
-        if (v)
+      In units[2];
+      Sweep sweeps[2];
+      load_sweep(0, sweeps[0]);
+      load_unit(last, units[0]);
+#pragma unroll
+      for (int v = 0; v < UNITS - 1; ++v) {
+        if (v >= last) break;
+        const Sweep& now = sweeps[v % 2];
+        load_sweep(v + 1 < last ? v + 1 : v, sweeps[(v + 1) % 2]);
+        if (v >= KEPT)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int k = 0; k < NL; ++k) subs[v - 1][j * NL + k][threadIdx.x] = h[0][j][k];
+            for (int k = 0; k < NL; ++k) subs[v - KEPT][j * NL + k][threadIdx.x] = h[0][j][k];
+        const uint32_t fresh = begins >> (v * U) & ((1 << U) - 1);
         float delta[U];
         bool held = false;
 #pragma unroll
@@ -283,36 +296,34 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int k = 0; k < NL; ++k)  // B may hold anything where a column's step has size 0
-              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && now.fresh[e] ? 0.f : h[0][j][k],
+              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && fresh >> e & 1 ? 0.f : h[0][j][k],
                                 slow() ? mul_or_0(u[j], B[k]) : u[j] * B[k]);
         };
-        if (!(now.fresh[0] | now.fresh[1]) && !any(held)) {
+        if (!fresh && !any(held)) {
 #pragma unroll
           for (int e = 0; e < U; ++e) step(e, std::false_type());
         } else {
 #pragma unroll
           for (int e = 0; e < U; ++e) step(e, std::true_type());
         }
-        now = next;
       }
       float dA[4][NL], sD = 0.f, sb = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int k = 0; k < NL; ++k) dA[j][k] = 0.f;
-      for (int v = last; v >= 0; --v) {
+      const auto unit = [&](int v, const In& r) {
         const int m = n - v * U < U ? n - v * U : U;  // the unit's steps
         const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb, tu = t0 + v * U;
-        if (v != last) load_unit(v, r);
-        uint32_t(&fresh)[U] = r.fresh;
+        const bool fresh[U] = {(begins >> (v * U) & 1) != 0, (begins >> (v * U + 1) & 1) != 0};
         if (v != last) {
-          if (v == 0) {
+          if (v < KEPT) {
             load_states(mark, h[0]);
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int k = 0; k < NL; ++k) h[0][j][k] = subs[v - 1][j * NL + k][threadIdx.x];
+              for (int k = 0; k < NL; ++k) h[0][j][k] = subs[v - KEPT][j * NL + k][threadIdx.x];
           }
         }
         float delta[U], ov[U], sz[U], f[U][4][NL], tB[U], tA[U], ty[U], p[U][2 * NL];
@@ -329,7 +340,6 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           }
           // a step that is not there changes nothing
           if (!ok || e >= m) delta[e] = ov[e] = 0.f;
-          if (e >= m) fresh[e] = 0;
         }
         const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(r.x[e])); };
         const auto forth = [&](int e, auto first, auto some_held) {
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
             for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
         };
-        if (!any(held) && !(fresh[0] | fresh[1])) {
+        if (!any(held) && !fresh[0] && !fresh[1]) {
           forth(0, std::false_type(), std::false_type());
           forth(1, std::false_type(), std::false_type());
         } else {
@@ -461,6 +471,14 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
             }
           }
         if constexpr (NW > 1) par ^= 1;
+      };
+      for (int v = last;; v -= 2) {
+        load_unit(v > 0 ? v - 1 : 0, units[1]);  // while this one runs
+        unit(v, units[0]);
+        if (v == 0) break;
+        load_unit(v > 1 ? v - 2 : 0, units[0]);
+        unit(v - 1, units[1]);
+        if (v == 1) break;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
