@@ -317,7 +317,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         const int64_t xu = x0 + v * U * cb, nu = n0 + v * U * rb, tu = t0 + v * U;
         const bool fresh[U] = {(begins >> (v * U) & 1) != 0, (begins >> (v * U + 1) & 1) != 0};
         if (v != last) {
-          if (v < KEPT) {
+          if (KEPT && v < KEPT) {
             load_states(mark, h[0]);
           } else {
 #pragma unroll
