@@ -70,14 +70,13 @@ struct Place {
 };
 
 // Steps since the last start at or before step t, at most W: how far back step t
-// + 1's predecessors go.
+// + 1's predecessors go.  A lane looks at one step.
 template <int W>
 __device__ __forceinline__ int age_at(const uint8_t* starts, int64_t t) {
-  int n = W;
-  if (starts)
-    for (int k = W - 1; k >= 0; --k)
-      if (t - k >= 0 && starts[t - k]) n = k;
-  return n;
+  if (!starts || t < 0) return W;
+  const int lane = threadIdx.x & 63, k = lane < W && lane <= t ? lane : 0;
+  const uint64_t m = __builtin_amdgcn_ballot_w64(starts[t - k] != 0 && k == lane);
+  return m ? __builtin_ctzll(m) : W;
 }
 
 template <int W, class P>
@@ -93,20 +92,6 @@ __device__ __forceinline__ void load_taps(const ConvArgs& a, const P& p, float (
       for (int j = 1; j < W; ++j) all[j] = a.w[(int64_t)c * W + j];
 #pragma unroll
     for (int j = 0; j < W; ++j) w[j][k] = all[j];
-  }
-}
-
-// Inputs t0 - (W - 1) .. t0 - 1 of a row, oldest first.
-template <int TYPE, int W, class P>
-__device__ __forceinline__ void load_before(const ConvArgs& a, const P& p, int64_t t0, int64_t C, int64_t i, bool ok,
-                                            float (*xs)[V]) {
-#pragma unroll
-  for (int j = 0; j < W - 1; ++j) {
-    const int64_t t = t0 - (W - 1) + j;
-#pragma unroll
-    for (int k = 0; k < V; ++k) xs[j][k] = 0.f;
-    if (ok && t >= 0) p.template load<TYPE>(a.x, t * C + i, xs[j]);
-    else if (ok && a.past) p.template load<TYPE>(a.past, (t + W - 1) * C + i, xs[j]);
   }
 }
 
@@ -130,35 +115,86 @@ __device__ __forceinline__ void taps(const float (*xs)[V], const float (&w)[W][V
   }
 }
 
-// What some steps bring, as it lies in memory; N arrays.  PAST: read past the caches.
+// A thread's columns of a step, as they lie in memory.
+template <int TYPE, bool NEAR, bool PAST>
+__device__ __forceinline__ void load_raw(const Place<TYPE, NEAR>& p, const void* x, int64_t i, Raw<TYPE, V, NEAR>& r) {
+  const Elem<TYPE>* const q = (const Elem<TYPE>*)x + i;
+  if constexpr (!NEAR) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) __builtin_memcpy(&r.w[k], q + p.at(k), sizeof(*q));
+  } else if constexpr (PAST) {
+    r.stream((const char*)q);
+  } else {
+    r.load((const char*)q, 0, 0, V);
+  }
+}
+
+// What some steps bring; N arrays.  PAST: read past the caches.  Loaded a unit ahead of
+// its use, without a branch between the loads or around them: where its ways meet, the
+// compiler waits as for the one with the fewest loads.
 template <int TYPE, int STEPS, int N, bool NEAR, bool PAST>
 struct Inputs {
   Raw<TYPE, V, NEAR> v[N][STEPS];
-  uint32_t fresh[STEPS];
   // steps t .. of those before `end` (the last of them again for those that are not)
-  __device__ __forceinline__ void load(const ConvArgs& a, const Place<TYPE, NEAR>& p, const void* x, const void* y, int64_t t,
-                                       int64_t end, int64_t C, int64_t i) {
-    if (t >= end) return;
+  __device__ __forceinline__ void load(const Place<TYPE, NEAR>& p, const void* x, const void* y, int64_t t, int64_t end,
+                                       int64_t C, int64_t i) {
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
       const int64_t s = t + e < end ? t + e : end - 1;
-      one(p, x, s * C + i, v[0][e]);
-      if constexpr (N > 1) one(p, y, s * C + i, v[1][e]);
-      fresh[e] = a.starts ? a.starts[s] : 0;
+      load_raw<TYPE, NEAR, PAST>(p, x, s * C + i, v[0][e]);
+      if constexpr (N > 1) load_raw<TYPE, NEAR, PAST>(p, y, s * C + i, v[1][e]);
     }
   }
-  __device__ __forceinline__ void one(const Place<TYPE, NEAR>& p, const void* x, int64_t i, Raw<TYPE, V, NEAR>& r) {
-    const Elem<TYPE>* const q = (const Elem<TYPE>*)x + i;
-    if constexpr (!NEAR) {
+};
+
+// unit(in, t, all) for the units of steps t0 .. t1, each one's inputs (the first's are
+// there) loaded while the one before it runs; all: it has all of its STEPS steps.
+template <int STEPS, class In, class Load, class Unit>
+__device__ __forceinline__ void in_units(int64_t t0, int64_t t1, In (&in)[2], Load load, Unit unit) {
+  int64_t t = t0;
+  while (t + STEPS < t1) {
+    load(in[1], t + STEPS);
+    unit(in[0], t, std::true_type());
+    t += STEPS;
+    if (t + STEPS >= t1) {
+      in[0] = in[1];
+      break;
+    }
+    load(in[0], t + STEPS);
+    unit(in[1], t, std::true_type());
+    t += STEPS;
+  }
+  unit(in[0], t, std::false_type());
+}
+
+// The window BY steps on: a unit's, or (its indexes have to be constants) one after
+// each step of a unit that may have fewer.
+template <int BY, int N>
+__device__ __forceinline__ void forward(float (&v)[N][V]) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        if constexpr (TYPE == MGN_BF16) r.w[k] = q[p.at(k)];
-        else r.w[k] = __float_as_uint(q[p.at(k)]);
-      }
-    } else if constexpr (PAST) {
-      r.stream((const char*)q);
-    } else {
-      r.load((const char*)q, 0, 0, V);
+  for (int j = 0; j + BY < N; ++j)
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[j][k] = v[j + BY][k];
+}
+
+// Inputs t0 - (W - 1) .. t0 - 1 of a row, oldest first.
+template <int TYPE, int W, bool NEAR>
+struct Before {
+  Raw<TYPE, V, NEAR> v[W > 1 ? W - 1 : 1];
+  __device__ __forceinline__ void load(const ConvArgs& a, const Place<TYPE, NEAR>& p, int64_t t0, int64_t C, int64_t i) {
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      const int64_t t = t0 - (W - 1) + j;
+      const void* const from = t >= 0 || !a.past ? a.x : a.past;  // (without past anything that is there)
+      load_raw<TYPE, NEAR, false>(p, from, (t >= 0 ? t : a.past ? t + W - 1 : 0) * C + i, v[j]);
+    }
+  }
+  __device__ __forceinline__ void get(const ConvArgs& a, int64_t t0, bool ok, float (*xs)[V]) const {
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      v[j].get(0, V, xs[j]);
+#pragma unroll
+      for (int k = 0; k < V; ++k) xs[j][k] = ok && (t0 - (W - 1) + j >= 0 || a.past) ? xs[j][k] : 0.f;
     }
   }
 };
@@ -175,37 +211,34 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V];
-    Inputs<TYPE, STEPS, 1, NEAR, PAST> now, next;
-    now.load(a, p, a.x, nullptr, t0, t1, C, i);
-    load_before<TYPE, W>(a, p, t0, C, i, ok, xs);
+    Starts starts(a.starts, t0, t1);
+    Before<TYPE, W, NEAR> before;
+    Inputs<TYPE, STEPS, 1, NEAR, PAST> in[2];
+    before.load(a, p, t0, C, i);
+    in[0].load(p, a.x, nullptr, t0, t1, C, i);
     int age = age_at<W>(a.starts, t0 - 1);
-    for (int64_t t = t0; t < t1; t += STEPS) {
-      next.load(a, p, a.x, nullptr, t + STEPS, t1, C, i);  // while these steps run
-      const int n = t1 - t < STEPS ? (int)(t1 - t) : STEPS;
+    before.get(a, t0, ok, xs);
+    const auto unit = [&](const Inputs<TYPE, STEPS, 1, NEAR, PAST>& now, int64_t t, auto all) __attribute__((always_inline)) {
+      const int n = all() || t1 - t >= STEPS ? STEPS : (int)(t1 - t);
+      const uint32_t fresh = starts.at<STEPS>(t);
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) now.v[0][e].get(0, V, xs[W - 1 + e]);
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
-        age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
+        age = fresh >> e & 1 ? 0 : age < W ? age + 1 : W;
         float v[V];
-        taps<W>(xs + e, w, b, age, v);
+        taps<W>(xs + (all() ? e : 0), w, b, age, v);
         if (a.silu) {
 #pragma unroll
           for (int k = 0; k < V; ++k) v[k] *= sigmoid(v[k]);
         }
         if (ok) p.template store<TYPE>(a.y, (t + e) * C + i, v);
+        if (!all()) forward<1>(xs);
       }
-      // the last W - 1 inputs to the front
-#pragma unroll
-      for (int e = 1; e <= STEPS; ++e)
-        if (e == n)
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-            for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k];
-      now = next;
-    }
+      if (all()) forward<STEPS>(xs);
+    };
+    in_units<STEPS>(t0, t1, in, [&](auto& to, int64_t t) { to.load(p, a.x, nullptr, t, t1, C, i); }, unit);
     if (a.past_out && ok && s + 1 == a.segs) {
       // what the next window's steps see: nothing from before the last start
 #pragma unroll
@@ -253,23 +286,26 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
     const bool ok = p.ok && r < a.rows;
     const int64_t i = ok ? r * a.cols + p.c : 0;
     float xs[W - 1 + STEPS][V], g[W - 1 + STEPS][V];  // g[j]: gradient of the input of xs[j]
-    Inputs<TYPE, STEPS, 2, NEAR, false> now, next;
-    now.load(a, p, a.x, a.dy, t0, te, C, i);
-    load_before<TYPE, W>(a, p, t0, C, i, ok, xs);
+    Starts starts(a.starts, t0, te);
+    Before<TYPE, W, NEAR> before;
+    Inputs<TYPE, STEPS, 2, NEAR, false> in[2];
+    before.load(a, p, t0, C, i);
+    in[0].load(p, a.x, a.dy, t0, te, C, i);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
 #pragma unroll
       for (int k = 0; k < V; ++k) g[j][k] = 0.f;
     int age = age_at<W>(a.starts, t0 - 1);
+    before.get(a, t0, ok, xs);
     // the gradient of input t, complete
     const auto out = [&](int64_t t, const float (&v)[V]) {
       if (!ok || t >= t1) return;
       if (t >= t0) p.template store<TYPE>(a.y, t * C + i, v);
       else if (t < 0 && a.d_past) p.template store<MGN_FP32>(a.d_past, (t + W - 1) * C + i, v);
     };
-    for (int64_t t = t0; t < te; t += STEPS) {
-      next.load(a, p, a.x, a.dy, t + STEPS, te, C, i);  // while these steps run
-      const int n = te - t < STEPS ? (int)(te - t) : STEPS;
+    const auto unit = [&](const Inputs<TYPE, STEPS, 2, NEAR, false>& now, int64_t t, auto all) __attribute__((always_inline)) {
+      const uint32_t fresh = starts.at<STEPS>(t);
+      const int n = all() || te - t >= STEPS ? STEPS : (int)(te - t);
       float d[STEPS][V];
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
@@ -284,10 +320,11 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
-        age = now.fresh[e] ? 0 : age < W ? age + 1 : W;
+        const int at = all() ? e : 0;
+        age = fresh >> e & 1 ? 0 : age < W ? age + 1 : W;
         if (a.silu) {
           float v[V];
-          taps<W>(xs + e, w, b, age, v);
+          taps<W>(xs + at, w, b, age, v);
 #pragma unroll
           for (int k = 0; k < V; ++k) {
             const float f = sigmoid(v[k]);
@@ -300,24 +337,19 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
           if (W - 1 - j <= age)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-              g[e + j][k] = fmaf(w[j][k], d[e][k], g[e + j][k]);
-              if (mine) sw[j][k] = fmaf(d[e][k], xs[e + j][k], sw[j][k]);
+              g[at + j][k] = fmaf(w[j][k], d[e][k], g[at + j][k]);
+              if (mine) sw[j][k] = fmaf(d[e][k], xs[at + j][k], sw[j][k]);
             }
         if (mine)
 #pragma unroll
           for (int k = 0; k < V; ++k) sb[k] += d[e][k];
-        out(t + e - (W - 1), g[e]);
+        out(t + e - (W - 1), g[at]);
+        if (!all()) forward<1>(xs), forward<1>(g);
       }
       if (++turn % (SUM_STEPS / STEPS) == 0) add();
-#pragma unroll
-      for (int e = 1; e <= STEPS; ++e)
-        if (e == n)
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-            for (int k = 0; k < V; ++k) xs[j][k] = xs[e + j][k], g[j][k] = g[e + j][k];
-      now = next;
-    }
+      if (all()) forward<STEPS>(xs), forward<STEPS>(g);
+    };
+    in_units<STEPS>(t0, te, in, [&](auto& to, int64_t t) { to.load(p, a.x, a.dy, t, te, C, i); }, unit);
     if (s + 1 == a.segs) {
       // the inputs that steps after the last one see
 #pragma unroll
@@ -449,7 +481,7 @@ hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
       constexpr int STEPS = 4;
       if (near && past) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, true>), grid, dim3(NT), 0, st, m);
       else if (near) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, false>), grid, dim3(NT), 0, st, m);
-      else hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, false, false>), grid, dim3(NT), 0, st, m);
+      else hipLaunchKernelGGL((conv_kernel<ty(), w(), 2, false, false>), grid, dim3(NT), 0, st, m);
     };
     if (type == MGN_BF16) go(Int<MGN_BF16>());
     else go(Int<MGN_FP32>());

@@ -38,6 +38,35 @@ __device__ __forceinline__ void write1(char* base, uint32_t o, float v) {
   if constexpr (TYPE == MGN_BF16) *(uint16_t*)(base + here(o)) = (uint16_t)pack_bf16(v, 0.f);
   else *(float*)(base + here(o)) = v;
 }
+// The starts of trajectories, a bit a step, from the lanes' loads of one step each: 64
+// steps at once, those of the next 64 on their way while these are used.
+struct Starts {
+  const uint8_t* starts;
+  int64_t first, end;
+  uint64_t bits = 0;
+  uint8_t ahead = 0;
+  __device__ __forceinline__ Starts(const uint8_t* s, int64_t t0, int64_t t1) : starts(s), first(t0), end(t1) {
+    if (starts) look(t0);
+  }
+  __device__ __forceinline__ void look(int64_t t) {
+    t += threadIdx.x & 63;
+    ahead = 0;
+    if (t < end) ahead = starts[t];
+  }
+  // Those of steps t .. t + STEPS - 1 in the lowest bits; asked for in order, from t0 on.
+  template <int STEPS>
+  __device__ __forceinline__ uint32_t at(int64_t t) {
+    static_assert(64 % STEPS == 0);
+    if (!starts) return 0;
+    if ((t - first) % 64 == 0) {
+      bits = __builtin_amdgcn_ballot_w64(ahead != 0);
+      look(t + 64);
+    } else {
+      bits >>= STEPS;
+    }
+    return (uint32_t)bits & ((1u << STEPS) - 1);
+  }
+};
 // NL numbers as they lie in memory, so that a load in flight is not waited for
 // before its step comes: numbers s .. of the n at byte o.
 template <int TYPE, int NL, bool FULL>

@@ -86,26 +86,9 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   float sum = 0.f;
-  // the starts of 64 steps, a bit each, from the lanes' loads of one; those of the next
-  // 64 are on their way
-  uint64_t begins = 0;
-  uint8_t ahead = 0;
-  const int lane = threadIdx.x & 63;
-  const auto look = [&](int64_t t) {
-    if (t + lane < te) ahead = a.starts[t + lane];
-    else ahead = 0;
-  };
-  if (a.starts) look(ts);
+  Starts starts(a.starts, ts, te);
 
   const auto run = [&](const In& v, int64_t t) {
-    if (a.starts) {
-      if ((t - ts) % 64 == 0) {
-        begins = __builtin_amdgcn_ballot_w64(ahead != 0);
-        look(t + 64);
-      } else {
-        begins >>= STEPS;
-      }
-    }
     const int n = te - t < STEPS ? (int)(te - t) : STEPS;
     if (PASS != LOCAL_ENDS && a.marks && t % MGN_MARK_STEPS == 0)
 #pragma unroll
@@ -115,7 +98,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
     // what is done once a column
     float x[STEPS], delta[STEPS], y[STEPS], f[STEPS];
     bool held = false;
-    const uint32_t fresh = (uint32_t)begins & ((1u << n) - 1);
+    const uint32_t fresh = starts.at<STEPS>(t);
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
       x[e] = value1<TYPE>(v.x[e]);
