@@ -20,7 +20,7 @@ namespace mgn {
 namespace {
 
 constexpr int NT = 256;
-enum Pass { WHOLE_AXIS, LOCAL_ENDS, FROM_STATES, ONE_STEP };
+enum Pass { WHOLE_AXIS, MANY_ROWS, LOCAL_ENDS, FROM_STATES, ONE_STEP };
 
 // What some steps bring, as it lies in memory.
 template <int TYPE, int NL, bool FULL, int STEPS>
@@ -31,7 +31,10 @@ struct Inputs {
 
 template <int TYPE, int NL, bool FULL, int PASS>
 __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
-  constexpr int STEPS = PASS == ONE_STEP || NL == 16 ? 1 : NL == 8 ? 2 : 4;  // steps whose loads are in flight together
+  // Steps whose loads are in flight together.  With many rows two of them and a third
+  // wave in a SIMD's registers: 20 steps of 20,011 x 64 bf16 135 us, 161 with four;
+  // 600 steps of 1,885 x 64, two waves a SIMD in any case, 418 and 411.
+  constexpr int STEPS = PASS == ONE_STEP || NL == 16 ? 1 : NL == 8 || (NL == 4 && PASS == MANY_ROWS) ? 2 : 4;
   using E = Elem<TYPE>;
   using In = Inputs<TYPE, NL, FULL, STEPS>;
   constexpr int SIZE = sizeof(E);
@@ -269,6 +272,7 @@ hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
     }
     return e;
   };
+  if constexpr (PASS == MANY_ROWS) return go(Int<4>());
   if (a.n <= 4) return go(Int<1>());
   if (a.n <= 8) return go(Int<2>());
   if (a.n <= 16) return go(Int<4>());
@@ -279,7 +283,11 @@ hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
 template <int TYPE>
 hipError_t launch_typed(SsmArgs& a, hipStream_t st) {
   if (a.steps == 1) return launch_pass<TYPE, ONE_STEP>(a, 1, st);
-  if (a.chunks == 1) return launch_pass<TYPE, WHOLE_AXIS>(a, 1, st);
+  if (a.chunks == 1) {
+    const int64_t waves = (a.rows * ((a.cols + 3) / 4) + 15) / 16;
+    if (a.n > 8 && a.n <= 16 && waves > WAVES) return launch_pass<TYPE, MANY_ROWS>(a, 1, st);
+    return launch_pass<TYPE, WHOLE_AXIS>(a, 1, st);
+  }
   hipError_t e = launch_pass<TYPE, LOCAL_ENDS>(a, a.chunks - 1, st);
   if (e == hipSuccess) e = launch_ssm_join(a, a.h0, false, st);
   return e == hipSuccess ? launch_pass<TYPE, FROM_STATES>(a, a.chunks, st) : e;

@@ -573,10 +573,13 @@ Deal deal(int64_t steps, int64_t rows, int cols, int n) {
 template <class F>
 hipError_t by_states(int n, F f) {
   const std::false_type part;
+  const std::true_type whole;
   if (n <= 4) return f(Int<1>(), Int<1>(), part);
-  if (n == 16) return f(Int<4>(), Int<1>(), std::true_type());
+  if (n == 16) return f(Int<4>(), Int<1>(), whole);
   if (n <= 16) return f(Int<4>(), Int<1>(), part);
+  if (n == 32) return f(Int<4>(), Int<2>(), whole);
   if (n <= 32) return f(Int<4>(), Int<2>(), part);
+  if (n == 64) return f(Int<4>(), Int<4>(), whole);
   return f(Int<4>(), Int<4>(), part);
 }
 template <class F>
