@@ -12,6 +12,10 @@
 // The backward adds w d_t to the gradients of the W inputs that step t saw, and
 // passes on the oldest: it needs each d once, and the pre-activation is formed
 // again from the inputs that it holds.
+//
+// Bound by memory.  20 steps of 100,003 x 64 bf16, 4 taps, 91 us (5.6 TB/s); the
+// backward of 600 steps of 1,885 x 128 fp32 350 us (5.0 TB/s).  8 columns a lane took
+// 129 us of then 117; 2 steps a unit in the backward 389 of 350 (fp32).
 #include <type_traits>
 
 #include "raw.h"
@@ -418,8 +422,8 @@ __global__ __launch_bounds__(NT) void past_tail_kernel(ConvArgs a, int W) {
 constexpr int64_t FWD_WGS = 4096;   // workgroups that a forward launch wants
 constexpr int64_t MOST_WGS = 1 << 20;
 // A forward that moves more than the last-level cache holds reads past it: 20 steps of
-// 100,003 x 64 bf16 115 us through it, 108 past it; its backward 352 and 354 (600 steps
-// of 1,885 x 128 fp32).
+// 100,003 x 64 bf16 94 us through it, 91 past it (the backward of 600 steps of 1,885 x
+// 128 fp32 gained nothing).
 constexpr int64_t CACHE = (int64_t)256 << 20;
 constexpr int64_t LEAST_SEG = 8;    // steps of a segment (a short one reads its neighbours' steps again, but only where the card has room)
 
@@ -478,6 +482,8 @@ hipError_t launch_conv(ConvArgs a, int type, int width, hipStream_t st) {
   const dim3 grid((unsigned)(items < MOST_WGS ? items : MOST_WGS), (unsigned)a.tiles);
   const hipError_t e = by_width(width, [&](auto w) {
     const auto go = [&](auto ty) {
+      // (columns apart take four times the loads: 6 steps of 120,113 x 61 bf16, 6 taps, 121
+      // us with 2 steps a unit, 153 with 4)
       constexpr int STEPS = 4;
       if (near && past) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, true>), grid, dim3(NT), 0, st, m);
       else if (near) hipLaunchKernelGGL((conv_kernel<ty(), w(), STEPS, true, false>), grid, dim3(NT), 0, st, m);
@@ -510,6 +516,8 @@ hipError_t launch_conv_grad(ConvArgs a, int type, int width, float* dw, float* d
     const dim3 grid((unsigned)parts, (unsigned)a.tiles);
     const hipError_t e = by_width(width, [&](auto w) {
       const auto go = [&](auto ty) {
+        // (4 taps with 2 steps: fp32 389 us of 350, bf16 249 of 260; more taps leave no
+        // registers for 4)
         constexpr int STEPS = w() > 4 ? 2 : 4;
         if (near) hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), STEPS, true>), grid, dim3(NT), 0, st, a);
         else hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), 2, false>), grid, dim3(NT), 0, st, a);

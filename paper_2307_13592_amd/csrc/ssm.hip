@@ -11,9 +11,12 @@
 // sum is one number a column), a third runs every chunk from the state that enters
 // it.  A chunk's work is then done twice but for y.
 //
-// Bound by the vector units: an exponential takes the time of 4 other
-// instructions, and there are 4 of these for a state and step, against 6 - 16 bytes
-// an element; with one step by the states' 8 n bytes.
+// Bound by the vector units: 4 products and sums and an exponential, which takes two
+// instructions' time, for a state and step, and some 60 instructions a step for what is
+// done once a column and for the exchanges, against 6 - 16 bytes an element.  600 steps
+// of 1,885 x 64 bf16, 16 states, 400 us (the units busy 76 %: some SIMDs have one wave,
+// some two), 466 where loads stood in branches; 20 steps of 20,011 x 64 133 us.  With
+// one step by the states' 8 n bytes: 1,885 x 128 fp32 7.3 us, 4.7 TB/s.
 #include "ssm.h"
 
 namespace mgn {

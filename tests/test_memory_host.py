@@ -166,6 +166,8 @@ def test_gradient_list_refusals():
     _refused(create((None, b, 5, F32))[0], "NULL")
     _refused(create((a + 2, None, 5, F32))[0], "misaligned")
     _refused(create((a, b + 1, 5, BF16))[0], "misaligned")
+    for t in ((1 << 48, None, 5, F32), (a, 1 << 60, 5, F32)):
+        _refused(create(t)[0], "device address")
     for ts in ([(a, None, 5, F32), (a, None, 5, F32)], [(a, None, 5, F32), (a + 16, b, 5, F32)], [(a, a + 4, 5, F32)],
                [(a, b, 5, F32), (c, b + 8, 5, F32)], [(a, b, 5, F32), (b, c, 5, F32)], [(a, c, 50, F32), (a + 40, a + 400, 5, BF16), (b, a + 100, 3, F32)]):
         _refused(create(*ts)[0], "overlapping")
