@@ -81,6 +81,30 @@ def test_trajectories_in_one_window(T, rows, cols, dtype, starts):
         _check(_case(T, rows, cols, W, dtype, starts=starts, state=False, silu=False, seed=2))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,rows,cols,W,starts", [(70, 33_000, 64, 4, True), (131, 140_000, 9, 8, True), (67, 33_000, 62, 3, False)])
+def test_long_segments_of_many_rows(T, rows, cols, W, starts, dtype):
+    """More than 64 steps at once (whose starts are looked at 64 at a time): some rows."""
+    print(f"[conv] long {T} x {rows} x {cols}, {W} {dtype}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    t = lambda *s: torch.randn(s, generator=g, device="cuda")
+    c = dict(x=t(T, rows, cols).to(dtype), weight=t(cols, W), bias=t(cols), silu=True, starts=None,
+             past=t(W - 1, rows, cols).to(dtype), dy=t(T, rows, cols).to(dtype), d_past_out=t(W - 1, rows, cols))
+    if starts:
+        c["starts"] = torch.zeros(T, dtype=torch.uint8, device="cuda")
+        c["starts"][[3, 4, 40, 63, 64, 66]] = 1
+    got = _run(c) + _back(c)
+    some = [0, 15, 16, rows // 2, rows - 1]
+    few = {k: v[:, some].contiguous() if k in ("x", "past", "dy", "d_past_out") else v for k, v in c.items()}
+    a = _ref(few)
+    y64, e, out64 = ref.conv(*a)
+    ref.near("y", got[0][:, some], y64, e, dtype)
+    assert np.array_equal(ref.f64(got[1][:, some]), out64)
+    r = ref.conv_grad(*a, ref.f64(few["dy"]), ref.f64(few["d_past_out"]))
+    ref.near("dx", got[2][:, some], r[0], r[4], dtype)
+    ref.near("d_past", got[5][:, some], r[3], r[7])
+
+
 @pytest.mark.parametrize("T,rows,cols", [(9, 30, 64), (700, 1, 33)])
 def test_nothing_before_a_start_is_seen(T, rows, cols):
     """NaN and infinite inputs, past and gradients before a start stay there."""

@@ -107,6 +107,31 @@ def test_every_kind_of_width(cols):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,rows,cols,n", [(75, 2101, 64, 16), (130, 1100, 62, 11), (66, 2500, 60, 13), (67, 1100, 64, 3), (129, 600, 128, 8),
+                                           (65, 1030, 64, 40)])
+def test_long_axes_of_many_rows(T, rows, cols, n, dtype):
+    """More than 64 steps at once (whose starts are looked at 64 at a time), up to more
+    waves than the card holds: some rows."""
+    print(f"[ssm] long {T} x {rows} x {cols}, {n} {dtype}", flush=True)
+    c = _case(T, rows, cols, n, dtype, starts=0.05, seed=15)
+    c["starts"][[2, 63, 64]] = 1
+    assert mgn.mgn_selective_scan_work(T, rows, cols, n) == 0
+    y, last, marks = _forward(c)
+    g = _backward(c, marks)
+    some = [0, 15, 16, rows // 2, rows - 1]
+    few = {k: v[:, some].contiguous() if k in ("x", "dt", "B", "C", "z", "dy") else v[some].contiguous() if k in ("h0", "dh_last") else v
+           for k, v in c.items()}
+    r = _ref(few)
+    f = ref.ssm(r, T)
+    ref.near("y", y[:, some], f["y"], f["ey"], dtype)
+    ref.near("h_last", last[some], f["last"], f["elast"])
+    want = ref.ssm_grad(r, f, r["dy"], r["dh_last"], tiles=-(-cols // 64), chunk=T)
+    for k in ("dx", "ddt", "dB", "dC", "dz"):
+        ref.near(k, g[k][:, some], *want[k], dtype)
+    ref.near("dh0", g["dh0"][some], *want["dh0"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("T,rows,cols,n", [(1, 5, 64, 16), (20, 33, 64, 16), (30, 2, 7, 3), (700, 1, 70, 16), (130, 1, 64, 40)])
 @pytest.mark.parametrize("starts", [0.03, 0.3, 1.1])
 def test_trajectories_in_one_window(T, rows, cols, n, dtype, starts):
