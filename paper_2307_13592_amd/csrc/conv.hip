@@ -129,7 +129,7 @@ __device__ __forceinline__ void load_raw(const Place<TYPE, NEAR>& p, const void*
   } else if constexpr (PAST) {
     r.stream((const char*)q);
   } else {
-    r.load((const char*)q, 0, 0, V);
+    r.load((const char*)q, 0);
   }
 }
 
@@ -196,7 +196,7 @@ struct Before {
   __device__ __forceinline__ void get(const ConvArgs& a, int64_t t0, bool ok, float (*xs)[V]) const {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
-      v[j].get(0, V, xs[j]);
+      v[j].get(xs[j]);
 #pragma unroll
       for (int k = 0; k < V; ++k) xs[j][k] = ok && (t0 - (W - 1) + j >= 0 || a.past) ? xs[j][k] : 0.f;
     }
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(NT) void conv_kernel(ConvArgs a) {
       const int n = all() || t1 - t >= STEPS ? STEPS : (int)(t1 - t);
       const uint32_t fresh = starts.at<STEPS>(t);
 #pragma unroll
-      for (int e = 0; e < STEPS; ++e) now.v[0][e].get(0, V, xs[W - 1 + e]);
+      for (int e = 0; e < STEPS; ++e) now.v[0][e].get(xs[W - 1 + e]);
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
@@ -313,8 +313,8 @@ __global__ __launch_bounds__(NT) void conv_grad_kernel(ConvArgs a) {
       float d[STEPS][V];
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
-        now.v[0][e].get(0, V, xs[W - 1 + e]);
-        now.v[1][e].get(0, V, d[e]);
+        now.v[0][e].get(xs[W - 1 + e]);
+        now.v[1][e].get(d[e]);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
           g[W - 1 + e][k] = 0.f;

@@ -68,19 +68,13 @@ struct Starts {
   }
 };
 // NL numbers as they lie in memory, so that a load in flight is not waited for
-// before its step comes: numbers s .. of the n at byte o.
-template <int TYPE, int NL, bool FULL>
+// before its step comes.  NEAR: neighbours, which are read at once.
+template <int TYPE, int NL, bool NEAR>
 struct Raw {
-  static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = FULL ? (NL * SIZE + 3) / 4 : NL;
-  std::conditional_t<FULL, uint32_t, Word<TYPE>> w[WORDS];
-  __device__ __forceinline__ void load(const char* base, uint32_t o, int s, int n) {
-    if constexpr (FULL) {
-      __builtin_memcpy(w, base + here(o + (uint32_t)(s * SIZE)), NL * SIZE);
-    } else {
-#pragma unroll
-      for (int k = 0; k < NL; ++k) w[k] = raw1<TYPE>(base, o + (uint32_t)((s + k < n ? s + k : n - 1) * SIZE));
-    }
-  }
+  static constexpr int SIZE = sizeof(Elem<TYPE>), WORDS = NEAR ? (NL * SIZE + 3) / 4 : NL;
+  std::conditional_t<NEAR, uint32_t, Word<TYPE>> w[WORDS];
+  // Those from byte `o` from the base on.
+  __device__ __forceinline__ void load(const char* base, uint32_t o) { __builtin_memcpy(w, base + here(o), NL * SIZE); }
   // All numbers at p, past the caches.
   __device__ __forceinline__ void stream(const char* p) {
     if constexpr (WORDS == 2) {
@@ -92,12 +86,11 @@ struct Raw {
       w[0] = u[0], w[1] = u[1], w[2] = u[2], w[3] = u[3];
     }
   }
-  __device__ __forceinline__ void get(int s, int n, float (&v)[NL]) const {
+  __device__ __forceinline__ void get(float (&v)[NL]) const {
 #pragma unroll
     for (int k = 0; k < NL; ++k) {
-      if constexpr (!FULL || TYPE != MGN_BF16) v[k] = value1<TYPE>((Word<TYPE>)w[k]);
+      if constexpr (!NEAR || TYPE != MGN_BF16) v[k] = value1<TYPE>((Word<TYPE>)w[k]);
       else v[k] = __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-      if constexpr (!FULL) v[k] = s + k < n ? v[k] : 0.f;
     }
   }
 };

@@ -62,21 +62,34 @@ __device__ __forceinline__ void store1(void* p, int64_t i, float v) {
   put<1>((Elem<TYPE>*)p + i, &v);
 }
 
-// NL of the n numbers at p + i, from number s on; FULL: all of them are there.
-template <int TYPE, int NL, bool FULL>
-__device__ __forceinline__ void load_n(const void* p, int64_t i, int s, int n, float (&v)[NL]) {
-  const Elem<TYPE>* r = (const Elem<TYPE>*)p + i + s;
-  if constexpr (FULL) {
-    constexpr int RUN = 16 / sizeof(Elem<TYPE>) < NL ? 16 / sizeof(Elem<TYPE>) : NL;
-#pragma unroll
-    for (int k = 0; k < NL; k += RUN) get<RUN>(r + k, v + k);
-  } else {
-#pragma unroll
-    for (int k = 0; k < NL; ++k) {
-      v[k] = 0.f;
-      if (s + k < n) get<1>(r + k, v + k);
+// A lane's states: the NL from `s` on, of which the first `skip` are another lane's and
+// count as zeros here.  Where n is no multiple of NL, the last lane's run ends with the
+// last state, so that every lane reads a whole run, and none behind its row.
+template <int NL, bool FULL>
+struct Share {
+  int s, skip;
+  __device__ __forceinline__ Share(int q, int n) : s(q * NL), skip(0) {
+    if constexpr (!FULL) {
+      s = q * NL < n - NL ? q * NL : n - NL;
+      skip = q * NL - s;
     }
   }
+  __device__ __forceinline__ bool has(int k) const { return FULL || k >= skip; }
+  __device__ __forceinline__ void mask(float (&v)[NL]) const {
+    if constexpr (!FULL)
+#pragma unroll
+      for (int k = 0; k < NL; ++k) v[k] = has(k) ? v[k] : 0.f;
+  }
+};
+
+// Those of the numbers that begin at p + i.
+template <int TYPE, int NL, bool FULL>
+__device__ __forceinline__ void load_n(const void* p, int64_t i, const Share<NL, FULL>& own, float (&v)[NL]) {
+  const Elem<TYPE>* r = (const Elem<TYPE>*)p + i;
+  constexpr int RUN = 16 / sizeof(Elem<TYPE>) < NL ? 16 / sizeof(Elem<TYPE>) : NL;
+#pragma unroll
+  for (int k = 0; k < NL; k += RUN) get<RUN>(r + k, v + k);
+  own.mask(v);
 }
 
 // Where a lane's groups and columns lie: the wave's first ones (the same for all of
@@ -109,15 +122,15 @@ struct Spot {
 };
 
 template <int NL, bool FULL>
-__device__ __forceinline__ void store_n(float* p, int64_t i, int s, int n, const float (&v)[NL]) {
-  float* r = p + i + s;
+__device__ __forceinline__ void store_n(float* p, int64_t i, const Share<NL, FULL>& own, const float (&v)[NL]) {
+  float* r = p + i;
   if constexpr (FULL) {
 #pragma unroll
     for (int k = 0; k < NL; k += NL < 4 ? NL : 4) put<(NL < 4 ? NL : 4)>(r + k, v + k);
   } else {
 #pragma unroll
     for (int k = 0; k < NL; ++k)
-      if (s + k < n) r[k] = v[k];
+      if (own.has(k)) r[k] = v[k];
   }
 }
 

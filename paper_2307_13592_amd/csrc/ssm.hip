@@ -26,10 +26,10 @@ constexpr int NT = 256;
 enum Pass { WHOLE_AXIS, MANY_ROWS, LOCAL_ENDS, FROM_STATES, ONE_STEP };
 
 // What some steps bring, as it lies in memory.
-template <int TYPE, int NL, bool FULL, int STEPS>
+template <int TYPE, int NL, int STEPS>
 struct Inputs {
   Word<TYPE> x[STEPS], dt[STEPS], z[STEPS];
-  Raw<TYPE, NL, FULL> B[STEPS], C[STEPS];
+  Raw<TYPE, NL, true> B[STEPS], C[STEPS];
 };
 
 template <int TYPE, int NL, bool FULL, int PASS>
@@ -39,11 +39,12 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   // 600 steps of 1,885 x 64, two waves a SIMD in any case, 418 and 411.
   constexpr int STEPS = PASS == ONE_STEP || NL == 16 ? 1 : NL == 8 || (NL == 4 && PASS == MANY_ROWS) ? 2 : 4;
   using E = Elem<TYPE>;
-  using In = Inputs<TYPE, NL, FULL, STEPS>;
+  using In = Inputs<TYPE, NL, STEPS>;
   constexpr int SIZE = sizeof(E);
-  const int q = threadIdx.x & 3, s = q * NL, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int q = threadIdx.x & 3, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t group = a.group0 + ((int64_t)blockIdx.x * (NT / 64) + wave) * 16;
   const Spot p(a, group, q);
+  const Share<NL, FULL> own(q, a.n);
   if (p.row0 >= a.rows) return;
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   const char *px = (const char*)a.x + x0, *pd = (const char*)a.dt + x0, *pz = (const char*)(a.z ? a.z : a.x) + x0;
   const char *pB = (const char*)a.B + n0, *pC = (const char*)a.C + n0;
   char* py = (char*)a.y + x0;
-  const uint32_t o = p.o * SIZE, ob = p.ob * SIZE;
+  const uint32_t o = p.o * SIZE, ob = (p.ob + own.s) * SIZE;
   const auto load = [&](In& v, int64_t left) {
     const int n = left < STEPS ? left < 1 ? 1 : (int)left : STEPS;
     int64_t xo = 0, no = 0;
@@ -66,8 +67,8 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
       v.x[e] = raw1<TYPE>(px + xo, o);
       v.dt[e] = raw1<TYPE>(pd + xo, o);
       if constexpr (PASS != LOCAL_ENDS) v.z[e] = raw1<TYPE>(pz + xo, o);
-      v.B[e].load(pB + no, ob, s, a.n);
-      if constexpr (PASS != LOCAL_ENDS) v.C[e].load(pC + no, ob, s, a.n);
+      v.B[e].load(pB + no, ob);
+      if constexpr (PASS != LOCAL_ENDS) v.C[e].load(pC + no, ob);
       if (e + 1 < n) xo += cb, no += rb;
     }
     if (left > STEPS) px += STEPS * cb, pd += STEPS * cb, pz += STEPS * cb, pB += STEPS * rb, pC += STEPS * rb;
@@ -82,8 +83,8 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) h[j][k] = A[j][k] = 0.f;
     if (p.in && p.g + j < a.cols) {
-      load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(p.g + j) * a.n, s, a.n, A[j]);
-      if (from) load_n<MGN_FP32, NL, FULL>(from + p.at0, p.oa + j * a.n, s, a.n, h[j]);
+      load_n<MGN_FP32>(a.A, (int64_t)(p.g + j) * a.n + own.s, own, A[j]);
+      if (from) load_n<MGN_FP32>(from + p.at0, p.oa + j * a.n + own.s, own, h[j]);
     }
   }
   const float bias = a.bias && p.ok ? a.bias[p.col] : 0.f, D = a.D && p.ok ? a.D[p.col] : 0.f;
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (p.in && p.g + j < a.cols)
-          store_n<NL, FULL>(a.marks + (t / MGN_MARK_STEPS * C * a.n + p.at0), p.oa + j * a.n, s, a.n, h[j]);
+          store_n(a.marks + (t / MGN_MARK_STEPS * C * a.n + p.at0), p.oa + j * a.n + own.s, own, h[j]);
     // what is done once a column
     float x[STEPS], delta[STEPS], y[STEPS], f[STEPS];
     bool held = false;
@@ -134,8 +135,9 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
       float d[4], w[4], r[4], B[NL], Cn[NL];
       quads(delta[e], d);
       quads(some_held() ? mul_or_0(delta[e], x[e]) : delta[e] * x[e], w);
-      v.B[e].get(s, a.n, B);
-      if constexpr (PASS != LOCAL_ENDS) v.C[e].get(s, a.n, Cn);
+      v.B[e].get(B);
+      own.mask(B);
+      if constexpr (PASS != LOCAL_ENDS) v.C[e].get(Cn), own.mask(Cn);
       else sum += delta[e];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   if (to)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (p.in && p.g + j < a.cols) store_n<NL, FULL>(to + p.at0, p.oa + j * a.n, s, a.n, h[j]);
+      if (p.in && p.g + j < a.cols) store_n(to + p.at0, p.oa + j * a.n + own.s, own, h[j]);
   if (PASS == LOCAL_ENDS && p.ok) a.sums[c * C + p.i0 + p.o] = sum;
 }
 

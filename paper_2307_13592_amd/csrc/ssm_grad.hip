@@ -95,7 +95,8 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
   constexpr int STEPS = NL <= 4 ? 4 : NL == 8 ? 2 : 1;
   const int per_row = (a.cols + 3) / 4, q = threadIdx.x & 3;
   const int64_t gi = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 4, row = gi / per_row;
-  const int g = (int)(gi - row * per_row) * 4, col = g + q, s = q * NL;
+  const int g = (int)(gi - row * per_row) * 4, col = g + q;
+  const Share<NL, FULL> own(q, a.n);
   const bool in = row < a.rows, ok = in && col < a.cols;
   const int c = blockIdx.y + 1;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) G[j][k] = A[j][k] = 0.f;
-    if (in && g + j < a.cols) load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(g + j) * a.n, s, a.n, A[j]);
+    if (in && g + j < a.cols) load_n<MGN_FP32>(a.A, (int64_t)(g + j) * a.n + own.s, own, A[j]);
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   }
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
         o[e] = load1<TYPE>(a.dy, (t - e) * C + i);
         if (GATE) z[e] = load1<TYPE>(a.z, (t - e) * C + i);
       }
-      if (in) load_n<TYPE, NL, FULL>(a.C, (t - e) * a.rows * a.n + bn, s, a.n, Cn[e]);
+      if (in) load_n<TYPE>(a.C, (t - e) * a.rows * a.n + bn + own.s, own, Cn[e]);
     }
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (in && g + j < a.cols) store_n<NL, FULL>(a.state + c * C * a.n, at + j * a.n, s, a.n, G[j]);
+    if (in && g + j < a.cols) store_n(a.state + c * C * a.n, at + j * a.n + own.s, own, G[j]);
   if (ok) a.sums[c * C + i] = sum;
 }
 
@@ -178,7 +179,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   const int lane = threadIdx.x & 63, w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane & 3;
   const int tile = blockIdx.x % a.tiles, sub = (lane >> 2) >> LG;
   const int64_t slot = blockIdx.x / a.tiles;
-  const int g = (tile * GP + ((lane >> 2) & (GP - 1))) * 4, col = g + q, s0 = (w * 4 + q) * NL;
+  const int g = (tile * GP + ((lane >> 2) & (GP - 1))) * 4, col = g + q;
+  const Share<NL, FULL> own(w * 4 + q, a.n);
   const int c = blockIdx.y;
   const int64_t ts = c * a.chunk, te = ts + a.chunk < a.steps ? ts + a.chunk : a.steps;
   const int64_t C = a.rows * a.cols, cb = C * SIZE, rb = a.rows * a.n * SIZE;  // a step's bytes
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   for (int j = 0; j < 4; ++j) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] = 0.f, accs[j * NL + k][threadIdx.x] = 0;
-    if (g + j < a.cols) load_n<MGN_FP32, NL, FULL>(a.A, (int64_t)(g + j) * a.n, s0, a.n, A[j]);
+    if (g + j < a.cols) load_n<MGN_FP32>(a.A, (int64_t)(g + j) * a.n + own.s, own, A[j]);
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   }
@@ -203,18 +205,18 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
   // What a unit's steps bring, as it lies in memory.
   struct In {
     Word<TYPE> x[U], dt[U], o[U], z[U];
-    Raw<TYPE, NL, FULL> B[U], C[U];
+    Raw<TYPE, NL, true> B[U], C[U];
   };
   struct Sweep {
     Word<TYPE> x[U], dt[U];
-    Raw<TYPE, NL, FULL> B[U];
+    Raw<TYPE, NL, true> B[U];
   };
 
   for (int64_t r0 = slot * RPW; r0 < a.rows; r0 += a.slots * RPW) {
     const bool row_in = r0 + sub < a.rows, in = row_in && g < a.cols, ok = in && col < a.cols;
     // the lane's column, states and n numbers from the wave's first row's on
     // (lanes without one read that row's first)
-    const uint32_t o = ok ? (uint32_t)(sub * a.cols + col) * SIZE : 0, ob = row_in ? (uint32_t)(sub * a.n) * SIZE : 0;
+    const uint32_t o = ok ? (uint32_t)(sub * a.cols + col) * SIZE : 0, ob = ((row_in ? (uint32_t)(sub * a.n) : 0) + own.s) * SIZE;
     const uint32_t oh = in ? (uint32_t)((sub * a.cols + g) * a.n) : 0;
     float G[4][NL], h[U + 1][4][NL];
     const auto load_states = [&](const float* from, float (&v)[4][NL]) {
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
         for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
         if (from && in && g + j < a.cols)
-          load_n<MGN_FP32, NL, FULL>(from + r0 * a.cols * a.n, here(oh + j * a.n + s0), 0, a.n - s0, v[j]);
+          load_n<MGN_FP32>(from + r0 * a.cols * a.n, here(oh + j * a.n + own.s), own, v[j]);
       }
     };
     load_states(a.chunks > 1 ? a.state + c * C * a.n : a.dh_last, G);
@@ -249,8 +251,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           r.dt[e] = raw1<TYPE>((const char*)a.dt + i, o);
           r.o[e] = raw1<TYPE>((const char*)a.dy + i, o);
           if (GATE) r.z[e] = raw1<TYPE>((const char*)a.z + i, o);
-          r.B[e].load((const char*)a.B + b, ob, s0, a.n);
-          r.C[e].load((const char*)a.C + b, ob, s0, a.n);
+          r.B[e].load((const char*)a.B + b, ob);
+          r.C[e].load((const char*)a.C + b, ob);
         }
       };
       const auto load_sweep = [&](int v, Sweep& r) {
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           const int at = v * U + e < n ? e : 0;
           r.x[e] = raw1<TYPE>((const char*)a.x + (xu + at * cb), o);
           r.dt[e] = raw1<TYPE>((const char*)a.dt + (xu + at * cb), o);
-          r.B[e].load((const char*)a.B + (nu + at * rb), ob, s0, a.n);
+          r.B[e].load((const char*)a.B + (nu + at * rb), ob);
         }
       };
       const uint32_t begins =
@@ -292,7 +294,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         }
         const auto step = [&](int e, auto slow) {
           float d[4], u[4], B[NL];
-          now.B[e].get(s0, a.n, B);
+          now.B[e].get(B);
+          own.mask(B);
           quads(delta[e], d);
           quads(slow() ? mul_or_0(delta[e], value1<TYPE>(now.x[e])) : delta[e] * value1<TYPE>(now.x[e]), u);
 #pragma unroll
@@ -347,7 +350,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(r.x[e])); };
         const auto forth = [&](int e, auto first, auto some_held) {
           float d[4], u[4], B[NL];
-          r.B[e].get(s0, a.n, B);
+          r.B[e].get(B);
+          own.mask(B);
           quads(delta[e], d);
           quads(input(e), u);
 #pragma unroll
@@ -367,8 +371,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         };
         const auto back = [&](int e) {
           float B[NL], Cn[NL], d[4], u[4], ot[4], sB[4], sA[4], y[4];
-          r.B[e].get(s0, a.n, B);
-          r.C[e].get(s0, a.n, Cn);
+          r.B[e].get(B);
+          own.mask(B);
+          r.C[e].get(Cn);
+          own.mask(Cn);
           quads(delta[e], d);
           quads(input(e), u);
           quads(ov[e], ot);
@@ -425,14 +431,14 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         if (row_in && where.keeps)
 #pragma unroll
           for (int k = 0; k < Sums::LEFT; ++k) {
-            const int x = where.first + k, st = s0 + (x < NL ? x : x - NL);
-            if (!FULL && st >= a.n) continue;
+            const int x = where.first + k, st = x < NL ? x : x - NL;
+            if (!own.has(st)) continue;
 #pragma unroll
             for (int e = 0; e < U; ++e) {
               if (e >= m) continue;
               if (a.tiles > 1)
                 write1<MGN_FP32>((char*)a.bc + ((tile * a.steps + tu + e) * a.rows + r0) * 2 * a.n * 4,
-                                 (uint32_t)(sub * 2 * a.n + (x < NL ? 0 : a.n) + st) * 4, p[e][k]);
+                                 (uint32_t)(sub * 2 * a.n + (x < NL ? 0 : a.n) + own.s + st) * 4, p[e][k]);
               else if (x < NL)
                 write1<TYPE>((char*)a.dB + (nu + e * rb), ob + (uint32_t)(st * SIZE), p[e][k]);
               else
@@ -493,7 +499,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
     if (ts == 0 && a.dh0)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (in && g + j < a.cols) store_n<NL, FULL>(a.dh0 + r0 * a.cols * a.n, oh + j * a.n, s0, a.n, G[j]);
+        if (in && g + j < a.cols) store_n(a.dh0 + r0 * a.cols * a.n, oh + j * a.n + own.s, own, G[j]);
   }
   if (!a.part) return;
   const int64_t width = (int64_t)a.cols * (a.n + 2);
@@ -509,7 +515,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) {
       const double v = rows(accs[j * NL + k][threadIdx.x]);
-      if (sub == 0 && g + j < a.cols && s0 + k < a.n) dst[(int64_t)(g + j) * a.n + s0 + k] = (float)v;
+      if (sub == 0 && g + j < a.cols && own.has(k)) dst[(int64_t)(g + j) * a.n + own.s + k] = (float)v;
     }
   if constexpr (NW > 1) {  // the waves' steps
     double* const t = &accs[0][0];
