@@ -584,6 +584,7 @@ hipError_t by_states(int n, F f) {
   const std::false_type part;
   const std::true_type whole;
   if (n <= 4) return f(Int<1>(), Int<1>(), part);
+  if (n <= 8) return f(Int<2>(), Int<1>(), part);
   if (n == 16) return f(Int<4>(), Int<1>(), whole);
   if (n <= 16) return f(Int<4>(), Int<1>(), part);
   if (n == 32) return f(Int<4>(), Int<2>(), whole);
