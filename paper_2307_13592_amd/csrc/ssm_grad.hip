@@ -16,7 +16,8 @@
 // rows, leave one partial each of it; a block's products are added in fp32, the blocks
 // in fp64.  With few columns the time axis is cut into chunks as in the forward.
 //
-// Bound by the vector units: 13 instructions and two exponentials a state and step.  20
+// Bound by the vector units: 15 instructions and two exponentials a state and step (the
+// states before a unit are formed first, then its own again).  20
 // steps of 20,011 x 64 bf16, 16 states, 490 us, the units busy 77 % of them with the two
 // waves a SIMD that 256 registers leave; 570 without a unit's loads ahead.  A unit of 4
 // steps spills (1.3 ms and more).
