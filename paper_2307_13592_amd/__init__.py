@@ -667,6 +667,14 @@ def mgn_causal_conv_grad(x, weight, dy, dx, dweight=None, dbias=None, bias=None,
     overwritten or added to) and d_past (float32), each of them or None.  work:
     float32 scratch of MGN_CONV_PARTS * cols * (width + 1) for dweight and dbias
     (None: allocated)."""
+    _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_past_out, starts, silu, accumulate, work,
+                      stream)()
+
+
+def _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_past_out, starts, silu, accumulate, work,
+                      stream):
+    """The binding's checks of mgn_causal_conv_grad now, its launch when the result is
+    called: so that of several calls none runs if one would be refused."""
     import torch
     shape, dev, width, before, head = _conv_args(x, weight, bias, past, starts)
     T, rows, cols = shape
@@ -675,10 +683,11 @@ def mgn_causal_conv_grad(x, weight, dy, dx, dweight=None, dbias=None, bias=None,
     if work is not None:
         _devt(work, f32, "work", min_numel=floats)
     pw, _, keep = _given(work, "work", 4 * floats if sums else 0, dev, stream)
-    _run("mgn_causal_conv_grad", dev, stream, *head, _need(_arr(dy, "dy", x.dtype, shape, dev), "dy"),
-         _arr(d_past_out, "d_past_out", f32, before, dev), T, rows, cols, 1 if silu else 0,
-         _need(_arr(dx, "dx", x.dtype, shape, dev), "dx"), _arr(dweight, "dweight", f32, (cols, width), dev),
-         _arr(dbias, "dbias", f32, (cols,), dev), 1 if accumulate else 0, _arr(d_past, "d_past", f32, before, dev), pw)
+    args = (*head, _need(_arr(dy, "dy", x.dtype, shape, dev), "dy"), _arr(d_past_out, "d_past_out", f32, before, dev), T,
+            rows, cols, 1 if silu else 0, _need(_arr(dx, "dx", x.dtype, shape, dev), "dx"),
+            _arr(dweight, "dweight", f32, (cols, width), dev), _arr(dbias, "dbias", f32, (cols,), dev),
+            1 if accumulate else 0, _arr(d_past, "d_past", f32, before, dev), pw)
+    return lambda _=keep: _run("mgn_causal_conv_grad", dev, stream, *args)
 
 
 @functools.lru_cache(maxsize=256)
@@ -732,14 +741,20 @@ def mgn_selective_scan(x, dt, A, B, C, y, D=None, dt_bias=None, z=None, h0=None,
     float32 [rows][cols][n] or None; marks of mgn_selective_marks, for the backward;
     starts: uint8 [steps].  work: device scratch of mgn_selective_scan_work bytes
     (None: allocated)."""
+    _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts, softplus, work, stream)()
+
+
+def _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts, softplus, work, stream):
+    """mgn_selective_scan as _causal_conv_grad."""
     import torch
     shape, dev, n, s = _ssm_args(x, dt, A, B, C, D, dt_bias, z, starts, softplus)
     T, rows, cols = shape
     f32, state = torch.float32, (rows, cols, n)
     pw, nb, keep = _given(work, "work", mgn_selective_scan_work(T, rows, cols, n) if work is None else 0, dev, stream)
-    _run("mgn_selective_scan", dev, stream, _byref(s), _arr(h0, "h0", f32, state, dev),
-         _need(_arr(y, "y", x.dtype, shape, dev), "y"), _arr(h_last, "h_last", f32, state, dev),
-         _arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), pw, nb)
+    args = (_byref(s), _arr(h0, "h0", f32, state, dev), _need(_arr(y, "y", x.dtype, shape, dev), "y"),
+            _arr(h_last, "h_last", f32, state, dev), _arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev),
+            pw, nb)
+    return lambda _=keep: _run("mgn_selective_scan", dev, stream, *args)
 
 
 def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=None, d_bias=None, dz=None, D=None,
@@ -750,6 +765,13 @@ def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=N
     dA, dD, d_bias (float32, overwritten or added to, each of them or None); dh0
     (float32, or None; it may be dh_last).  work: device scratch of
     mgn_selective_scan_grad_work bytes (None: allocated)."""
+    _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_bias, dz, D, dt_bias, z, dh_last, dh0,
+                         starts, softplus, accumulate, work, stream)()
+
+
+def _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_bias, dz, D, dt_bias, z, dh_last, dh0,
+                         starts, softplus, accumulate, work, stream):
+    """mgn_selective_scan_grad as _causal_conv_grad."""
     import torch
     shape, dev, n, s = _ssm_args(x, dt, A, B, C, D, dt_bias, z, starts, softplus)
     T, rows, cols = shape
@@ -761,10 +783,22 @@ def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=N
                       1 if accumulate else 0)
     pw, nb, keep = _given(work, "work", mgn_selective_scan_grad_work(T, rows, cols, n) if work is None else 0, dev,
                           stream)
-    _run("mgn_selective_scan_grad", dev, stream, _byref(s),
-         _need(_arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), "marks"),
-         _need(_arr(dy, "dy", ty, shape, dev), "dy"), _arr(dh_last, "dh_last", f32, state, dev), _byref(g),
-         _arr(dh0, "dh0", f32, state, dev), pw, nb)
+    args = (_byref(s), _need(_arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), "marks"),
+            _need(_arr(dy, "dy", ty, shape, dev), "dy"), _arr(dh_last, "dh_last", f32, state, dev), _byref(g),
+            _arr(dh0, "dh0", f32, state, dev), pw, nb)
+    return lambda _=keep: _run("mgn_selective_scan_grad", dev, stream, *args)
+
+
+def _apart(fn: str, read, written) -> None:
+    """Refuses two calls in a row of which the second would read, in the tensors `read`
+    (None: not there), what is written by either in the tensors `written`."""
+    spans = [(p, p + t.nbytes) for t in written if (p := t.data_ptr())]
+    for t in read:
+        if t is not None and (p := t.data_ptr()):
+            q = p + t.nbytes
+            for b, e in spans:
+                if p < e and b < q:
+                    raise MgnError(MGN_E_ARG, f"{fn}: overlapping arrays")
 
 
 class mgn_grad_list:

@@ -11,8 +11,8 @@ from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_d
                mgn_norm_accumulate, mgn_norm_apply, MGN_NORM_WORK_PER_COL, mgn_rollout_update, mgn_set_h1_stash,
                mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
                mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on, mgn_causal_conv,
-               mgn_causal_conv_grad, mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad,
-               mgn_selective_marks, mgn_selective_scan, mgn_selective_scan_grad)
+               mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad, mgn_selective_marks, _apart,
+               _causal_conv_grad, _selective_scan, _selective_scan_grad)
 
 
 class Session:
@@ -357,7 +357,8 @@ class SelectiveMemory:
     the states along a rollout (Session.rollout(memory=...)); scan() and grad() run
     whole trajectories.  The parameters are float32: conv_weight [cols][width],
     conv_bias, A [cols][states] (negative), D, dt_bias (the step size is the softplus of
-    dt + dt_bias); their gradients lie in `grads`, by the same names."""
+    dt + dt_bias); their gradients lie in `grads`, by the same names.  A call that is
+    refused changes nothing."""
 
     def __init__(self, rows: int, cols: int, states: int = 16, width: int = 4, dtype=torch.float32, device: str = "cuda",
                  dt=None, B=None, C=None):
@@ -379,9 +380,7 @@ class SelectiveMemory:
         if dt is None or B is None or C is None:
             raise ValueError("dt, B, C: not given")
         u, y = self._out[0], self._out[1]
-        mgn_causal_conv(x[None], self.conv_weight, u, self.conv_bias, self.past, self.past, None, True, stream)
-        mgn_selective_scan(u, dt[None], self.A, B[None], C[None], y, self.D, self.dt_bias, None if z is None else z[None],
-                           self.state, self.state, None, None, True, None, stream)
+        self._run(x[None], u, dt[None], B[None], C[None], y, None if z is None else z[None], None, None, stream)
         return y[0]
 
     def scan(self, x, dt, B, C, z=None, starts=None, stream=None):
@@ -390,10 +389,17 @@ class SelectiveMemory:
         with _on(stream, x.device):
             u, y, past = torch.empty_like(x), torch.empty_like(x), self.past.clone()
         marks = mgn_selective_marks(x, self.A, stream)
-        mgn_causal_conv(x, self.conv_weight, u, self.conv_bias, self.past, self.past, starts, True, stream)
-        mgn_selective_scan(u, dt, self.A, B, C, y, self.D, self.dt_bias, z, self.state, self.state, marks, starts, True,
-                           None, stream)
+        self._run(x, u, dt, B, C, y, z, marks, starts, stream)
         return y, (past, u, marks)
+
+    def _run(self, x, u, dt, B, C, y, z, marks, starts, stream):
+        """The convolution into u and the scan into y.  The convolution moves `past`
+        on, so the scan's arguments are checked before it."""
+        scan = _selective_scan(u, dt, self.A, B, C, y, self.D, self.dt_bias, z, self.state, self.state, marks, starts,
+                               True, None, stream)
+        _apart("mgn_selective_scan", (dt, B, C, z, starts), (self.past, y, self.state))
+        mgn_causal_conv(x, self.conv_weight, u, self.conv_bias, self.past, self.past, starts, True, stream)
+        scan()
 
     def grad(self, x, dt, B, C, kept, dy, z=None, starts=None, dh_last=None, d_past=None, accumulate: bool = False,
              stream=None):
@@ -407,8 +413,12 @@ class SelectiveMemory:
             dh0 = torch.empty_like(self.state)
             d_before = torch.empty(past.shape, dtype=torch.float32, device=x.device)
         p, g = self, self.grads
-        mgn_selective_scan_grad(u, dt, p.A, B, C, marks, dy, du, ddt, g["A"], dB, dC, g["D"], g["dt_bias"], dz, p.D,
-                                p.dt_bias, z, dh_last, dh0, starts, True, accumulate, None, stream)
-        mgn_causal_conv_grad(x, p.conv_weight, du, dx, g["conv_weight"], g["conv_bias"], p.conv_bias, past, d_before,
-                             d_past, starts, True, accumulate, None, stream)
+        # (the scan's part of the gradients is not added before the convolution's arguments are checked)
+        scan = _selective_scan_grad(u, dt, p.A, B, C, marks, dy, du, ddt, g["A"], dB, dC, g["D"], g["dt_bias"], dz, p.D,
+                                    p.dt_bias, z, dh_last, dh0, starts, True, accumulate, None, stream)
+        conv = _causal_conv_grad(x, p.conv_weight, du, dx, g["conv_weight"], g["conv_bias"], p.conv_bias, past, d_before,
+                                 d_past, starts, True, accumulate, None, stream)
+        _apart("mgn_causal_conv_grad", (x, starts, d_past), g.values())
+        scan()
+        conv()
         return dict(dx=dx, ddt=ddt, dB=dB, dC=dC, dz=dz, dh0=dh0, d_past=d_before)
