@@ -449,8 +449,9 @@ mgn_status mgn_grads_work(const mgn_grads* list, size_t* bytes);
 mgn_status mgn_grad_norm(const mgn_grads* list, float* norm, void* work, size_t work_bytes, mgn_stream stream);
 /* Scales to max_norm (positive and finite).  given == 0: norm[0] takes the tensors'
  * own norm; else it is read: that of all the parts of a job, say.  A norm that is NaN
- * or infinite scales nothing.  Tensors that are not scaled are copied to their
- * out. */
+ * or infinite scales nothing, and one of finite values that passes the fp32 range is
+ * infinite there: what comes next should look at norm[0].  Tensors that are not scaled
+ * are copied to their out. */
 mgn_status mgn_grad_clip(const mgn_grads* list, float max_norm, int32_t given, float* norm, void* work,
                          size_t work_bytes, mgn_stream stream);
 

@@ -858,7 +858,7 @@ def mgn_grad_norm(grads, norm, work=None, stream=None) -> None:
 def mgn_grad_clip(grads, max_norm: float, norm, given: bool = False, work=None, stream=None) -> None:
     """Scales grads (an mgn_grad_list, into its outs; or a sequence of tensors, in
     place) by min(1, max_norm / norm); norm (float32 [1], device) takes the tensors'
-    own or, given, is read."""
+    own or, given, is read.  A norm that is not finite (in float32) scales nothing."""
     dev, p, pn, tail, keep = _grads(grads, norm, work, stream)
     _run("mgn_grad_clip", dev, stream, p, float(max_norm), 1 if given else 0, pn, *tail)
 

@@ -130,19 +130,22 @@ __global__ __launch_bounds__(NT) void grad_norm_kernel(double* part, int64_t par
   else part[0] = s;
 }
 
-// out = g scale.  A norm that is not a number, or infinite, scales nothing.
+// out = g scale rest.  A norm that is not a number, or infinite in fp32 as it is stored,
+// scales nothing.  The quotient goes in one fp32 number, or, below the normal ones (which
+// would leave it few digits or none), 2^126 times it and the exact rest.
 __global__ __launch_bounds__(NT) void grad_clip_kernel(GradTable t, const double* part, int64_t parts, float max_norm,
                                                        bool given, bool write, float* norm) {
   __shared__ double lds[NT / 64];
   const float n = given ? *norm : (float)sqrt(all_squares(part, parts, lds));
   if (write && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
-  const float scale = n > max_norm && n < INFINITY ? max_norm / n : 1.f;
+  float scale = n > max_norm && n < INFINITY ? max_norm / n : 1.f, rest = 1.f;
+  if (scale < 0x1p-126f) scale = (float)((double)max_norm / (double)n * 0x1p126), rest = 0x1p-126f;
   const Lookup tensor(t);
   const uint32_t tiles = t.first[t.count];
   for (uint32_t b = blockIdx.x; b < tiles; b += gridDim.x) {
     const uint32_t tile = tiles - 1 - b;
     const int k = tensor(tile);
-    if (scale == 1.f && t.out(k) == t.g(k)) continue;
+    if (scale == 1.f && rest == 1.f && t.out(k) == t.g(k)) continue;
     const int64_t n = t.n(k), at = (int64_t)(tile - t.first[k]) * GRAD_TILE, to = at + GRAD_TILE;
     const auto scaled = [&](auto* p) {
       using E = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(NT) void grad_clip_kernel(GradTable t, const double
 #pragma unroll
         for (int r = 0; r < runs(); ++r) {
 #pragma unroll
-          for (int e = 0; e < count(); ++e) v[r][e] *= scale;
+          for (int e = 0; e < count(); ++e) v[r][e] = v[r][e] * scale * rest;
           put<count()>(out + i + r * (int64_t)NT * count(), v[r]);
         }
       });

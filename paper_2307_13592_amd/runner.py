@@ -101,8 +101,9 @@ class Session:
 
     def sgd(self, lr: float, grad=None, stream=None, max_norm=None):
         """Parameter update with the last backward's gradient (or `grad`); max_norm:
-        that is first scaled, in place, to at most this norm.  Returns the norm that
-        it had (float32 [1] on the device; None without max_norm)."""
+        that is first scaled, in place, to at most this norm (not where its norm is
+        not finite in float32).  Returns the norm that it had (float32 [1] on the
+        device; None without max_norm)."""
         grad = self.d_params if grad is None else grad
         if grad.numel() != self.n_params:
             raise ValueError("gradient vector has the wrong length")
@@ -295,7 +296,7 @@ class LayerNorm:
 def clip_grads(grads, max_norm: float, stream=None):
     """Scales gradients (tensors, or an mgn_grad_list of them) to at most max_norm
     together, in place (into the list's outs); returns the norm that they had, a
-    float32 [1] on their device."""
+    float32 [1] on their device.  A norm that is not finite there scales nothing."""
     grads = grads if isinstance(grads, mgn_grad_list) else mgn_grad_list(grads)
     device = grads.tensors[0][0].device if grads.tensors[0] else "cuda"
     with _on(stream, device):
