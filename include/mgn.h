@@ -385,7 +385,7 @@ mgn_status mgn_causal_conv_grad(const void* x, int32_t type, const float* weight
  * (softplus of -infinity, say) leaves the states as they were whatever x and B hold;
  * a state that is NaN or infinite stays one of them until a start.  States may grow
  * (delta A > 0), but a nonzero one only so far that exp(A sum of delta) over the steps
- * of a call stays within the fp32 range. */
+ * of a call stays within the fp32 range; zero states stay zero through any growth. */
 #define MGN_STATES_MAX 64
 #define MGN_MARK_STEPS 8
 typedef struct {
@@ -413,7 +413,9 @@ mgn_status mgn_selective_scan(const mgn_ssm* s, const float* h0, void* y, float*
  * to when accumulate != 0; dh0 (NULL: not wanted; it may be dh_last) = dL/dh0.
  * A step of size 0 gives x and B no gradient, nor dt where its softplus is level; with
  * dy = 0 there too, no gradient takes anything from what x and B hold (C and z are
- * finite). */
+ * finite).  A nonzero gradient grows on its way back only so far as a state may; a step
+ * whose own factor exp(delta A) passes the fp32 range (of zero states, by the above)
+ * passes none on to the states before it. */
 typedef struct {
   void *dx, *ddt, *dB, *dC, *dz;
   float *dA, *dD, *d_bias;

@@ -22,6 +22,17 @@ __device__ __forceinline__ float mul_or_0(float a, float b) { return a == 0.f ? 
 // Whether any lane of the wave says so.
 __device__ __forceinline__ bool any(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
 
+// How a wave takes a step: as it comes; or where a column's step has size 0, at which x
+// and B may hold anything, or a factor may pass the fp32 range (100 steps of 4,000 x 64
+// bf16, 16 states: 132 us; with sizes of 0 in three tenths of the rows' steps 170).
+enum Way { PLAIN, CAREFUL };
+
+// The state f h + b.  Zero states stay zero whatever f is.
+__device__ __forceinline__ float carried(float f, float h, float b) { return h == 0.f ? b : fmaf(f, h, b); }
+// A factor on the way back.  Past the fp32 range it is one of a zero state and passes no
+// gradient on.
+__device__ __forceinline__ float passed(float f) { return f == INFINITY ? 0.f : f; }
+
 // log(1 + e^v), to a few half-steps of itself at any v: with e = e^-|v| the
 // logarithm of 1 + e is 2 atanh(s), s = e / (2 + e), an odd series in s <= 1 / 3
 // (five terms, fitted in s^2 to 5e-9 of the sum).
@@ -42,6 +53,20 @@ __device__ __forceinline__ float quad(float v) {
 }
 __device__ __forceinline__ void quads(float v, float (&u)[4]) {
   u[0] = quad<0>(v), u[1] = quad<1>(v), u[2] = quad<2>(v), u[3] = quad<3>(v);
+}
+// The largest rate of growth among the wave's states (A: times log2(e)), at least 0: a
+// factor passes the range at a step of more than 128 / rate, or of less than 0.
+template <int NL>
+__device__ __forceinline__ float growth(const float (&A)[4][NL]) {
+  float most = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int k = 0; k < NL; ++k) most = fmaxf(most, A[j][k]);
+  if (!any(most > 0.f)) return 0.f;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(most)));
 }
 // Sum over the four lanes of v[q], in lane q.
 __device__ __forceinline__ float quad_sums(const float (&v)[4]) {

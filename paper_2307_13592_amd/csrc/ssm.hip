@@ -92,6 +92,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
+  const float rate = growth(A);
   float sum = 0.f;
   Starts starts(a.starts, ts, te);
 
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
           store_n(a.marks + (t / MGN_MARK_STEPS * C * a.n + p.at0), p.oa + j * a.n + own.s, own, h[j]);
     // what is done once a column
     float x[STEPS], delta[STEPS], y[STEPS], f[STEPS];
-    bool held = false;
+    bool careful = false;
     const uint32_t fresh = starts.at<STEPS>(t);
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
@@ -117,9 +118,12 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
       for (int e = 0; e < STEPS; ++e) delta[e] = softplus(delta[e]);
 #pragma unroll
     for (int e = 0; e < STEPS; ++e) {
-      held = held || (p.ok && delta[e] == 0.f);
+      careful = careful || (p.ok && !(delta[e] > 0.f));
       delta[e] = p.ok ? delta[e] : 0.f;
     }
+    if (__float_as_int(rate) > 0)
+#pragma unroll
+      for (int e = 0; e < STEPS; ++e) careful = careful || delta[e] * rate > 127.f;
     if constexpr (PASS != LOCAL_ENDS) {
       if (a.D)
 #pragma unroll
@@ -131,10 +135,10 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
           f[e] = z * sigmoid(z);
         }
     }
-    const auto step = [&](int e, auto some_held) {
+    const auto step = [&](int e, auto way) {
       float d[4], w[4], r[4], B[NL], Cn[NL];
       quads(delta[e], d);
-      quads(some_held() ? mul_or_0(delta[e], x[e]) : delta[e] * x[e], w);
+      quads(way() == CAREFUL ? mul_or_0(delta[e], x[e]) : delta[e] * x[e], w);
       v.B[e].get(B);
       own.mask(B);
       if constexpr (PASS != LOCAL_ENDS) v.C[e].get(Cn), own.mask(Cn);
@@ -144,18 +148,18 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
         r[j] = 0.f;
 #pragma unroll
         for (int k = 0; k < NL; ++k) {
-          const float b = some_held() ? mul_or_0(w[j], B[k]) : w[j] * B[k];
-          h[j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), h[j][k], b);
+          const float keep = __builtin_amdgcn_exp2f(d[j] * A[j][k]), b = way() == CAREFUL ? mul_or_0(w[j], B[k]) : w[j] * B[k];
+          h[j][k] = way() == CAREFUL ? carried(keep, h[j][k], b) : fmaf(keep, h[j][k], b);
           if constexpr (PASS != LOCAL_ENDS) r[j] = fmaf(Cn[k], h[j][k], r[j]);
         }
       }
       if constexpr (PASS != LOCAL_ENDS) y[e] = (quad_sums(r) + y[e]) * f[e];
     };
-    if (n == STEPS && !fresh && !any(held)) {
+    careful = any(careful);
+    if (n == STEPS && !fresh && !careful) {
 #pragma unroll
-      for (int e = 0; e < STEPS; ++e) step(e, std::false_type());
+      for (int e = 0; e < STEPS; ++e) step(e, Int<PLAIN>());
     } else {
-      // B may hold anything where a column's step has size 0
 #pragma unroll
       for (int e = 0; e < STEPS; ++e) {
         if (e >= n) break;
@@ -166,7 +170,8 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
             for (int k = 0; k < NL; ++k) h[j][k] = 0.f;
           sum = CUT;
         }
-        step(e, std::true_type());
+        if (careful) step(e, Int<CAREFUL>());
+        else step(e, Int<PLAIN>());
       }
     }
     if constexpr (PASS != LOCAL_ENDS) {
@@ -199,9 +204,6 @@ __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
 // (18 of 96,256 states 29 us with 16, of which 14 idle); two latencies for 256 chunks
 // with G = 16.
 constexpr int AHEAD = 16;
-// What leaves chunks that v enters.  Zero states stay zero whatever a chunk's factor is
-// (over many growing steps it passes the fp32 range).
-__device__ __forceinline__ float carried(float f, float v, float own) { return v == 0.f ? own : fmaf(f, v, own); }
 template <int G>
 __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* first, bool reverse) {
   constexpr int STATES = NT / G;
@@ -228,10 +230,11 @@ __global__ __launch_bounds__(NT) void ssm_join_kernel(SsmArgs a, const float* fi
         const bool here = k + e < a.chunks - 1 && f[e] == CUT;
         f[e] = k + e < a.chunks - 1 ? __builtin_amdgcn_exp2f(A * f[e]) : 1.f;
         if (here) f[e] = 0.f;
+        if (reverse) f[e] = passed(f[e]);
         cuts |= (uint32_t)here << e;
         if constexpr (G > 1) {
           q = here ? own[e] : carried(f[e], q, own[e]);
-          p *= f[e];
+          p = mul_or_0(p, f[e]);
         }
       }
       float mine = v;

@@ -111,6 +111,7 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   }
+  const bool growing = !a.softplus || growth(A) > 0.f;
   const float bias = a.bias && ok ? a.bias[col] : 0.f;
   float sum = 0.f;
   for (int64_t t = te - 1; t >= ts; t -= STEPS) {
@@ -131,30 +132,36 @@ __global__ __launch_bounds__(256) void ssm_carry_kernel(SsmArgs a) {
       }
       if (in) load_n<TYPE>(a.C, (t - e) * a.rows * a.n + bn + own.s, own, Cn[e]);
     }
+    const auto back = [&](auto growing) {
 #pragma unroll
-    for (int e = 0; e < STEPS; ++e) {
-      if (t - e < ts) break;
-      float delta = dt[e] + bias;
-      if (a.softplus) delta = softplus(delta);
-      delta = ok ? delta : 0.f;
-      sum += delta;
-      if (GATE) o[e] *= z[e] * sigmoid(z[e]);
-      float d[4], ov[4];
-      quads(delta, d);
-      quads(o[e], ov);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int k = 0; k < NL; ++k)
-          G[j][k] = fmaf(Cn[e][k], ov[j], G[j][k]) * __builtin_amdgcn_exp2f(d[j] * A[j][k]);
-      if (fresh[e]) {
+      for (int e = 0; e < STEPS; ++e) {
+        if (t - e < ts) break;
+        float delta = dt[e] + bias;
+        if (a.softplus) delta = softplus(delta);
+        delta = ok ? delta : 0.f;
+        sum += delta;
+        if (GATE) o[e] *= z[e] * sigmoid(z[e]);
+        float d[4], ov[4];
+        quads(delta, d);
+        quads(o[e], ov);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int k = 0; k < NL; ++k) G[j][k] = 0.f;
-        sum = CUT;
+          for (int k = 0; k < NL; ++k) {
+            const float f = __builtin_amdgcn_exp2f(d[j] * A[j][k]);
+            G[j][k] = fmaf(Cn[e][k], ov[j], G[j][k]) * (growing() ? passed(f) : f);
+          }
+        if (fresh[e]) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < NL; ++k) G[j][k] = 0.f;
+          sum = CUT;
+        }
       }
-    }
+    };
+    if (growing) back(std::true_type());
+    else back(std::false_type());
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -195,6 +202,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
 #pragma unroll
     for (int k = 0; k < NL; ++k) A[j][k] *= LOG2E;
   }
+  const float rate = growth(A);
   const float bias = a.bias && col < a.cols ? a.bias[col] : 0.f, D = a.D && col < a.cols ? a.D[col] : 0.f;
   double dD = 0, d_bias = 0;
   int par = 0;
@@ -228,6 +236,12 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
         if (from && in && g + j < a.cols)
           load_n<MGN_FP32>(from + r0 * a.cols * a.n, here(oh + j * a.n + own.s), own, v[j]);
       }
+    };
+    const auto zero = [](float (&v)[4][NL]) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
     };
     load_states(a.chunks > 1 ? a.state + c * C * a.n : a.dh_last, G);
     // the starts of a block's steps, from the lanes' loads of one; those of the block
@@ -287,31 +301,38 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
             for (int k = 0; k < NL; ++k) subs[v - KEPT][j * NL + k][threadIdx.x] = h[0][j][k];
         const uint32_t fresh = begins >> (v * U) & ((1 << U) - 1);
         float delta[U];
-        bool held = false;
+        bool careful = false;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
           delta[e] = step_size(now.dt[e], ok);
-          held = held || (ok && delta[e] == 0.f);
+          careful = careful || (ok && !(delta[e] > 0.f));
         }
-        const auto step = [&](int e, auto slow) {
+        if (__float_as_int(rate) > 0) careful = careful || delta[0] * rate > 127.f || delta[1] * rate > 127.f;
+        careful = any(careful);
+        const auto step = [&](int e, auto way) {
           float d[4], u[4], B[NL];
           now.B[e].get(B);
           own.mask(B);
           quads(delta[e], d);
-          quads(slow() ? mul_or_0(delta[e], value1<TYPE>(now.x[e])) : delta[e] * value1<TYPE>(now.x[e]), u);
+          quads(way() == CAREFUL ? mul_or_0(delta[e], value1<TYPE>(now.x[e])) : delta[e] * value1<TYPE>(now.x[e]), u);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int k = 0; k < NL; ++k)  // B may hold anything where a column's step has size 0
-              h[0][j][k] = fmaf(__builtin_amdgcn_exp2f(d[j] * A[j][k]), slow() && fresh >> e & 1 ? 0.f : h[0][j][k],
-                                slow() ? mul_or_0(u[j], B[k]) : u[j] * B[k]);
+            for (int k = 0; k < NL; ++k) {
+              const float keep = __builtin_amdgcn_exp2f(d[j] * A[j][k]), b = way() == CAREFUL ? mul_or_0(u[j], B[k]) : u[j] * B[k];
+              h[0][j][k] = fmaf(way() == CAREFUL ? passed(keep) : keep, h[0][j][k], b);
+            }
         };
-        if (!fresh && !any(held)) {
+        if (!fresh && !careful) {
 #pragma unroll
-          for (int e = 0; e < U; ++e) step(e, std::false_type());
+          for (int e = 0; e < U; ++e) step(e, Int<PLAIN>());
         } else {
 #pragma unroll
-          for (int e = 0; e < U; ++e) step(e, std::true_type());
+          for (int e = 0; e < U; ++e) {
+            if (fresh >> e & 1) zero(h[0]);
+            if (careful) step(e, Int<CAREFUL>());
+            else step(e, Int<PLAIN>());
+          }
         }
       }
       float dA[4][NL], sD = 0.f, sb = 0.f;
@@ -334,11 +355,11 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           }
         }
         float delta[U], ov[U], sz[U], f[U][4][NL], tB[U], tA[U], ty[U], p[U][2 * NL];
-        bool held = false;
+        bool careful = false;
 #pragma unroll
         for (int e = 0; e < U; ++e) {
           delta[e] = step_size(r.dt[e], ok);
-          held = held || (ok && delta[e] == 0.f);
+          careful = careful || (ok && !(delta[e] > 0.f));
           ov[e] = value1<TYPE>(r.o[e]);
           if (GATE) {
             const float z = value1<TYPE>(r.z[e]);
@@ -348,8 +369,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           // a step that is not there changes nothing
           if (!ok || e >= m) delta[e] = ov[e] = 0.f;
         }
+        if (__float_as_int(rate) > 0) careful = careful || delta[0] * rate > 127.f || delta[1] * rate > 127.f;
+        careful = any(careful);
         const auto input = [&](int e) { return mul_or_0(delta[e], value1<TYPE>(r.x[e])); };
-        const auto forth = [&](int e, auto first, auto some_held) {
+        const auto forth = [&](int e, auto first, auto way) {
           float d[4], u[4], B[NL];
           r.B[e].get(B);
           own.mask(B);
@@ -359,16 +382,17 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int k = 0; k < NL; ++k) {
-              // B may hold anything where a column's step has size 0
-              const float b = some_held() ? mul_or_0(u[j], B[k]) : u[j] * B[k];
-              f[e][j][k] = first() ? 0.f : __builtin_amdgcn_exp2f(d[j] * A[j][k]);
+              const float b = way() == CAREFUL ? mul_or_0(u[j], B[k]) : u[j] * B[k];
+              const float keep = first() ? 0.f : __builtin_amdgcn_exp2f(d[j] * A[j][k]);
+              f[e][j][k] = way() == CAREFUL ? passed(keep) : keep;
               h[e + 1][j][k] = first() ? b : fmaf(f[e][j][k], h[e][j][k], b);
             }
           __builtin_amdgcn_sched_barrier(0);
         };
         const auto forth_any = [&](int e) {
-          if (fresh[e]) forth(e, std::true_type(), std::true_type());
-          else forth(e, std::false_type(), std::true_type());
+          if (fresh[e]) forth(e, std::true_type(), Int<CAREFUL>());
+          else if (careful) forth(e, std::false_type(), Int<CAREFUL>());
+          else forth(e, std::false_type(), Int<PLAIN>());
         };
         const auto back = [&](int e) {
           float B[NL], Cn[NL], d[4], u[4], ot[4], sB[4], sA[4], y[4];
@@ -402,15 +426,9 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
           Sums()(p[e]);
           __builtin_amdgcn_sched_barrier(0);
         };
-        const auto zero = [](float (&v)[4][NL]) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int k = 0; k < NL; ++k) v[j][k] = 0.f;
-        };
-        if (!any(held) && !fresh[0] && !fresh[1]) {
-          forth(0, std::false_type(), std::false_type());
-          forth(1, std::false_type(), std::false_type());
+        if (!careful && !fresh[0] && !fresh[1]) {
+          forth(0, std::false_type(), Int<PLAIN>());
+          forth(1, std::false_type(), Int<PLAIN>());
         } else {
           forth_any(0);
           forth_any(1);
