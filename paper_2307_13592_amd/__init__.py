@@ -667,14 +667,15 @@ def mgn_causal_conv_grad(x, weight, dy, dx, dweight=None, dbias=None, bias=None,
     overwritten or added to) and d_past (float32), each of them or None.  work:
     float32 scratch of MGN_CONV_PARTS * cols * (width + 1) for dweight and dbias
     (None: allocated)."""
-    _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_past_out, starts, silu, accumulate, work,
-                      stream)()
+    call, keep = _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_past_out, starts, silu,
+                                   accumulate, work, stream)
+    _run(*call)
 
 
 def _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_past_out, starts, silu, accumulate, work,
                       stream):
-    """The binding's checks of mgn_causal_conv_grad now, its launch when the result is
-    called: so that of several calls none runs if one would be refused."""
+    """The checks and marshalling of mgn_causal_conv_grad: _run's arguments, and last the
+    scratch that it keeps.  (Of several calls in a row none runs if one would be refused.)"""
     import torch
     shape, dev, width, before, head = _conv_args(x, weight, bias, past, starts)
     T, rows, cols = shape
@@ -687,7 +688,7 @@ def _causal_conv_grad(x, weight, dy, dx, dweight, dbias, bias, past, d_past, d_p
             rows, cols, 1 if silu else 0, _need(_arr(dx, "dx", x.dtype, shape, dev), "dx"),
             _arr(dweight, "dweight", f32, (cols, width), dev), _arr(dbias, "dbias", f32, (cols,), dev),
             1 if accumulate else 0, _arr(d_past, "d_past", f32, before, dev), pw)
-    return lambda _=keep: _run("mgn_causal_conv_grad", dev, stream, *args)
+    return ("mgn_causal_conv_grad", dev, stream, *args), keep
 
 
 @functools.lru_cache(maxsize=256)
@@ -741,7 +742,8 @@ def mgn_selective_scan(x, dt, A, B, C, y, D=None, dt_bias=None, z=None, h0=None,
     float32 [rows][cols][n] or None; marks of mgn_selective_marks, for the backward;
     starts: uint8 [steps].  work: device scratch of mgn_selective_scan_work bytes
     (None: allocated)."""
-    _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts, softplus, work, stream)()
+    call, keep = _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts, softplus, work, stream)
+    _run(*call)
 
 
 def _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts, softplus, work, stream):
@@ -754,7 +756,7 @@ def _selective_scan(x, dt, A, B, C, y, D, dt_bias, z, h0, h_last, marks, starts,
     args = (_byref(s), _arr(h0, "h0", f32, state, dev), _need(_arr(y, "y", x.dtype, shape, dev), "y"),
             _arr(h_last, "h_last", f32, state, dev), _arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev),
             pw, nb)
-    return lambda _=keep: _run("mgn_selective_scan", dev, stream, *args)
+    return ("mgn_selective_scan", dev, stream, *args), keep
 
 
 def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=None, d_bias=None, dz=None, D=None,
@@ -765,8 +767,9 @@ def mgn_selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD=N
     dA, dD, d_bias (float32, overwritten or added to, each of them or None); dh0
     (float32, or None; it may be dh_last).  work: device scratch of
     mgn_selective_scan_grad_work bytes (None: allocated)."""
-    _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_bias, dz, D, dt_bias, z, dh_last, dh0,
-                         starts, softplus, accumulate, work, stream)()
+    call, keep = _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_bias, dz, D, dt_bias, z,
+                                      dh_last, dh0, starts, softplus, accumulate, work, stream)
+    _run(*call)
 
 
 def _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_bias, dz, D, dt_bias, z, dh_last, dh0,
@@ -786,7 +789,7 @@ def _selective_scan_grad(x, dt, A, B, C, marks, dy, dx, ddt, dA, dB, dC, dD, d_b
     args = (_byref(s), _need(_arr(marks, "marks", f32, (-(-T // MGN_MARK_STEPS),) + state, dev), "marks"),
             _need(_arr(dy, "dy", ty, shape, dev), "dy"), _arr(dh_last, "dh_last", f32, state, dev), _byref(g),
             _arr(dh0, "dh0", f32, state, dev), pw, nb)
-    return lambda _=keep: _run("mgn_selective_scan_grad", dev, stream, *args)
+    return ("mgn_selective_scan_grad", dev, stream, *args), keep
 
 
 def _apart(fn: str, read, written) -> None:

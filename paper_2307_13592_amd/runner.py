@@ -11,7 +11,7 @@ from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_d
                mgn_norm_accumulate, mgn_norm_apply, MGN_NORM_WORK_PER_COL, mgn_rollout_update, mgn_set_h1_stash,
                mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
                mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on, mgn_causal_conv,
-               mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad, mgn_selective_marks, _apart,
+               mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad, mgn_selective_marks, _apart, _run,
                _causal_conv_grad, _selective_scan, _selective_scan_grad)
 
 
@@ -381,7 +381,7 @@ class SelectiveMemory:
         if dt is None or B is None or C is None:
             raise ValueError("dt, B, C: not given")
         u, y = self._out[0], self._out[1]
-        self._run(x[None], u, dt[None], B[None], C[None], y, None if z is None else z[None], None, None, stream)
+        self._advance(x[None], u, dt[None], B[None], C[None], y, None if z is None else z[None], None, None, stream)
         return y[0]
 
     def scan(self, x, dt, B, C, z=None, starts=None, stream=None):
@@ -390,17 +390,17 @@ class SelectiveMemory:
         with _on(stream, x.device):
             u, y, past = torch.empty_like(x), torch.empty_like(x), self.past.clone()
         marks = mgn_selective_marks(x, self.A, stream)
-        self._run(x, u, dt, B, C, y, z, marks, starts, stream)
+        self._advance(x, u, dt, B, C, y, z, marks, starts, stream)
         return y, (past, u, marks)
 
-    def _run(self, x, u, dt, B, C, y, z, marks, starts, stream):
+    def _advance(self, x, u, dt, B, C, y, z, marks, starts, stream):
         """The convolution into u and the scan into y.  The convolution moves `past`
         on, so the scan's arguments are checked before it."""
-        scan = _selective_scan(u, dt, self.A, B, C, y, self.D, self.dt_bias, z, self.state, self.state, marks, starts,
-                               True, None, stream)
+        scan, keep = _selective_scan(u, dt, self.A, B, C, y, self.D, self.dt_bias, z, self.state, self.state, marks, starts,
+                                     True, None, stream)
         _apart("mgn_selective_scan", (dt, B, C, z, starts), (self.past, y, self.state))
         mgn_causal_conv(x, self.conv_weight, u, self.conv_bias, self.past, self.past, starts, True, stream)
-        scan()
+        _run(*scan)
 
     def grad(self, x, dt, B, C, kept, dy, z=None, starts=None, dh_last=None, d_past=None, accumulate: bool = False,
              stream=None):
@@ -415,11 +415,11 @@ class SelectiveMemory:
             d_before = torch.empty(past.shape, dtype=torch.float32, device=x.device)
         p, g = self, self.grads
         # (the scan's part of the gradients is not added before the convolution's arguments are checked)
-        scan = _selective_scan_grad(u, dt, p.A, B, C, marks, dy, du, ddt, g["A"], dB, dC, g["D"], g["dt_bias"], dz, p.D,
-                                    p.dt_bias, z, dh_last, dh0, starts, True, accumulate, None, stream)
-        conv = _causal_conv_grad(x, p.conv_weight, du, dx, g["conv_weight"], g["conv_bias"], p.conv_bias, past, d_before,
-                                 d_past, starts, True, accumulate, None, stream)
+        scan, keep = _selective_scan_grad(u, dt, p.A, B, C, marks, dy, du, ddt, g["A"], dB, dC, g["D"], g["dt_bias"], dz,
+                                          p.D, p.dt_bias, z, dh_last, dh0, starts, True, accumulate, None, stream)
+        conv, keep2 = _causal_conv_grad(x, p.conv_weight, du, dx, g["conv_weight"], g["conv_bias"], p.conv_bias, past,
+                                        d_before, d_past, starts, True, accumulate, None, stream)
         _apart("mgn_causal_conv_grad", (x, starts, d_past), g.values())
-        scan()
-        conv()
+        _run(*scan)
+        _run(*conv)
         return dict(dx=dx, ddt=ddt, dB=dB, dC=dC, dz=dz, dh0=dh0, d_past=d_before)
