@@ -246,11 +246,19 @@ def mgn_set_params(model, params, stream=None) -> None:
         _check(lib().mgn_set_params(model, p, 0, _stream(stream)), model)
 
 
-def mgn_sgd_step(model, grad, lr: float, stream=None) -> None:
-    """params -= lr * grad on the device (grad: float32 device tensor)."""
+def _sgd_args(model, grad, lr: float):
+    """Checked arguments of mgn_sgd_step (the C ABI takes no type and no length)."""
+    import torch
     if grad.numel() != mgn_param_count(model):
         raise ValueError("gradient vector has the wrong length")
-    _check(lib().mgn_sgd_step(model, _dev(grad), float(lr), _stream(stream)), model)
+    if not np.isfinite(C.c_float(lr).value):
+        raise MgnError(MGN_E_ARG, "mgn_sgd_step: learning rate is not finite")
+    return _devt(grad, torch.float32, "grad"), float(lr)
+
+
+def mgn_sgd_step(model, grad, lr: float, stream=None) -> None:
+    """params -= lr * grad on the device (grad: float32 device tensor)."""
+    _check(lib().mgn_sgd_step(model, *_sgd_args(model, grad, lr), _stream(stream)), model)
 
 
 def mgn_get_params(model, stream=None) -> np.ndarray:

@@ -17,7 +17,7 @@ import numpy as np
 import torch
 
 from . import (mgn_halo_masks, mgn_lockstep_backward, mgn_lockstep_backward8, mgn_lockstep_forward,
-               mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step, _on)
+               mgn_lockstep_forward8, mgn_mse_grad_global, mgn_sgd_step, _on, _sgd_args)
 from .runner import LatentCache, Session, clip_grads
 
 
@@ -115,6 +115,8 @@ class Lockstep:
         """Every part's model takes the same update with the summed gradient,
         so the parts' parameters stay identical.  max_norm: that gradient is first
         scaled, in place, to at most this norm; returns the norm that it had."""
+        for s in self.sessions:
+            _sgd_args(s.model, self.d_params, lr)  # before the gradient is scaled
         norm = None if max_norm is None else clip_grads([self.d_params], max_norm, stream)
         for s in self.sessions:
             mgn_sgd_step(s.model, self.d_params, lr, stream)

@@ -12,7 +12,7 @@ from . import (MGN_BF16, MGN_FP32, graph_struct, mgn_backward, mgn_create, mgn_d
                mgn_set_inference, mgn_sgd_step, mgn_workspace_size, mgn_gated_scan, mgn_gated_scan_grad, mgn_rms_norm,
                mgn_rms_norm_grad, mgn_rows_load8, mgn_rows_store8, rows8_blocks, _on, mgn_causal_conv,
                mgn_grad_clip, mgn_grad_list, mgn_layer_norm, mgn_layer_norm_grad, mgn_selective_marks, _apart, _run,
-               _causal_conv_grad, _selective_scan, _selective_scan_grad)
+               _causal_conv_grad, _selective_scan, _selective_scan_grad, _sgd_args)
 
 
 class Session:
@@ -105,8 +105,7 @@ class Session:
         not finite in float32).  Returns the norm that it had (float32 [1] on the
         device; None without max_norm)."""
         grad = self.d_params if grad is None else grad
-        if grad.numel() != self.n_params:
-            raise ValueError("gradient vector has the wrong length")
+        _sgd_args(self.model, grad, lr)  # before grad is scaled
         norm = None if max_norm is None else clip_grads([grad], max_norm, stream)
         mgn_sgd_step(self.model, grad, lr, stream)
         return norm
