@@ -280,12 +280,15 @@ hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
     }
     return e;
   };
-  if constexpr (PASS == MANY_ROWS) return go(Int<4>());
-  if (a.n <= 4) return go(Int<1>());
-  if (a.n <= 8) return go(Int<2>());
-  if (a.n <= 16) return go(Int<4>());
-  if (a.n <= 32) return go(Int<8>());
-  return go(Int<16>());
+  if constexpr (PASS == MANY_ROWS) {
+    return go(Int<4>());
+  } else {
+    if (a.n <= 4) return go(Int<1>());
+    if (a.n <= 8) return go(Int<2>());
+    if (a.n <= 16) return go(Int<4>());
+    if (a.n <= 32) return go(Int<8>());
+    return go(Int<16>());
+  }
 }
 
 template <int TYPE>
