@@ -23,9 +23,9 @@ constexpr int RUN = 16, AT_ONCE = 4;   // bytes of a thread's access, and access
 constexpr int64_t WGS = 1536;           // workgroups of a norm launch with one table
 constexpr int64_t WGS_MANY = 256;       // with several
 // Partials, and tiles, above which a launch of its own adds the partials and a scaling
-// workgroup takes one tile: 480M bf16 values in 24 tensors 515 us, against 537 with
-// 16,384 workgroups that take several in turn and add the partials themselves, 572
-// with 4,096.  A model's 190 tensors (1.8M values) 12 us without that launch.
+// workgroup takes one tile: 480M bf16 values in 24 tensors 507 us (515 when 16,384
+// workgroups that take several in turn and add the partials themselves took 537, and
+// 4,096 572).  A model's 190 tensors (1.8M values) 12 us without that launch.
 constexpr int64_t FOLD = 4096, FOLD_TILES = 16384, CLIP_WGS = 1 << 22;
 
 // The tensor that holds a tile: how many of the tensors begin at or before it, each

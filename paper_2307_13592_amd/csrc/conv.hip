@@ -14,8 +14,8 @@
 // again from the inputs that it holds.
 //
 // Bound by memory.  20 steps of 100,003 x 64 bf16, 4 taps, 91 us (5.6 TB/s); the
-// backward of 600 steps of 1,885 x 128 fp32 350 us (5.0 TB/s).  8 columns a lane took
-// 129 us of then 117; 2 steps a unit in the backward 389 of 350 (fp32).
+// backward of 600 steps of 1,885 x 128 fp32 348 us (5.0 TB/s), bf16 222 (3.9: two waves a
+// SIMD keep too few bytes in flight).  8 columns a lane took 129 us of then 117.
 #include <type_traits>
 
 #include "raw.h"
@@ -516,8 +516,10 @@ hipError_t launch_conv_grad(ConvArgs a, int type, int width, float* dw, float* d
     const dim3 grid((unsigned)parts, (unsigned)a.tiles);
     const hipError_t e = by_width(width, [&](auto w) {
       const auto go = [&](auto ty) {
-        // (4 taps with 2 steps: fp32 389 us of 350, bf16 249 of 260; more taps leave no
-        // registers for 4)
+        // (fp32, 4 taps, with 2 steps: 600 steps of 1,885 x 128 387 us, 348 with 4; 20 of
+        // 100,003 x 64 330 and 314.  bf16 is of two minds: 222 and 222, 214 and 206, but 100
+        // of 20,003 x 64 172 and 200, and 2 taps 150 and 182.  More taps than 4 leave no
+        // registers for 4 steps.)
         constexpr int STEPS = w() > 4 ? 2 : 4;
         if (near) hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), STEPS, true>), grid, dim3(NT), 0, st, a);
         else hipLaunchKernelGGL((conv_grad_kernel<ty(), w(), 2, false>), grid, dim3(NT), 0, st, a);

@@ -10,7 +10,8 @@
 // of the deviations from the mean as it was rounded, so an offset costs no digits,
 // and what that rounding left, the mean of the deviations, is taken off in the same
 // pass: a row of equal values is its bias.  2M x 128 bf16 rows with a residual 336 us
-// (6.1 TB/s), the backward of 1M x 128 fp32 rows 361 us (5.7).
+// (6.1 TB/s), into 8-bit rows 286 (6.3); the backward of 1M x 128 fp32 rows 361 us (5.7),
+// bf16 188 (5.4).
 #include "row_deal.h"
 
 namespace mgn {

@@ -14,9 +14,9 @@
 // Bound by the vector units: 4 products and sums and an exponential, which takes two
 // instructions' time, for a state and step, and some 60 instructions a step for what is
 // done once a column and for the exchanges, against 6 - 16 bytes an element.  600 steps
-// of 1,885 x 64 bf16, 16 states, 400 us (the units busy 76 %: some SIMDs have one wave,
-// some two), 466 where loads stood in branches; 20 steps of 20,011 x 64 133 us.  With
-// one step by the states' 8 n bytes: 1,885 x 128 fp32 7.3 us, 4.7 TB/s.
+// of 1,885 x 64 bf16, 16 states, 404 us (the units busy 75 %: some SIMDs have one wave,
+// some two); 20 steps of 20,011 x 64 141 us (81 %).  With one step by the states' 8 n
+// bytes: 1,885 x 128 fp32 7.0 us, 4.9 TB/s.
 #include "ssm.h"
 
 namespace mgn {
@@ -35,8 +35,8 @@ struct Inputs {
 template <int TYPE, int NL, bool FULL, int PASS>
 __global__ __launch_bounds__(NT) void ssm_kernel(SsmArgs a) {
   // Steps whose loads are in flight together.  With many rows two of them and a third
-  // wave in a SIMD's registers: 20 steps of 20,011 x 64 bf16 135 us, 161 with four;
-  // 600 steps of 1,885 x 64, two waves a SIMD in any case, 418 and 411.
+  // wave in a SIMD's registers: 20 steps of 20,011 x 64 bf16 141 us, 163 with four (fp32
+  // 140 and 163); otherwise four: 600 steps of 1,885 x 64 404 us, 424 with two (396, 441).
   constexpr int STEPS = PASS == ONE_STEP || NL == 16 ? 1 : NL == 8 || (NL == 4 && PASS == MANY_ROWS) ? 2 : 4;
   using E = Elem<TYPE>;
   using In = Inputs<TYPE, NL, STEPS>;
@@ -274,6 +274,10 @@ hipError_t launch_pass(SsmArgs a, int64_t chunks, hipStream_t st) {
     for (a.group0 = 0; a.group0 < groups && e == hipSuccess; a.group0 += LAUNCH) {
       const int64_t n = groups - a.group0 < LAUNCH ? groups - a.group0 : LAUNCH;
       const dim3 grid((unsigned)((n * 4 + NT - 1) / NT), (unsigned)chunks);
+      // All states there: no run is masked.  100 steps of 4,000 x 64, 16 states, bf16 133 us,
+      // 148 as if some were missing, fp32 150 and 177; 32 bf16 222, 245, fp32 278, 234 (the
+      // one slower here: over 256 registers, one wave a SIMD); 64 513, 545 and 538, 556; 4
+      // 70, 71, 8 91, 95; one step of 1,885 x 128, 16 states, 10.5 and 14.4 with the call.
       if (a.n == 4 * NL) hipLaunchKernelGGL((ssm_kernel<TYPE, NL, true, PASS>), grid, dim3(NT), 0, st, a);
       else hipLaunchKernelGGL((ssm_kernel<TYPE, NL, false, PASS>), grid, dim3(NT), 0, st, a);
       e = hipGetLastError();

@@ -17,10 +17,12 @@
 // in fp64.  With few columns the time axis is cut into chunks as in the forward.
 //
 // Bound by the vector units: 15 instructions and two exponentials a state and step (the
-// states before a unit are formed first, then its own again).  20
-// steps of 20,011 x 64 bf16, 16 states, 490 us, the units busy 77 % of them with the two
-// waves a SIMD that 256 registers leave; 570 without a unit's loads ahead.  A unit of 4
-// steps spills (1.3 ms and more).
+// states before a unit are formed first, then its own again).  20 steps of 20,011 x 64
+// bf16, 16 states, 482 - 495 us under the profiler, the units busy 77 % of them with the
+// two waves a SIMD that 256 registers leave.  Most forms of more than 8 states spill some:
+// 8 registers here, 18 in fp32, 41 at most (2 waves, tiles of 4 groups, fp32).  That is
+// what the last unit's and the sweep's loads ahead cost, and still the faster way: 570 us
+// without.  A unit of 4 steps spills much more (1.3 ms and more).
 #include "ssm.h"
 
 namespace mgn {
@@ -596,8 +598,12 @@ Deal deal(int64_t steps, int64_t rows, int cols, int n) {
   return d;
 }
 
-// Calls f(NL, NW, FULL): states of a lane, waves that share a column's, whether
-// they are all there.
+// Calls f(NL, NW, FULL): states of a lane, waves that share a column's, whether they are
+// all there, so that no run is masked, which is faster though it spills more: forward and
+// backward of 20 steps of 20,011 x 64, 16 states, bf16 611 us, 737 as if some were
+// missing, fp32 651 and 754; 100 steps of 1,000 x 128, 32 states, 794, 931 and 907, 940;
+// 64 1,289, 1,658 and 1,382, 1,677.  (4 and 8: 228, 230 and 248, 259; their backward has
+// the general form only.)
 template <class F>
 hipError_t by_states(int n, F f) {
   const std::false_type part;
