@@ -409,8 +409,9 @@ mgn_status mgn_selective_scan(const mgn_ssm* s, const float* h0, void* y, float*
                               size_t work_bytes, mgn_stream stream);
 /* Its backward, from the forward's arguments, its marks, dy (x's type) and dh_last
  * (fp32 [rows][cols][n] = dL/dh_last, NULL: zeros): dx, ddt, dB, dC and (with z) dz
- * in x's type; dA, dD and d_bias fp32, each NULL if not wanted, overwritten or added
- * to when accumulate != 0; dh0 (NULL: not wanted; it may be dh_last) = dL/dh0.
+ * in x's type; dA, dD and d_bias fp32 (at zeros for a D or dt_bias that is NULL), each
+ * NULL if not wanted, overwritten or added to when accumulate != 0; dh0 (NULL: not
+ * wanted; it may be dh_last) = dL/dh0.
  * A step of size 0 gives x and B no gradient, nor dt where its softplus is level; with
  * dy = 0 there too, no gradient takes anything from what x and B hold (C and z are
  * finite).  A nonzero gradient grows on its way back only so far as a state may; a step

@@ -489,8 +489,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ssm_grad_kernel(SsmArgs a) {
             }
             const float x = value1<TYPE>(r.x[e]);
             float dx = mul_or_0(delta[e], tB[e]), dd = fmaf(tA[e], LN2, tB[e] * x);
-            // (x may hold anything at a step of size 0 that no gradient reaches)
-            if (a.D) dx = fmaf(D, ov[e], dx), sD += mul_or_0(ov[e], x);
+            if (a.D) dx = fmaf(D, ov[e], dx);
+            // (x may hold anything at a step of size 0 that no gradient reaches; a D that is
+            // left out has a gradient too)
+            sD += mul_or_0(ov[e], x);
             if (a.softplus) dd = mul_or_0(sigmoid(value1<TYPE>(r.dt[e]) + bias), dd);
             sb += dd;
             write1<TYPE>((char*)a.dx + (xu + e * cb), o, dx);
