@@ -414,9 +414,9 @@ mgn_status mgn_selective_scan(const mgn_ssm* s, const float* h0, void* y, float*
  * wanted; it may be dh_last) = dL/dh0.
  * A step of size 0 gives x and B no gradient, nor dt where its softplus is level; with
  * dy = 0 there too, no gradient takes anything from what x and B hold (C and z are
- * finite; without softplus ddt and d_bias do).  A nonzero gradient grows on its way back only so far as a state may; a step
- * whose own factor exp(delta A) passes the fp32 range (of zero states, by the above)
- * passes none on to the states before it. */
+ * finite; without softplus ddt and d_bias do).  A nonzero gradient grows on its way
+ * back only so far as a state may; a step whose own factor exp(delta A) passes the fp32
+ * range (of zero states, by the above) passes none on to the states before it. */
 typedef struct {
   void *dx, *ddt, *dB, *dC, *dz;
   float *dA, *dD, *d_bias;
